@@ -76,6 +76,15 @@ class CostaTiming(ctypes.Structure):
     _fields_ = [("ms", ctypes.c_double * 4), ("launches", _i64 * 4), ("bytes", _i64 * 4)]
 
 
+class CostaMatrix(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int), ("order", ctypes.c_int), ("rows", _i64), ("cols", _i64), ("ld", _i64),
+                ("data", _vp)]
+
+
+class CostaMx(ctypes.Structure):
+    _fields_ = [("format", ctypes.c_int), ("rows", _i64), ("cols", _i64), ("data", _vp), ("scales", _vp)]
+
+
 _SIGS = {
     "costa_layout_create": [_i64, _i64, _i32, _vp, _i32, _vp, _vp, _i32, ctypes.c_int, _vp, _vp, _P(_vp)],
     "costa_layout_create_block_cyclic": [_i64, _i64, _i64, _i64, _i32, _i32, ctypes.c_int, ctypes.c_int, _P(_vp)],
@@ -110,6 +119,15 @@ _SIGS = {
     "costa_timing_enable": [ctypes.c_int],
     "costa_timing_read": [_P(CostaTiming)],
     "costa_finalize": [],
+    "costa_mx_sizes": [ctypes.c_int, _i64, _i64, _P(_i64), _P(_i64)],
+    "costa_mx_quantize": [ctypes.c_float, _P(CostaMatrix), _P(CostaMx), _P(CostaMx), _vp],
+    "costa_mx_quantize_layout": [ctypes.c_int, ctypes.c_float, _vp, _vp, _P(CostaMx), _P(CostaMx), _vp],
+    "costa_mx_dequantize": [ctypes.c_float, _P(CostaMx), ctypes.c_float, _P(CostaMatrix), _vp],
+    "costa_mx_product": [ctypes.c_float, _P(CostaMx), _P(CostaMx), ctypes.c_float, _P(CostaMatrix), _vp,
+                         ctypes.c_size_t, _vp],
+    "costa_mx_product_real": [ctypes.c_float, ctypes.c_int, _P(CostaMatrix), _P(CostaMx), ctypes.c_float,
+                              _P(CostaMatrix), _vp, ctypes.c_size_t, _vp],
+    "costa_mx_workspace": [_i64, _i64, _i64, _P(ctypes.c_size_t)],
 }
 for _name, _args in _SIGS.items():
     _f = getattr(_lib, _name)
@@ -501,6 +519,121 @@ def costa_pztranu(m, n, alpha, a, ia, ja, desca, grida, beta, c, ic, jc, descc, 
 def costa_pztranc(m, n, alpha, a, ia, ja, desca, grida, beta, c, ic, jc, descc, gridc, stream=None) -> None:
     _pxtran_named("costa_pztranc", "c128", m, n, alpha, a, ia, ja, desca, grida, beta, c, ic, jc, descc, gridc,
                   stream)
+
+
+# ---------------------------------------------------------------------------
+# microscaled matrices (include/costa_mx.h)
+# ---------------------------------------------------------------------------
+MX_FORMATS = {4: 0, 8: 1}  # bits of an element: E2M1, E4M3
+REALS = {"f64": 0, "f32": 1, "bf16": 2, "f16": 3}
+_REAL_OF = {} if torch is None else {torch.float64: 0, torch.float32: 1, torch.bfloat16: 2, torch.float16: 3}
+
+
+def costa_mx_sizes(bits: int, rows: int, cols: int):
+    """(data bytes, scale bytes) of a rows x cols matrix."""
+    d, s = _i64(), _i64()
+    _check(_lib.costa_mx_sizes(MX_FORMATS[bits], rows, cols, ctypes.byref(d), ctypes.byref(s)), "costa_mx_sizes")
+    return d.value, s.value
+
+
+class MxMatrix:
+    """A microscaled matrix over two uint8 device tensors, any shape, that hold
+    costa_mx_sizes() bytes (kept alive by this object)."""
+
+    def __init__(self, bits: int, rows: int, cols: int, data, scales):
+        need = costa_mx_sizes(bits, rows, cols)
+        for t, n, what in ((data, need[0], "data"), (scales, need[1], "scales")):
+            if t.dtype != torch.uint8 or not t.is_contiguous() or not t.is_cuda:
+                raise ValueError(f"{what}: a contiguous uint8 tensor on the GPU is needed")
+            if t.numel() < n:
+                raise ValueError(f"{what}: {t.numel()} bytes, {n} are needed")
+        self.bits, self.rows, self.cols, self.data, self.scales = bits, rows, cols, data, scales
+        self._c = CostaMx(MX_FORMATS[bits], rows, cols, data.data_ptr() or None, scales.data_ptr() or None)
+        self._ref = ctypes.pointer(self._c)
+
+    @classmethod
+    def empty(cls, bits: int, rows: int, cols: int, device="cuda") -> "MxMatrix":
+        d, s = costa_mx_sizes(bits, rows, cols)
+        return cls(bits, rows, cols, torch.empty(d, dtype=torch.uint8, device=device),
+                   torch.empty(s, dtype=torch.uint8, device=device))
+
+
+def _mx(q):
+    return None if q is None else q._ref
+
+
+def _matrix(t) -> CostaMatrix:
+    """The view of a 2-D tensor on the GPU that has unit stride in one dimension."""
+    real = _REAL_OF.get(t.dtype)
+    if real is None or t.dim() != 2 or not t.is_cuda:
+        raise ValueError("a 2-D float64, float32, bfloat16 or float16 tensor on the GPU is needed")
+    (rows, cols), (s0, s1) = t.shape, t.stride()
+    if s1 == 1 or cols <= 1:
+        return CostaMatrix(real, 1, rows, cols, s0 if rows > 1 else max(1, cols), t.data_ptr() or None)
+    if s0 == 1 or rows <= 1:
+        return CostaMatrix(real, 0, rows, cols, s1, t.data_ptr() or None)
+    raise ValueError(f"strides {s0}, {s1}: one of them has to be 1")
+
+
+def costa_mx_quantize(alpha: float, B, Q: Optional[MxMatrix] = None, QT: Optional[MxMatrix] = None,
+                      stream=None) -> None:
+    """Q <- mx(alpha B) and QT <- mx(alpha B^T), either or both; B a 2-D tensor."""
+    _check(_lib.costa_mx_quantize(alpha, _matrix(B), _mx(Q), _mx(QT), _stream(stream)), "costa_mx_quantize")
+
+
+def costa_mx_quantize_layout(type: str, alpha: float, B, B_local: Sequence, Q: Optional[MxMatrix] = None,
+                             QT: Optional[MxMatrix] = None, stream=None) -> None:
+    """The same out of the ranks' buffers of layout B; type: "f64", "f32", "bf16" or "f16"."""
+    keep: List = []
+    _check(_lib.costa_mx_quantize_layout(REALS[type], alpha, _h(B), _pointers(B_local, keep), _mx(Q), _mx(QT),
+                                         _stream(stream)), "costa_mx_quantize_layout")
+
+
+def costa_mx_dequantize(alpha: float, Q: MxMatrix, beta: float, A, stream=None) -> None:
+    """A <- alpha Q^ + beta A; A a 2-D tensor."""
+    _check(_lib.costa_mx_dequantize(alpha, _mx(Q), beta, _matrix(A), _stream(stream)), "costa_mx_dequantize")
+
+
+def costa_mx_workspace(m: int, n: int, k: int) -> int:
+    b = ctypes.c_size_t()
+    _check(_lib.costa_mx_workspace(m, n, k, ctypes.byref(b)), "costa_mx_workspace")
+    return b.value
+
+
+def _product_workspace(m: int, n: int, k: int, workspace, device, stream):
+    """(address, bytes, tensor to keep until the call returns) of a product's
+    workspace: the caller's uint8 tensor, or one from torch's allocator.  That
+    one belongs to torch's current stream; it is marked as used on `stream`
+    where the call runs on another."""
+    if workspace is None:
+        n = costa_mx_workspace(m, n, k)
+        if n == 0:
+            return None, 0, None
+        workspace = torch.empty(n, dtype=torch.uint8, device=device)
+        if stream is not None:
+            at = _stream(stream)
+            if at != torch.cuda.current_stream().cuda_stream:
+                workspace.record_stream(torch.cuda.ExternalStream(at) if at else torch.cuda.default_stream())
+    elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or not workspace.is_cuda:
+        raise ValueError("workspace: a contiguous uint8 tensor on the GPU is needed")
+    return workspace.data_ptr() or None, workspace.numel(), workspace
+
+
+def costa_mx_product(alpha: float, A: MxMatrix, B: MxMatrix, beta: float, C, workspace=None, stream=None) -> None:
+    """C <- alpha A^ B^^T + beta C; C a 2-D tensor.  workspace: a uint8 tensor
+    (by default costa_mx_workspace() bytes from torch's allocator, where any)."""
+    at, size, _keep = _product_workspace(A.rows, B.rows, A.cols, workspace, C.device, stream)
+    _check(_lib.costa_mx_product(alpha, _mx(A), _mx(B), beta, _matrix(C), at, size, _stream(stream)),
+           "costa_mx_product")
+
+
+def costa_mx_product_real(alpha: float, op: str, A, B: MxMatrix, beta: float, C, workspace=None,
+                          stream=None) -> None:
+    """C <- alpha op(A) B^^T + beta C; A and C 2-D tensors."""
+    m, k = A.shape if op == "N" else A.shape[::-1]
+    at, size, _keep = _product_workspace(m, B.rows, k, workspace, C.device, stream)
+    _check(_lib.costa_mx_product_real(alpha, OPS[op], _matrix(A), _mx(B), beta, _matrix(C), at, size,
+                                      _stream(stream)), "costa_mx_product_real")
 
 
 def costa_set_workspace_limit(nbytes: int) -> None:

@@ -12,6 +12,7 @@
 #include <string>
 
 #include "index_math.hpp"
+#include "mx.hpp"
 #include "plan.hpp"
 
 namespace costa {
@@ -1503,6 +1504,7 @@ extern "C" costa_status costa_finalize(void) {
     // outside the state lock: a ScaLAPACK-style call takes the layout cache's
     // lock and then the state lock, never the other way round
     release_scalapack_layouts();
+    release_mx_tables();
     return COSTA_SUCCESS;
   });
 }

@@ -1,0 +1,146 @@
+"""Microscaled matrices without a GPU: exported symbols, sizes, and what each
+call refuses before any device work."""
+import ctypes
+import os
+import re
+
+import numpy as np
+import pytest
+
+C = pytest.importorskip("paper_2106_06601_amd")
+import mx_formula as F  # noqa: E402
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+E2M1, E4M3 = 0, 1
+F64, F32, BF16, F16 = range(4)
+COL, ROW = 0, 1
+ref = ctypes.byref
+BUF = 1 << 20  # an address that no refused call reads
+
+
+def M(type=F32, order=ROW, rows=4, cols=6, ld=6, data=BUF):
+    return C.CostaMatrix(type, order, rows, cols, ld, data)
+
+
+def Q(fmt=E2M1, rows=4, cols=6, data=2 * BUF, scales=3 * BUF):
+    return C.CostaMx(fmt, rows, cols, data, scales)
+
+
+def test_every_declared_symbol_is_exported():
+    header = open(os.path.join(ROOT, "include", "costa_mx.h")).read()
+    names = set(re.findall(r"^\s*costa_status\s+(costa_\w+)\s*\(", header, re.M))
+    assert len(names) == 7
+    lib = ctypes.CDLL(C.LIB_PATH)
+    assert not [n for n in sorted(names) if not hasattr(lib, n)]
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("rows,cols", [(0, 0), (0, 9), (9, 0), (1, 1), (3, 128), (3, 129), (5, 256), (5, 257), (7, 1000)])
+def test_sizes_are_those_of_the_formula(bits, rows, cols):
+    data, scales = F.encode(np.zeros((rows, cols), np.float32), bits)
+    assert C.costa_mx_sizes(bits, rows, cols) == (data.size, scales.size)
+    assert data.shape[1] % 128 == 0
+
+
+def test_sizes_refusals():
+    a, b = ctypes.c_int64(), ctypes.c_int64()
+    f = C._lib.costa_mx_sizes
+    assert f(2, 1, 1, ref(a), ref(b)) == C.INVALID_VALUE
+    assert f(E2M1, -1, 1, ref(a), ref(b)) == C.INVALID_VALUE
+    assert f(E2M1, 1, -1, ref(a), ref(b)) == C.INVALID_VALUE
+    assert f(E2M1, 1, 1, None, ref(b)) == C.INVALID_VALUE
+    assert f(E2M1, 2**31, 1, ref(a), ref(b)) == C.NOT_SUPPORTED
+    assert f(E4M3, 2**31 - 1, 2**31 - 1, ref(a), ref(b)) == C.SUCCESS and a.value == (2**31 - 1) * 2**31
+
+
+BAD_MATRIX = [
+    (dict(type=7), C.INVALID_VALUE), (dict(order=5), C.INVALID_VALUE), (dict(rows=-1), C.INVALID_VALUE),
+    (dict(cols=-1), C.INVALID_VALUE), (dict(ld=5), C.INVALID_VALUE), (dict(ld=0), C.INVALID_VALUE),
+    (dict(order=COL, ld=3), C.INVALID_VALUE), (dict(data=None), C.INVALID_VALUE), (dict(data=BUF + 1), C.INVALID_VALUE),
+    (dict(rows=2**31), C.NOT_SUPPORTED), (dict(cols=2**31, ld=2**31), C.NOT_SUPPORTED),
+    (dict(ld=2**57), C.NOT_SUPPORTED)]
+BAD_MX = [
+    (dict(fmt=2), C.INVALID_VALUE), (dict(rows=-1), C.INVALID_VALUE), (dict(cols=-1), C.INVALID_VALUE),
+    (dict(data=None), C.INVALID_VALUE), (dict(scales=None), C.INVALID_VALUE), (dict(data=2 * BUF + 8), C.INVALID_VALUE),
+    (dict(scales=3 * BUF + 4), C.INVALID_VALUE), (dict(rows=2**31), C.NOT_SUPPORTED)]
+
+
+@pytest.mark.parametrize("how,status", BAD_MATRIX, ids=str)
+def test_plain_matrices_that_are_refused(how, status):
+    b = M(**how)
+    assert C._lib.costa_mx_quantize(1.0, ref(b), ref(Q()), None, None) == status
+    assert C._lib.costa_mx_dequantize(1.0, ref(Q()), 0.0, ref(b), None) == status
+    ok = Q(rows=5, cols=6)
+    assert C._lib.costa_mx_product_real(1.0, 0, ref(b), ref(ok), 0.0, ref(M(cols=5, data=4 * BUF)), None, 0, None) == status
+    assert C._lib.costa_mx_product(1.0, ref(Q(cols=8)), ref(Q(rows=6, cols=8, data=5 * BUF, scales=6 * BUF)), 0.0,
+                                   ref(b), None, 0, None) == status
+    assert C.costa_last_error()
+
+
+@pytest.mark.parametrize("how,status", BAD_MX, ids=str)
+def test_stored_matrices_that_are_refused(how, status):
+    q = Q(**how)
+    assert C._lib.costa_mx_quantize(1.0, ref(M()), ref(q), None, None) == status
+    assert C._lib.costa_mx_dequantize(1.0, ref(q), 0.0, ref(M()), None) == status
+    assert C._lib.costa_mx_product_real(1.0, 0, ref(M(rows=3)), ref(q), 0.0, ref(M(rows=3, cols=4, data=4 * BUF)), None,
+                                        0, None) == status
+    other = Q(rows=5, data=7 * BUF, scales=8 * BUF)
+    assert C._lib.costa_mx_product(1.0, ref(q), ref(other), 0.0, ref(M(cols=5)), None, 0, None) == status
+    assert C._lib.costa_mx_product(1.0, ref(other), ref(q), 0.0, ref(M(rows=5, cols=4)), None, 0, None) == status
+
+
+def test_shapes_that_do_not_fit():
+    S = C.SHAPE_MISMATCH
+    assert C._lib.costa_mx_quantize(1.0, ref(M()), ref(Q(rows=5)), None, None) == S
+    assert C._lib.costa_mx_quantize(1.0, ref(M()), None, ref(Q()), None) == S  # QT has the transposed shape
+    assert C._lib.costa_mx_quantize(1.0, ref(M()), None, None, None) == C.INVALID_VALUE
+    assert C._lib.costa_mx_quantize(1.0, None, ref(Q()), None, None) == C.INVALID_VALUE
+    assert C._lib.costa_mx_dequantize(1.0, ref(Q(cols=7)), 0.0, ref(M()), None) == S
+    b = Q(rows=5, data=7 * BUF, scales=8 * BUF)
+    c = M(cols=5)
+    assert C._lib.costa_mx_product(1.0, ref(Q(cols=7)), ref(b), 0.0, ref(c), None, 0, None) == S
+    assert C._lib.costa_mx_product(1.0, ref(Q()), ref(b), 0.0, ref(M()), None, 0, None) == S
+    for op in (1, 2):
+        assert C._lib.costa_mx_product_real(1.0, op, ref(M(data=9 * BUF)), ref(b), 0.0, ref(c), None, 0, None) == S
+    assert C._lib.costa_mx_product_real(1.0, 3, ref(M(data=9 * BUF)), ref(b), 0.0, ref(c), None, 0, None) == C.INVALID_VALUE
+
+
+def test_products_of_doubles_overlaps_and_workspaces_are_refused():
+    b = Q(rows=5, data=7 * BUF, scales=8 * BUF)
+    f = C._lib.costa_mx_product_real
+    c = M(cols=5)
+    assert f(1.0, 0, ref(M(F64, data=9 * BUF)), ref(b), 0.0, ref(c), None, 0, None) == C.NOT_SUPPORTED
+    assert f(1.0, 0, ref(M(data=9 * BUF)), ref(b), 0.0, ref(M(F64, cols=5)), None, 0, None) == C.NOT_SUPPORTED
+    assert f(1.0, 0, ref(M(data=BUF + 4)), ref(b), 0.0, ref(c), None, 0, None) == C.INVALID_VALUE  # C over A
+    assert f(1.0, 0, ref(M(data=9 * BUF)), ref(b), 0.0, ref(M(cols=5, data=7 * BUF + 256)), None, 0, None) == C.INVALID_VALUE
+    assert f(1.0, 0, ref(M(data=9 * BUF)), ref(b), 0.0, ref(M(cols=5, data=8 * BUF)), None, 0, None) == C.INVALID_VALUE
+    assert f(1.0, 0, ref(M(data=9 * BUF)), ref(b), 0.0, ref(c), 10 * BUF + 4, 64, None) == C.INVALID_VALUE
+    assert f(1.0, 0, ref(M(data=9 * BUF)), ref(b), 0.0, ref(c), BUF, 64, None) == C.INVALID_VALUE  # C over the workspace
+    n = ctypes.c_size_t()
+    assert C._lib.costa_mx_workspace(1, -1, 1, ref(n)) == C.INVALID_VALUE
+    assert C._lib.costa_mx_workspace(1, 1, 1, None) == C.INVALID_VALUE
+
+
+def test_layouts_that_are_refused():
+    L = C.Layout.block_cyclic(8, 6, 2, 2, 2, 1)
+    f = lambda type, lay, bufs, q, qt=None: C._lib.costa_mx_quantize_layout(  # noqa: E731
+        type, 1.0, lay, (ctypes.c_void_p * len(bufs))(*bufs) if bufs else None, q and ref(q), qt and ref(qt), None)
+    q = Q(rows=8, cols=6)
+    assert f(9, L.handle, [BUF, BUF], q) == C.INVALID_VALUE
+    assert f(F32, None, [BUF, BUF], q) == C.INVALID_VALUE
+    assert f(F32, L.handle, None, q) == C.INVALID_VALUE
+    assert f(F32, L.handle, [BUF, None], q) == C.INVALID_VALUE
+    assert f(F32, L.handle, [BUF, BUF + 2], q) == C.INVALID_VALUE
+    assert f(F32, L.handle, [BUF, BUF], None) == C.INVALID_VALUE
+    assert f(F32, L.handle, [BUF, BUF], Q(rows=6, cols=8)) == C.SHAPE_MISMATCH
+    assert f(F32, L.handle, [BUF, BUF], q, q) == C.SHAPE_MISMATCH
+    many = C.Layout.block_cyclic(600, 6, 2, 2, 257, 1)
+    assert f(F32, many.handle, [BUF] * 257, Q(rows=600)) == C.NOT_SUPPORTED
+
+
+def test_python_views_are_checked():
+    import torch
+    with pytest.raises(ValueError):  # host memory never reaches a kernel
+        C.costa_mx_quantize(1.0, torch.zeros(4, 4), None, None)
+    with pytest.raises(ValueError):
+        C.MxMatrix(4, 1, 1, torch.zeros(128, dtype=torch.uint8), torch.zeros(8, dtype=torch.uint8))
