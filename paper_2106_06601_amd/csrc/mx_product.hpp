@@ -1,0 +1,135 @@
+// Shared by the product kernels.
+#pragma once
+
+#include "mx_device.hpp"
+
+namespace costa {
+
+// Kinds of left operands.
+enum Source : int { SRC_MX4, SRC_MX8, SRC_BF16, SRC_F16, SRC_F32 };
+// bfloat16 parts that hold an element of each.
+constexpr int parts_of(int src) { return src == SRC_F32 ? 3 : src == SRC_F16 ? 2 : 1; }
+constexpr int bytes_of(int src) { return src == SRC_F32 ? 4 : 2; }  // of plain elements
+
+// Where the sums go: C, or a part's place in the workspace.
+struct Epilogue {
+  void* c;
+  int64_t rs, cs;
+  int32_t type;
+  int32_t vec;  // four elements of a row from a multiple of four on make one aligned store
+  float alpha, beta;
+};
+
+template <typename T>
+__device__ inline void put_elem(const Epilogue& e, int64_t at, float acc) {
+  T* p = static_cast<T*>(e.c) + at;
+  float v = e.alpha * acc;
+  if (e.beta != 0.0f) v += e.beta * (float)*p;
+  *p = (T)v;
+}
+
+// n (at most 4) elements of row i from column j on.
+template <typename T>
+__device__ inline void put_typed(const Epilogue& e, int64_t i, int64_t j, v4f acc, int n) {
+  const int64_t at = i * e.rs + j * e.cs;
+  if (e.vec && n == 4) {
+    typedef T V __attribute__((ext_vector_type(4)));
+    V* p = reinterpret_cast<V*>(static_cast<T*>(e.c) + at);
+    v4f v;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = e.alpha * acc[q];
+    if (e.beta != 0.0f) {
+      const V old = *p;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] += e.beta * (float)old[q];
+    }
+    V out;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) out[q] = (T)v[q];
+    *p = out;
+    return;
+  }
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    if (q < n) put_elem<T>(e, at + q * e.cs, acc[q]);
+}
+__device__ inline void put_four(const Epilogue& e, int64_t i, int64_t j, v4f acc, int n) {
+  if (n <= 0) return;
+  if (e.type == COSTA_REAL_F32) put_typed<float>(e, i, j, acc, n);
+  else if (e.type == COSTA_REAL_BF16) put_typed<__bf16>(e, i, j, acc, n);
+  else put_typed<_Float16>(e, i, j, acc, n);
+}
+
+// Arguments of the product kernels.
+struct Args {
+  int64_t m, n, k;
+  MxView a, b;
+  const void* real;
+  int64_t a_rs, a_cs;
+  Epilogue e;
+  int64_t part;  // elements between the parts of a split sum (0: not split)
+};
+
+// Eight consecutive elements of a line of a plain matrix at p, of which n
+// (at most 8) are there; the rest zero.  Vector loads need no alignment.
+template <int SRC>
+struct Raw8 {
+  uint32_t w[2 * bytes_of(SRC)];
+};
+template <int SRC>
+__device__ inline Raw8<SRC> load8(const char* p, int64_t n) {
+  Raw8<SRC> r;
+  if (n >= 8) {
+    __builtin_memcpy(r.w, p, sizeof r.w);
+  } else if (bytes_of(SRC) == 4) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) r.w[q % (2 * bytes_of(SRC))] = q < n ? reinterpret_cast<const uint32_t*>(p)[q] : 0u;
+  } else {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const uint32_t lo = 2 * q < n ? reinterpret_cast<const uint16_t*>(p)[2 * q] : 0u;
+      const uint32_t hi = 2 * q + 1 < n ? reinterpret_cast<const uint16_t*>(p)[2 * q + 1] : 0u;
+      r.w[q] = lo | hi << 16;
+    }
+  }
+  return r;
+}
+
+// The element's value; parts of eight elements.
+template <int SRC>
+__device__ inline float raw_value(const Raw8<SRC>& r, int q) {
+  if (SRC == SRC_F32) return __builtin_bit_cast(float, r.w[q % (2 * bytes_of(SRC))]);
+  const uint16_t h = (uint16_t)(r.w[q / 2] >> (q % 2 * 16));
+  return (float)__builtin_bit_cast(_Float16, h);
+}
+template <int SRC>
+__device__ inline void raw_parts(const Raw8<SRC>& r, v4u out[parts_of(SRC)]) {
+  if (SRC == SRC_BF16) {
+    out[0] = v4u{r.w[0], r.w[1], r.w[2], r.w[3]};
+    return;
+  }
+  constexpr int P = parts_of(SRC);
+  uint16_t w[8][P];
+#pragma unroll
+  for (int q = 0; q < 8; ++q) bf16_parts<P>(raw_value<SRC>(r, q), w[q]);
+#pragma unroll
+  for (int t = 0; t < P; ++t)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) out[t][q] = w[2 * q][t] | (uint32_t)w[2 * q + 1][t] << 16;
+}
+
+__device__ inline v4f mfma_bf16(v4u a, v4u b, v4f c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
+}
+
+// How a product runs; a function of sizes and types alone.
+enum Variant : int { FEW_ROWS, TILES_BF16, TILES_SCALED };
+struct ProductPlan {
+  Variant variant;
+  int bm, bn;   // tile of C (rows, columns)
+  int splits;   // workgroups that share a tile's sum
+};
+hipError_t launch_tiles_bf16(int src, const Args& p, const ProductPlan& plan, hipStream_t stream);
+hipError_t launch_tiles_scaled(const Args& p, const ProductPlan& plan, hipStream_t stream);
+
+}  // namespace costa

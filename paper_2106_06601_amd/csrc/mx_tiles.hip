@@ -1,0 +1,416 @@
+// Products of microscaled matrices in tiles of C, with both operands staged in
+// shared memory.
+//
+// Both kernels run 8 waves on a tile and keep two stages of k: while the matrix
+// instructions work on one, the next one's loads are on their way to registers;
+// they are then written to the other stage, one barrier a step.  The operands
+// of a matrix instruction are passed with B first: lane l then ends up with row
+// l % 16 of C and four neighbouring columns, which makes wide stores.
+#include <algorithm>
+
+#include "mx_product.hpp"
+
+namespace costa {
+namespace {
+
+constexpr int kWaves = 8;
+constexpr int kLanes = 64 * kWaves;
+
+// Tile (tm, tn) of workgroup b of a launch over nm x nn tiles.  Workgroups go
+// round the 8 XCDs in turn; each XCD gets a run of neighbouring tiles (8 tile
+// rows wide, by columns), whose operands its L2 holds.
+__device__ inline void tile_of(int64_t b, int64_t nm, int64_t nn, int64_t& tm, int64_t& tn) {
+  const int64_t total = nm * nn, per = total / 8, more = total % 8, x = b % 8;
+  const int64_t t = x * per + min(x, more) + b / 8;
+  const int64_t group = t / (8 * nn), rows = min((int64_t)8, nm - group * 8), in = t - group * 8 * nn;
+  tm = group * 8 + in % rows;
+  tn = in / rows;
+}
+
+// ---- plain (or decoded) left operand: bfloat16 instructions --------------------------
+// k goes by 64.  The left tile is held as bfloat16 parts, 128 bytes a row, its 16-byte
+// chunks (8 elements) permuted within a row so that lanes on neighbouring rows meet
+// different banks; the right tile as stored, decoded on the way to the matrix
+// instruction (16 elements of a row a lane and step, 8 for each of two
+// instructions; the left operand is read in the same order of k).
+constexpr int kStepBf16 = 64;
+__device__ inline int chunk_at(int row, int chunk) { return row * 8 + (chunk ^ ((row ^ row >> 3) & 7)); }
+
+template <int SRC, bool TRANS, int BM>
+struct LeftStage {
+  static constexpr bool MX = SRC == SRC_MX4 || SRC == SRC_MX8;
+  static constexpr int BITS = SRC == SRC_MX4 ? 4 : 8;
+  static constexpr int P = parts_of(SRC);
+  static constexpr int ES = bytes_of(SRC);
+  static constexpr int PASSES = BM / 64;  // chunks of a lane (k next to one another)
+  static constexpr int MPT = BM / 64;     // rows of a lane (rows next to one another)
+  static constexpr int TW = (MPT * ES + 3) / 4;
+
+  Raw8<SRC> raw[TRANS || MX ? 1 : PASSES];
+  v2u code[MX ? PASSES : 1];
+  uint32_t scale[MX ? PASSES : 1];
+  uint32_t line[TRANS ? 8 : 1][TW];
+
+  __device__ inline void load(const Args& p, int64_t i0, int64_t k0) {
+    const int t = threadIdx.x;
+    if constexpr (TRANS) {
+      // wave w has k = k0 + 8 w .. + 7, lane l rows MPT l .. of each
+      const int64_t i = i0 + MPT * (t % 64);
+      const int64_t left = p.m - i;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const int64_t k = k0 + 8 * (t / 64) + q;
+        const char* at = static_cast<const char*>(p.real) + (k * p.a_cs + i) * ES;
+#pragma unroll
+        for (int w = 0; w < TW; ++w) line[q][w] = 0;
+        if (k < p.k) {
+          if (left >= MPT) {
+            __builtin_memcpy(line[q], at, MPT * ES);
+          } else {
+#pragma unroll
+            for (int e = 0; e < MPT; ++e)
+              if (e < left) {
+                if (ES == 4) line[q][e % TW] = reinterpret_cast<const uint32_t*>(at)[e];
+                else line[q][e / 2 % TW] |= (uint32_t) reinterpret_cast<const uint16_t*>(at)[e] << (e % 2 * 16);
+              }
+          }
+        }
+      }
+    } else {
+      const int c = t % 8;
+#pragma unroll
+      for (int q = 0; q < PASSES; ++q) {
+        const int64_t i = min(i0 + t / 8 + 64 * q, p.m - 1), k = k0 + 8 * c;
+        if constexpr (MX) {
+          code[q] = v2u{0u, 0u};
+          scale[q] = 0;
+          if (k < p.a.row_scales * kMxBlock) {
+            const uint8_t* at = p.a.data + i * p.a.row_bytes;
+            if (BITS == 4) code[q].x = *reinterpret_cast<const uint32_t*>(at + k / 2);
+            else code[q] = *reinterpret_cast<const v2u*>(at + k);
+            scale[q] = p.a.scales[i * p.a.row_scales + k / kMxBlock];
+          }
+        } else {
+          raw[q] = load8<SRC>(static_cast<const char*>(p.real) + (i * p.a_rs + k) * ES, p.k - k);
+        }
+      }
+    }
+  }
+
+  // stage: P planes of BM x 8 chunks
+  __device__ inline void store(v4u* stage) const {
+    const int t = threadIdx.x;
+    if constexpr (TRANS) {
+#pragma unroll
+      for (int e = 0; e < MPT; ++e) {
+        v4u out[P];
+        if constexpr (SRC == SRC_BF16) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q)  // halves of two k side by side
+            out[0][q] = __builtin_amdgcn_perm(line[2 * q + 1][e / 2], line[2 * q][e / 2],
+                                              e % 2 ? 0x07060302u : 0x05040100u);
+        } else {
+          Raw8<SRC> r;
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            if constexpr (ES == 4) r.w[q] = line[q][e];
+            else if (q % 2 == 0) r.w[q / 2] = __builtin_amdgcn_perm(line[q + 1][e / 2], line[q][e / 2],
+                                                                    e % 2 ? 0x07060302u : 0x05040100u);
+          }
+          raw_parts<SRC>(r, out);
+        }
+#pragma unroll
+        for (int x = 0; x < P; ++x) stage[x * BM * 8 + chunk_at(MPT * (t % 64) + e, t / 64)] = out[x];
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < PASSES; ++q) {
+        v4u out[P];
+        if constexpr (MX) out[0] = mx_decode8_bf16<BITS>(code[q], scale[q]);
+        else raw_parts<SRC>(raw[q], out);
+#pragma unroll
+        for (int x = 0; x < P; ++x) stage[x * BM * 8 + chunk_at(t / 8 + 64 * q, t % 8)] = out[x];
+      }
+    }
+  }
+};
+
+template <int BBITS, int BN>
+struct RightStage {
+  static constexpr int BYTES = kStepBf16 * BBITS / 8;         // of a row
+  static constexpr int CHUNKS = BYTES / 16;                   // 2 or 4 of them
+  static constexpr int PASSES = (BN * CHUNKS + kLanes - 1) / kLanes;
+  v4u data[PASSES];
+  uint32_t scale;
+  __device__ inline void load(const Args& p, int64_t j0, int64_t k0) {
+    const int t = threadIdx.x;
+#pragma unroll
+    for (int q = 0; q < PASSES; ++q) {
+      const int at = t + q * kLanes;
+      if (BN * CHUNKS % kLanes == 0 || at < BN * CHUNKS) {
+        const int64_t j = min(j0 + at / CHUNKS, p.n - 1);
+        data[q] = *reinterpret_cast<const v4u*>(p.b.data + j * p.b.row_bytes + k0 * BBITS / 8 + at % CHUNKS * 16);
+      }
+    }
+    if (t < BN) {
+      const int64_t j = min(j0 + t, p.n - 1);
+      scale = *reinterpret_cast<const uint16_t*>(p.b.scales + j * p.b.row_scales + k0 / kMxBlock);
+    }
+  }
+  __device__ inline void store(v4u* stage, uint16_t* scales) const {
+    const int t = threadIdx.x;
+#pragma unroll
+    for (int q = 0; q < PASSES; ++q) {
+      const int at = t + q * kLanes;
+      if (BN * CHUNKS % kLanes == 0 || at < BN * CHUNKS) stage[at] = data[q];
+    }
+    if (t < BN) scales[t] = (uint16_t)scale;
+  }
+};
+
+template <int SRC, bool TRANS, int BBITS, int BM, int BN, int WM>
+__global__ __launch_bounds__(kLanes) void tiles_bf16(Args p, int64_t nm, int64_t nn) {
+  constexpr int WN = kWaves / WM, MT = BM / WM / 16, NT = BN / WN / 16, P = parts_of(SRC);
+  constexpr int BROW = kStepBf16 * BBITS / 8;
+  __shared__ v4u left[2][P * BM * 8];
+  __shared__ v4u right[2][BN * BROW / 16];
+  __shared__ uint16_t scales[2][BN];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, r = lane % 16, g = lane / 16;
+  const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
+  int64_t tm, tn;
+  tile_of(blockIdx.x, nm, nn, tm, tn);
+  const int64_t i0 = tm * BM, j0 = tn * BN;
+  const int64_t steps = (p.k + kStepBf16 - 1) / kStepBf16;
+  const int64_t first = steps * blockIdx.y / gridDim.y, last = steps * (blockIdx.y + 1) / gridDim.y;
+
+  v4f acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = v4f{0, 0, 0, 0};
+
+  LeftStage<SRC, TRANS, BM> ls;
+  RightStage<BBITS, BN> rs;
+  ls.load(p, i0, first * kStepBf16);
+  rs.load(p, j0, first * kStepBf16);
+  ls.store(left[0]);
+  rs.store(right[0], scales[0]);
+  if (first + 1 < last) {
+    ls.load(p, i0, (first + 1) * kStepBf16);
+    rs.load(p, j0, (first + 1) * kStepBf16);
+  }
+  __syncthreads();
+  for (int64_t t = first; t < last; ++t) {
+    const int s = (int)(t - first) & 1;
+    v4u b[NT];
+    uint32_t sc[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const int row = wn + 16 * j + r;
+      if (BBITS == 4) {
+        const v2u d = reinterpret_cast<const v2u*>(right[s])[row * 4 + g];
+        b[j] = v4u{d.x, d.y, 0u, 0u};
+      } else {
+        b[j] = right[s][row * 4 + g];
+      }
+      sc[j] = reinterpret_cast<const uint8_t*>(scales[s])[row * 2 + g / 2];
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      v4u w[NT];
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+        w[j] = mx_decode8_bf16<BBITS>(BBITS == 4 ? v2u{b[j][h], 0u} : v2u{b[j][2 * h], b[j][2 * h + 1]}, sc[j]);
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int x = 0; x < P; ++x) {
+          const v4u a = left[s][x * BM * 8 + chunk_at(wm + 16 * i + r, 2 * g + h)];
+#pragma unroll
+          for (int j = 0; j < NT; ++j) acc[i][j] = mfma_bf16(w[j], a, acc[i][j]);
+        }
+    }
+    if (t + 1 < last) {
+      ls.store(left[1 - s]);
+      rs.store(right[1 - s], scales[1 - s]);
+      if (t + 2 < last) {
+        ls.load(p, i0, (t + 2) * kStepBf16);
+        rs.load(p, j0, (t + 2) * kStepBf16);
+      }
+    }
+    __syncthreads();
+  }
+  Epilogue e = p.e;
+  if (p.part) e.c = static_cast<float*>(e.c) + blockIdx.y * p.part;
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int64_t row = i0 + wm + 16 * i + r;
+    if (row < p.m)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const int64_t col = j0 + wn + 16 * j + 4 * g;
+        put_four(e, row, col, acc[i][j], (int)max((int64_t)0, min((int64_t)4, p.n - col)));
+      }
+  }
+}
+
+// ---- both operands in 4 bits: the scaled instructions -----------------------------------
+// An instruction sums 128 products, each block of 32 with its scales: exactly, then
+// rounded into a 32-bit sum.  (The same instruction on 8-bit elements drops what is
+// some 2^-13 of its largest product: 1.5e-5 of a product of normal matrices, more
+// where a few columns stand out; those products take the bfloat16 kernel.)  k goes
+// by 256, so that a step's row is 128 bytes.
+constexpr int kStep4 = 256;
+constexpr int kRowChunks = 8;  // 16-byte chunks of a step's row
+__device__ inline int code_at(int row, int chunk) { return row * kRowChunks + (chunk ^ (row & 7)); }
+
+template <int BR>
+struct CodeStage {
+  static constexpr int PASSES = BR * kRowChunks / kLanes;
+  v4u data[PASSES];
+  __device__ inline void load(const MxView& q, int64_t row0, int64_t k0) {
+#pragma unroll
+    for (int c = 0; c < PASSES; ++c) {
+      const int at = threadIdx.x + c * kLanes;
+      const int64_t row = min(row0 + at / kRowChunks, q.rows - 1);
+      data[c] = *reinterpret_cast<const v4u*>(q.data + row * q.row_bytes + k0 / 2 + at % kRowChunks * 16);
+    }
+  }
+  __device__ inline void store(v4u* stage) const {
+#pragma unroll
+    for (int c = 0; c < PASSES; ++c) {
+      const int at = threadIdx.x + c * kLanes;
+      stage[code_at(at / kRowChunks, at % kRowChunks)] = data[c];
+    }
+  }
+};
+__device__ inline v8i operand4(v4u d) {  // the instruction reads four of the eight registers
+  const v4i c = __builtin_bit_cast(v4i, d);
+  return __builtin_shufflevector(c, c, 0, 1, 2, 3, -1, -1, -1, -1);
+}
+
+template <int BM, int BN, int WM>
+__global__ __launch_bounds__(kLanes) void tiles_scaled(Args p, int64_t nm, int64_t nn) {
+  constexpr int WN = kWaves / WM, MT = BM / WM / 16, NT = BN / WN / 16;
+  __shared__ v4u left[2][BM * kRowChunks];
+  __shared__ v4u right[2][BN * kRowChunks];
+  __shared__ v2u scales[2][BM + BN];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, r = lane % 16, g = lane / 16;
+  const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
+  int64_t tm, tn;
+  tile_of(blockIdx.x, nm, nn, tm, tn);
+  const int64_t i0 = tm * BM, j0 = tn * BN;
+  const int64_t steps = (p.k + kStep4 - 1) / kStep4;
+  const int64_t first = steps * blockIdx.y / gridDim.y, last = steps * (blockIdx.y + 1) / gridDim.y;
+
+  v4f acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = v4f{0, 0, 0, 0};
+
+  // a lane stages the scales of one row of either operand
+  static_assert(BM + BN <= kLanes, "a lane a row");
+  const bool mine = threadIdx.x < BM + BN, of_a = threadIdx.x < BM;
+  const MxView& sv = of_a ? p.a : p.b;
+  const int64_t srow = of_a ? min(i0 + threadIdx.x, p.m - 1) : min(j0 + threadIdx.x - BM, p.n - 1);
+  const uint8_t* sp = sv.scales + srow * sv.row_scales;
+  v2u sreg;
+  CodeStage<BM> as;
+  CodeStage<BN> bs;
+  auto load = [&](int64_t t) {
+    as.load(p.a, i0, t * kStep4);
+    bs.load(p.b, j0, t * kStep4);
+    if (mine) sreg = *reinterpret_cast<const v2u*>(sp + t * (kStep4 / kMxBlock));
+  };
+  auto store = [&](int s) {
+    as.store(left[s]);
+    bs.store(right[s]);
+    if (mine) scales[s][threadIdx.x] = sreg;
+  };
+  load(first);
+  store(0);
+  if (first + 1 < last) load(first + 1);
+  __syncthreads();
+  for (int64_t t = first; t < last; ++t) {
+    const int s = (int)(t - first) & 1;
+    const uint8_t* sc = reinterpret_cast<const uint8_t*>(scales[s]);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      v8i b[NT];
+      int sb[NT];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const int row = wn + 16 * j + r;
+        b[j] = operand4(right[s][code_at(row, 4 * h + g)]);
+        sb[j] = sc[(BM + row) * 8 + 4 * h + g];
+      }
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const int row = wm + 16 * i + r;
+        const v8i a = operand4(left[s][code_at(row, 4 * h + g)]);
+        const int sa = sc[row * 8 + 4 * h + g];
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j], a, acc[i][j], 4, 4, 0, sb[j], 0, sa);
+      }
+    }
+    if (t + 1 < last) {
+      store(1 - s);
+      if (t + 2 < last) load(t + 2);
+    }
+    __syncthreads();
+  }
+  Epilogue e = p.e;
+  if (p.part) e.c = static_cast<float*>(e.c) + blockIdx.y * p.part;
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int64_t row = i0 + wm + 16 * i + r;
+    if (row < p.m)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const int64_t col = j0 + wn + 16 * j + 4 * g;
+        put_four(e, row, col, acc[i][j], (int)max((int64_t)0, min((int64_t)4, p.n - col)));
+      }
+  }
+}
+
+template <int SRC, bool TRANS, int BBITS>
+hipError_t launch_bf16(const Args& p, const ProductPlan& plan, hipStream_t stream) {
+  constexpr int BM = parts_of(SRC) == 1 ? 256 : 128;
+  const int64_t nm = (p.m + plan.bm - 1) / plan.bm, nn = (p.n + plan.bn - 1) / plan.bn;
+  const dim3 grid((unsigned)(nm * nn), plan.splits);
+  if (plan.bn == 256) tiles_bf16<SRC, TRANS, BBITS, BM, 256, 2><<<grid, kLanes, 0, stream>>>(p, nm, nn);
+  else tiles_bf16<SRC, TRANS, BBITS, 128, 64, 4><<<grid, kLanes, 0, stream>>>(p, nm, nn);
+  return hipGetLastError();
+}
+template <int SRC, bool TRANS>
+hipError_t launch_bf16_bits(const Args& p, const ProductPlan& plan, hipStream_t stream) {
+  return p.b.bits == 4 ? launch_bf16<SRC, TRANS, 4>(p, plan, stream) : launch_bf16<SRC, TRANS, 8>(p, plan, stream);
+}
+template <int SRC>
+hipError_t launch_bf16_op(const Args& p, const ProductPlan& plan, hipStream_t stream) {
+  return p.a_cs == 1 ? launch_bf16_bits<SRC, false>(p, plan, stream) : launch_bf16_bits<SRC, true>(p, plan, stream);
+}
+
+}  // namespace
+
+hipError_t launch_tiles_bf16(int src, const Args& p, const ProductPlan& plan, hipStream_t stream) {
+  switch (src) {
+    case SRC_MX4: return launch_bf16_bits<SRC_MX4, false>(p, plan, stream);
+    case SRC_MX8: return launch_bf16_bits<SRC_MX8, false>(p, plan, stream);
+    case SRC_BF16: return launch_bf16_op<SRC_BF16>(p, plan, stream);
+    case SRC_F16: return launch_bf16_op<SRC_F16>(p, plan, stream);
+    default: return launch_bf16_op<SRC_F32>(p, plan, stream);
+  }
+}
+
+hipError_t launch_tiles_scaled(const Args& p, const ProductPlan& plan, hipStream_t stream) {
+  const int64_t nm = (p.m + plan.bm - 1) / plan.bm, nn = (p.n + plan.bn - 1) / plan.bn;
+  const dim3 grid((unsigned)(nm * nn), plan.splits);
+  if (plan.bn == 256) tiles_scaled<256, 256, 2><<<grid, kLanes, 0, stream>>>(p, nm, nn);
+  else tiles_scaled<128, 128, 2><<<grid, kLanes, 0, stream>>>(p, nm, nn);
+  return hipGetLastError();
+}
+
+}  // namespace costa
