@@ -197,7 +197,8 @@ ProductPlan plan_product(int src, bool k_next, int bbits, int64_t m, int64_t n, 
     r.splits = splits_for((n + r.bn - 1) / r.bn, kCUs, units, 4 * kFewWaves, m, n);
     return r;
   }
-  const bool scaled = src == SRC_MX4 && bbits == 4;
+  // (the scaled kernel counts a tile's bytes in 32 bits)
+  const bool scaled = src == SRC_MX4 && bbits == 4 && k <= 1 << 24;
   r.variant = scaled ? TILES_SCALED : TILES_BF16;
   const int big = scaled || parts_of(src) == 1 ? 256 : 128;
   const auto tiles = [&](int64_t bm, int64_t bn) { return (m + bm - 1) / bm * ((n + bn - 1) / bn); };

@@ -23,8 +23,9 @@ __device__ inline void tile_of(int64_t b, int64_t nm, int64_t nn, int64_t& tm, i
   const int64_t total = nm * nn, per = total / 8, more = total % 8, x = b % 8;
   const int64_t t = x * per + min(x, more) + b / 8;
   const int64_t group = t / (8 * nn), rows = min((int64_t)8, nm - group * 8), in = t - group * 8 * nn;
-  tm = group * 8 + in % rows;
-  tn = in / rows;
+  // (the division runs on vector registers: both are the wave's, not a lane's)
+  tm = __builtin_amdgcn_readfirstlane((int)(group * 8 + in % rows));
+  tn = __builtin_amdgcn_readfirstlane((int)(in / rows));
 }
 
 // ---- plain (or decoded) left operand: bfloat16 instructions --------------------------
@@ -175,7 +176,7 @@ __global__ __launch_bounds__(kLanes) void tiles_bf16(Args p, int64_t nm, int64_t
   __shared__ v4u left[2][P * BM * 8];
   __shared__ v4u right[2][BN * BROW / 16];
   __shared__ uint16_t scales[2][BN];
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, r = lane % 16, g = lane / 16;
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, g = lane / 16;
   const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
   int64_t tm, tn;
   tile_of(blockIdx.x, nm, nn, tm, tn);
@@ -264,26 +265,37 @@ constexpr int kStep4 = 256;
 constexpr int kRowChunks = 8;  // 16-byte chunks of a step's row
 __device__ inline int code_at(int row, int chunk) { return row * kRowChunks + (chunk ^ (row & 7)); }
 
+// A stage of BR rows goes from memory to shared memory without registers: a lane
+// names 16 bytes, the wave's 1024 bytes land next to one another.  The permutation
+// of a row's chunks is in the lanes' addresses.  The compiler does not see these
+// loads: wait_stage() waits for them.
 template <int BR>
 struct CodeStage {
   static constexpr int PASSES = BR * kRowChunks / kLanes;
-  v4u data[PASSES];
-  __device__ inline void load(const MxView& q, int64_t row0, int64_t k0) {
+  uint32_t offset[PASSES];  // of the lane's bytes from the tile's first row
+  const uint8_t* base;
+  __device__ inline CodeStage(const MxView& q, int64_t row0) : base(q.data + row0 * q.row_bytes) {
 #pragma unroll
     for (int c = 0; c < PASSES; ++c) {
-      const int at = threadIdx.x + c * kLanes;
-      const int64_t row = min(row0 + at / kRowChunks, q.rows - 1);
-      data[c] = *reinterpret_cast<const v4u*>(q.data + row * q.row_bytes + k0 / 2 + at % kRowChunks * 16);
+      const int at = threadIdx.x + c * kLanes, row = at / kRowChunks;
+      const uint32_t there = (uint32_t)min((int64_t)row, q.rows - 1 - row0);
+      offset[c] = there * (uint32_t)q.row_bytes + (at % kRowChunks ^ (row & 7)) * 16;
     }
   }
-  __device__ inline void store(v4u* stage) const {
+  __device__ inline void load(int64_t t, v4u* stage) const {
+    const uint8_t* from = base + t * (kRowChunks * 16);
 #pragma unroll
     for (int c = 0; c < PASSES; ++c) {
-      const int at = threadIdx.x + c * kLanes;
-      stage[code_at(at / kRowChunks, at % kRowChunks)] = data[c];
+      const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(
+          __attribute__((address_space(3))) v4u*)(stage + c * kLanes + threadIdx.x / 64 * 64));
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                   :
+                   : "s"(to), "v"(offset[c]), "s"(from)
+                   : "memory");
     }
   }
 };
+__device__ inline void wait_stage() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 __device__ inline v8i operand4(v4u d) {  // the instruction reads four of the eight registers
   const v4i c = __builtin_bit_cast(v4i, d);
   return __builtin_shufflevector(c, c, 0, 1, 2, 3, -1, -1, -1, -1);
@@ -295,7 +307,7 @@ __global__ __launch_bounds__(kLanes) void tiles_scaled(Args p, int64_t nm, int64
   __shared__ v4u left[2][BM * kRowChunks];
   __shared__ v4u right[2][BN * kRowChunks];
   __shared__ v2u scales[2][BM + BN];
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, r = lane % 16, g = lane / 16;
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, g = lane / 16;
   const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
   int64_t tm, tn;
   tile_of(blockIdx.x, nm, nn, tm, tn);
@@ -316,24 +328,23 @@ __global__ __launch_bounds__(kLanes) void tiles_scaled(Args p, int64_t nm, int64
   const int64_t srow = of_a ? min(i0 + threadIdx.x, p.m - 1) : min(j0 + threadIdx.x - BM, p.n - 1);
   const uint8_t* sp = sv.scales + srow * sv.row_scales;
   v2u sreg;
-  CodeStage<BM> as;
-  CodeStage<BN> bs;
-  auto load = [&](int64_t t) {
-    as.load(p.a, i0, t * kStep4);
-    bs.load(p.b, j0, t * kStep4);
+  const CodeStage<BM> as(p.a, i0);
+  const CodeStage<BN> bs(p.b, j0);
+  auto load = [&](int64_t t, int s) {
     if (mine) sreg = *reinterpret_cast<const v2u*>(sp + t * (kStep4 / kMxBlock));
+    as.load(t, left[s]);
+    bs.load(t, right[s]);
   };
-  auto store = [&](int s) {
-    as.store(left[s]);
-    bs.store(right[s]);
+  auto arrive = [&](int s) {
+    wait_stage();
     if (mine) scales[s][threadIdx.x] = sreg;
+    __syncthreads();
   };
-  load(first);
-  store(0);
-  if (first + 1 < last) load(first + 1);
-  __syncthreads();
+  load(first, 0);
+  arrive(0);
   for (int64_t t = first; t < last; ++t) {
     const int s = (int)(t - first) & 1;
+    if (t + 1 < last) load(t + 1, 1 - s);
     const uint8_t* sc = reinterpret_cast<const uint8_t*>(scales[s]);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -355,11 +366,7 @@ __global__ __launch_bounds__(kLanes) void tiles_scaled(Args p, int64_t nm, int64
           acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j], a, acc[i][j], 4, 4, 0, sb[j], 0, sa);
       }
     }
-    if (t + 1 < last) {
-      store(1 - s);
-      if (t + 2 < last) load(t + 2);
-    }
-    __syncthreads();
+    if (t + 1 < last) arrive(1 - s);
   }
   Epilogue e = p.e;
   if (p.part) e.c = static_cast<float*>(e.c) + blockIdx.y * p.part;
