@@ -99,8 +99,8 @@ __device__ inline void mx_decode8(v2u d, uint32_t s, float x[8]) {
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    x[2 * i] = s == 255u ? __builtin_nanf("") : p[i].x;
-    x[2 * i + 1] = s == 255u ? __builtin_nanf("") : p[i].y;
+    x[2 * i] = p[i].x;
+    x[2 * i + 1] = p[i].y;
   }
 }
 
@@ -122,7 +122,7 @@ __device__ inline v4u mx_decode8_bf16(v2u d, uint32_t s) {
   }
   v4u r;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) r[i] = s == 255u ? 0x7fc07fc0u : __builtin_bit_cast(uint32_t, p[i]);
+  for (int i = 0; i < 4; ++i) r[i] = __builtin_bit_cast(uint32_t, p[i]);
   return r;
 }
 

@@ -11,42 +11,84 @@ constexpr int kCUs = 256;
 
 // ---- few rows ------------------------------------------------------------------
 // C has at most 16 MT rows: the time is that of reading B once.  A workgroup
-// makes 16 NT columns; its 8 waves take 128-byte pieces of B's rows in turn, so
+// makes 16 NT columns; its waves take 128-byte pieces of B's rows in turn, so
 // that they read whole lines of neighbouring addresses, straight to registers.
 // Lane l holds row l % 16 of either operand; of a piece, 16 bytes at 16 (l / 16)
 // and 16 at 64 + 16 (l / 16), and the left operand's elements of the same k: any
-// order of k will do as long as both sides agree.  The waves' sums are joined
+// order of k will do as long as both sides agree.  The left operand goes by slabs
+// of 16 rows by 128 of k: a wave reads one as it lies in memory, makes it
+// bfloat16 parts once, and turns it to the instruction's order through a piece of
+// shared memory of its own.  (Read in that order straight from memory, a load
+// touches 64 pieces of 16 bytes, and the left operand costs more than B.)  The next piece of
+// B and the next slab are on their way meanwhile.  The waves' sums are joined
 // through shared memory, pairwise, in a fixed order.
-constexpr int kFewWaves = 8;
+constexpr int kFewWaves = 4;
+constexpr int kSlab = 128;
 
+// A slab: lane l has, of rows l / 16 + 4 q, the eight elements 8 (l % 16) ..
 template <int SRC>
-__device__ inline void few_left(const Args& p, int64_t row, bool there, int64_t k0, v4u out[parts_of(SRC)]) {
-  if (SRC == SRC_MX4 || SRC == SRC_MX8) {
-    constexpr int BITS = SRC == SRC_MX4 ? 4 : 8;
-    v2u d = {0u, 0u};
-    uint32_t s = 0;
-    if (there && k0 < p.a.row_scales * kMxBlock) {
-      const uint8_t* at = p.a.data + row * p.a.row_bytes;
-      if (BITS == 4) d.x = *reinterpret_cast<const uint32_t*>(at + k0 / 2);
-      else d = *reinterpret_cast<const v2u*>(at + k0);
-      s = p.a.scales[row * p.a.row_scales + k0 / kMxBlock];
+struct FewSlab {
+  static constexpr bool MX = SRC == SRC_MX4 || SRC == SRC_MX8;
+  static constexpr int BITS = SRC == SRC_MX4 ? 4 : 8;
+  static constexpr int P = parts_of(SRC);
+  Raw8<SRC> raw[MX ? 1 : 4];
+  v2u code[MX ? 4 : 1];
+  uint32_t scale[MX ? 4 : 1];
+  // rows row0 .. of the operand, of which those past its last repeat it (their
+  // results are not stored); k0: the slab's first k, `end` elements are there
+  __device__ inline void load(const Args& p, int64_t row0, int64_t k0, int64_t end) {
+    const int lane = threadIdx.x % 64;
+    const int64_t k = k0 + 8 * (lane % 16);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (q > 0 && row0 + 4 * q >= p.m) continue;
+      const int64_t row = min(row0 + 4 * q + lane / 16, p.m - 1);
+      if constexpr (MX) {  // (padded to whole slabs; past them nothing counts)
+        const uint8_t* at = p.a.data + row * p.a.row_bytes;
+        code[q] = v2u{0u, 0u};
+        scale[q] = 0;
+        if (k0 < end) {
+          if (BITS == 4) code[q].x = *reinterpret_cast<const uint32_t*>(at + k / 2);
+          else code[q] = *reinterpret_cast<const v2u*>(at + k);
+          scale[q] = p.a.scales[row * p.a.row_scales + k / kMxBlock];
+        }
+      } else {
+        const char* at = static_cast<const char*>(p.real) + (row * p.a_rs + k) * bytes_of(SRC);
+        if (k0 + kSlab <= end) __builtin_memcpy(raw[q].w, at, sizeof raw[q].w);
+        else raw[q] = load8<SRC>(at, end - k);
+      }
     }
-    out[0] = mx_decode8_bf16<BITS>(d, s);
-  } else {
-    const int64_t n = there ? p.k - k0 : 0;
-    raw_parts<SRC>(load8<SRC>(static_cast<const char*>(p.real) + (row * p.a_rs + k0) * bytes_of(SRC), n), out);
   }
-}
+  __device__ inline void store(const Args& p, int64_t row0, v4u* slab) const {
+    const int lane = threadIdx.x % 64;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (q > 0 && row0 + 4 * q >= p.m) continue;
+      v4u out[P];
+      if constexpr (MX) out[0] = mx_decode8_bf16<BITS>(code[q], scale[q]);
+      else raw_parts<SRC>(raw[q], out);
+      const int row = 4 * q + lane / 16;
+#pragma unroll
+      for (int x = 0; x < P; ++x) slab[x * 256 + row * 16 + (lane % 16 ^ (row & 7))] = out[x];
+    }
+  }
+};
 
 template <int SRC, int BBITS, int MT, int NT>
 __global__ __launch_bounds__(64 * kFewWaves) void few_rows(Args p, int splits, int64_t col0) {
   constexpr int UNIT = 1024 / BBITS;  // k of a 128-byte piece
-  constexpr int HALF = UNIT / 2, LANE = HALF / 4, STEPS = LANE / 8;
+  constexpr int SLABS = UNIT / kSlab, LOADS = 2 / SLABS;  // 16-byte loads of B a slab
+  constexpr int STEPS = 128 / 4 / 8 / LOADS;              // instructions a load
   constexpr int P = parts_of(SRC);
-  __shared__ v4f red[kFewWaves / 2][MT * NT][64];
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, r = lane % 16, g = lane / 16;
+  constexpr int SHARED = P * kFewWaves * 256 > kFewWaves / 2 * MT * NT * 64 ? P * kFewWaves * 256
+                                                                            : kFewWaves / 2 * MT * NT * 64;
+  __shared__ v4u shared[SHARED];  // a slab for each wave; then the sums
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16,
+            g = lane / 16;
+  v4u* const slab = shared + wave * P * 256;
   const int64_t j0 = col0 + (int64_t)(blockIdx.x / splits) * (16 * NT);
-  const int64_t units = (p.k + UNIT - 1) / UNIT;
+  const uint32_t units = (uint32_t)((p.k + UNIT - 1) / UNIT);
+  const int64_t a_end = FewSlab<SRC>::MX ? p.a.row_scales * kMxBlock : p.k;
   v4f acc[MT][NT];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
@@ -60,40 +102,83 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_rows(Args p, int splits, i
     data[j] = p.b.data + row * p.b.row_bytes + 16 * g;
     scales[j] = p.b.scales + row * p.b.row_scales + (BBITS == 4 ? g : g / 2);
   }
-  const int step = kFewWaves * splits;
-  for (int64_t u = (int64_t)(blockIdx.x % splits) * kFewWaves + wave; u < units; u += step) {
-    v4u b[NT][2];
-    uint32_t s[NT][2];
+  // this wave's pieces: first, first + step, ..; each workgroup begins at another one of
+  // them (rows a power of two apart would all be read at the same distance else)
+  const uint32_t step = kFewWaves * splits, first = blockIdx.x % splits * kFewWaves + wave;
+  const uint32_t turns = first < units ? (units - first + step - 1) / step : 0;
+  uint32_t turn = turns > 0 ? blockIdx.x / splits % turns : 0;
+  int64_t u = first + turn * step;
+  v4u b[NT][2];
+  uint32_t s[NT][2];
+  FewSlab<SRC> left;
+  auto load = [&](int64_t at) {
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        b[j][h] = *reinterpret_cast<const v4u*>(data[j] + u * 128 + 64 * h);
-        s[j][h] = scales[j][u * (UNIT / kMxBlock) + h * (HALF / kMxBlock)];
+        b[j][h] = *reinterpret_cast<const v4u*>(data[j] + at * 128 + 64 * h);
+        s[j][h] = scales[j][at * (UNIT / kMxBlock) + h * (UNIT / 2 / kMxBlock)];
       }
+  };
+  if (turns > 0) {
+    load(u);
+    left.load(p, 0, u * UNIT, a_end);
+  }
+  for (uint32_t to_go = turns; to_go > 0; --to_go) {
+    turn = turn + 1 < turns ? turn + 1 : 0;
+    const int64_t next = first + turn * step;
+    v4u w[NT][2];
+    uint32_t t[NT][2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int64_t k0 = u * UNIT + h * HALF + g * LANE;
+    for (int j = 0; j < NT; ++j)
 #pragma unroll
-      for (int q = 0; q < STEPS; ++q) {
-        v4u w[NT];
+      for (int h = 0; h < 2; ++h) w[j][h] = b[j][h], t[j][h] = s[j][h];
+    if (to_go > 1) load(next);
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          const v2u d = BBITS == 4 ? v2u{b[j][h][q], 0u} : v2u{b[j][h][2 * q % 4], b[j][h][(2 * q + 1) % 4]};
-          w[j] = mx_decode8_bf16<BBITS>(d, s[j][h]);
-        }
+    for (int h = 0; h < SLABS; ++h) {
+      v4u e[NT][LOADS][STEPS];  // the slab's part of B, decoded
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-          v4u a[P];
-          few_left<SRC>(p, 16 * i + r, 16 * i + r < p.m, k0 + 8 * q, a);
+      for (int j = 0; j < NT; ++j)
 #pragma unroll
-          for (int t = 0; t < P; ++t)
+        for (int l = 0; l < LOADS; ++l)
 #pragma unroll
-            for (int j = 0; j < NT; ++j) acc[i][j] = mfma_bf16(w[j], a[t], acc[i][j]);
-        }
+          for (int q = 0; q < STEPS; ++q) {
+            const v4u& c = w[j][h * LOADS + l];
+            e[j][l][q] = mx_decode8_bf16<BBITS>(BBITS == 4 ? v2u{c[q], 0u} : v2u{c[2 * q % 4], c[(2 * q + 1) % 4]},
+                                                t[j][h * LOADS + l]);
+          }
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        left.store(p, 16 * i, slab);
+        if (i + 1 < MT) left.load(p, 16 * (i + 1), u * UNIT + h * kSlab, a_end);
+        else if (h + 1 < SLABS) left.load(p, 0, u * UNIT + (h + 1) * kSlab, a_end);
+        else if (to_go > 1) left.load(p, 0, next * UNIT, a_end);
+        // (a wave's accesses to shared memory take effect in their order)
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+        for (int l = 0; l < LOADS; ++l)
+#pragma unroll
+          for (int q = 0; q < STEPS; ++q) {
+            const int chunk = l * (kSlab / 8 / LOADS) + g * STEPS + q;
+#pragma unroll
+            for (int x = 0; x < P; ++x) {
+              const v4u a = slab[x * 256 + r * 16 + (chunk ^ (r & 7))];
+#pragma unroll
+              for (int j = 0; j < NT; ++j) acc[i][j] = mfma_bf16(e[j][l][q], a, acc[i][j]);
+            }
+          }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
       }
     }
+    u = next;
   }
+  __syncthreads();
+  typedef v4f Sums[MT * NT][64];
+  Sums* const red = reinterpret_cast<Sums*>(shared);
 #pragma unroll
   for (int half = kFewWaves / 2; half > 0; half /= 2) {
     if (wave >= half && wave < 2 * half)
@@ -152,21 +237,38 @@ hipError_t launch_few(int src, const Args& p, const ProductPlan& plan, hipStream
 }
 
 // ---- the parts of a split sum, in their order -------------------------------------
+// LANES lanes share four elements of C, each adding every LANES-th part; their sums
+// are then added in turn.
+template <int LANES>
 __global__ __launch_bounds__(256) void join_parts(Epilogue e, const float* parts, int64_t m, int64_t n, int splits) {
+  constexpr int UNITS = 256 / LANES;  // of a workgroup
+  __shared__ v4f red[LANES][UNITS];
   const int64_t upr = (n + 3) / 4, units = m * upr;
-  for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (int64_t)gridDim.x * 256) {
+  const int mine = threadIdx.x / UNITS, at = threadIdx.x % UNITS;
+  for (int64_t u0 = (int64_t)blockIdx.x * UNITS; u0 < units; u0 += (int64_t)gridDim.x * UNITS) {
+    const int64_t u = u0 + at;
     const int64_t i = u / upr, j = (u - i * upr) * 4;
-    const int c = (int)min((int64_t)4, n - j);
+    const int c = u < units ? (int)min((int64_t)4, n - j) : 0;
     v4f acc = {0, 0, 0, 0};
     const float* p = parts + i * n + j;
     if (c == 4 && n % 4 == 0) {
-      for (int s = 0; s < splits; ++s) acc += *reinterpret_cast<const v4f*>(p + s * m * n);
+#pragma unroll 8
+      for (int s = mine; s < splits; s += LANES) acc += *reinterpret_cast<const v4f*>(p + s * m * n);
     } else {
-      for (int s = 0; s < splits; ++s)
+#pragma unroll 4
+      for (int s = mine; s < splits; s += LANES)
 #pragma unroll
         for (int q = 0; q < 4; ++q) acc[q] += q < c ? p[s * m * n + q] : 0.0f;
     }
-    put_four(e, i, j, acc, c);
+    if (LANES > 1) {
+      red[mine][at] = acc;
+      __syncthreads();
+      if (mine == 0)
+#pragma unroll
+        for (int s = 1; s < LANES; ++s) acc += red[s][at];
+    }
+    if (mine == 0) put_four(e, i, j, acc, c);
+    if (LANES > 1) __syncthreads();
   }
 }
 
@@ -192,7 +294,8 @@ ProductPlan plan_product(int src, bool k_next, int bbits, int64_t m, int64_t n, 
   if (m <= 64 && k_next) {
     r.variant = FEW_ROWS;
     r.bm = m <= 16 ? 16 : m <= 32 ? 32 : 64;
-    r.bn = m > 4 && n >= 32 * kCUs ? 32 : 16;
+    // (32 columns share a slab's way through shared memory; half as many workgroups)
+    r.bn = m > 4 && n >= 64 * kCUs ? 32 : 16;
     const int64_t units = (k + 1024 / bbits - 1) / (1024 / bbits);
     r.splits = splits_for((n + r.bn - 1) / r.bn, kCUs, units, 4 * kFewWaves, m, n);
     return r;
@@ -256,9 +359,12 @@ hipError_t launch_mx_product(const ProductArgs& a, hipStream_t stream) {
                    : plan.variant == TILES_BF16 ? launch_tiles_bf16(src, p, plan, stream)
                                                 : launch_tiles_scaled(p, plan, stream);
   if (err != hipSuccess || plan.splits == 1) return err;
-  const int64_t groups = (a.m * ((a.n + 3) / 4) + 255) / 256;
-  join_parts<<<dim3((unsigned)std::min<int64_t>(groups, 1 << 20)), 256, 0, stream>>>(e, a.workspace, a.m, a.n,
-                                                                                    plan.splits);
+  // (with 16 lanes, 256 parts of a 100 x 64 sum are joined in 5 us; with one, in 66)
+  const int lanes = plan.splits >= 16 ? 16 : 1;
+  const int64_t groups = (a.m * ((a.n + 3) / 4) * lanes + 255) / 256;
+  const dim3 grid((unsigned)std::min<int64_t>(groups, 1 << 20));
+  if (lanes == 16) join_parts<16><<<grid, 256, 0, stream>>>(e, a.workspace, a.m, a.n, plan.splits);
+  else join_parts<1><<<grid, 256, 0, stream>>>(e, a.workspace, a.m, a.n, plan.splits);
   return hipGetLastError();
 }
 

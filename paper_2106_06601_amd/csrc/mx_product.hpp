@@ -95,27 +95,59 @@ __device__ inline Raw8<SRC> load8(const char* p, int64_t n) {
   return r;
 }
 
-// The element's value; parts of eight elements.
-template <int SRC>
-__device__ inline float raw_value(const Raw8<SRC>& r, int q) {
-  if (SRC == SRC_F32) return __builtin_bit_cast(float, r.w[q % (2 * bytes_of(SRC))]);
-  const uint16_t h = (uint16_t)(r.w[q / 2] >> (q % 2 * 16));
-  return (float)__builtin_bit_cast(_Float16, h);
-}
+// bfloat16 parts of eight elements: each takes the leading 8 bits that are left
+// (by truncation, so that none overflows), which leaves nothing of 24 bits after
+// three and of 11 after two.  An infinity or a NaN is the first part alone.
 template <int SRC>
 __device__ inline void raw_parts(const Raw8<SRC>& r, v4u out[parts_of(SRC)]) {
-  if (SRC == SRC_BF16) {
-    out[0] = v4u{r.w[0], r.w[1], r.w[2], r.w[3]};
-    return;
-  }
   constexpr int P = parts_of(SRC);
-  uint16_t w[8][P];
+  if constexpr (SRC == SRC_BF16) {
+    out[0] = v4u{r.w[0], r.w[1], r.w[2], r.w[3]};
+  } else {
+    uint32_t x[8];
+    bool odd = false;  // an infinity or a NaN among them
+    if constexpr (SRC == SRC_F32) {
+      uint32_t most = 0;
 #pragma unroll
-  for (int q = 0; q < 8; ++q) bf16_parts<P>(raw_value<SRC>(r, q), w[q]);
+      for (int q = 0; q < 8; ++q) {
+        x[q] = r.w[q];
+        most = max(most, x[q] & 0x7fffffffu);
+      }
+      odd = most >= 0x7f800000u;
+    } else {
+      typedef unsigned short v2h __attribute__((ext_vector_type(2)));
+      v2h most = {0, 0};
 #pragma unroll
-  for (int t = 0; t < P; ++t)
+      for (int q = 0; q < 4; ++q) {
+        most = __builtin_elementwise_max(most, __builtin_bit_cast(v2h, r.w[q] & 0x7fff7fffu));
+        x[2 * q] = __builtin_bit_cast(uint32_t, (float)__builtin_bit_cast(_Float16, (uint16_t)r.w[q]));
+        x[2 * q + 1] = __builtin_bit_cast(uint32_t, (float)__builtin_bit_cast(_Float16, (uint16_t)(r.w[q] >> 16)));
+      }
+      odd = most.x >= 0x7c00 || most.y >= 0x7c00;
+    }
+    uint32_t rest[8];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) out[t][q] = w[2 * q][t] | (uint32_t)w[2 * q + 1][t] << 16;
+    for (int q = 0; q < 8; ++q) rest[q] = x[q];
+#pragma unroll
+    for (int t = 0; t < P; ++t) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) out[t][q] = __builtin_amdgcn_perm(rest[2 * q + 1], rest[2 * q], 0x07060302u);
+      if (t + 1 < P)
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+          rest[q] = __builtin_bit_cast(
+              uint32_t, __builtin_bit_cast(float, rest[q]) - __builtin_bit_cast(float, rest[q] & 0xffff0000u));
+    }
+    if (__any(odd)) {
+      uint16_t w[8][P];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) bf16_parts<P>(__builtin_bit_cast(float, x[q]), w[q]);
+#pragma unroll
+      for (int t = 0; t < P; ++t)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) out[t][q] = w[2 * q][t] | (uint32_t)w[2 * q + 1][t] << 16;
+    }
+  }
 }
 
 __device__ inline v4f mfma_bf16(v4u a, v4u b, v4f c) {

@@ -136,6 +136,7 @@ __global__ __launch_bounds__(kThreads) void quantize_tiles(TileArgs a, MxLayoutA
   __shared__ float tile[kTile * kTileStride];
   __shared__ int32_t line_cls[LAYOUT ? kTile : 1], place_cls[LAYOUT ? kTile : 1];
   __shared__ int64_t line_local[LAYOUT ? kTile : 1], place_local[LAYOUT ? kTile : 1];
+  constexpr int V = 16 / (int)sizeof(T);  // elements of a 16-byte load
   const int tid = threadIdx.x;
   for (int64_t t = blockIdx.x; t < a.tiles; t += gridDim.x) {
     const int64_t line0 = t / a.tiles_x * kTile, place0 = t % a.tiles_x * kTile;
@@ -148,19 +149,51 @@ __global__ __launch_bounds__(kThreads) void quantize_tiles(TileArgs a, MxLayoutA
         else locate(l.place, i, place_cls[k], place_local[k]);
       }
       __syncthreads();
-      const int place = tid % kTile;
-      const bool in = place0 + place < a.len;
-      for (int line = tid / kTile; line < kTile; line += kThreads / kTile) {
-        float x = 0.0f;
-        if (in && line0 + line < a.lines) {
-          const MxCell& cell = l.cells[(int64_t)line_cls[line] * l.nplace + place_cls[place]];
-          const T* p = static_cast<const T*>(ptrs.p[cell.rank]);
-          x = to_float(p[cell.offset + line_local[line] * cell.ld + place_local[place]]) * a.alpha;
+      // a lane takes V neighbouring places of every 8th (16th) line; where they lie
+      // next to one another in memory, in one load.  The cell changes where a line's
+      // block does.
+      constexpr int LANES = kTile / V, ROWS = kThreads / LANES, BATCH = 8;
+      const int place = tid % LANES * V;
+      const int64_t c = place0 + place;
+      const bool run = c + V <= a.len && place_cls[place] == place_cls[place + V - 1] &&
+                       place_local[place + V - 1] == place_local[place] + V - 1;
+      int32_t last_cls = -1;
+      const T* base = nullptr;
+      int64_t ld = 0;
+      for (int first = tid / LANES; first < kTile; first += ROWS * BATCH) {
+        alignas(16) T v[BATCH][V];
+#pragma unroll
+        for (int q = 0; q < BATCH; ++q) {
+          const int line = first + ROWS * q;
+          if (line0 + line >= a.lines) continue;
+          if (run) {
+            if (line_cls[line] != last_cls) {
+              last_cls = line_cls[line];
+              const MxCell& cell = l.cells[(int64_t)last_cls * l.nplace + place_cls[place]];
+              base = static_cast<const T*>(ptrs.p[cell.rank]) + cell.offset + place_local[place];
+              ld = cell.ld;
+            }
+            __builtin_memcpy(v[q], base + line_local[line] * ld, sizeof v[q]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+              if (c + e < a.len) {
+                const MxCell& cell = l.cells[(int64_t)line_cls[line] * l.nplace + place_cls[place + e]];
+                v[q][e] = static_cast<const T*>(
+                    ptrs.p[cell.rank])[cell.offset + line_local[line] * cell.ld + place_local[place + e]];
+              }
+          }
         }
-        tile[tile_at(line, place)] = x;
+#pragma unroll
+        for (int q = 0; q < BATCH; ++q) {
+          const int line = first + ROWS * q;
+#pragma unroll
+          for (int e = 0; e < V; ++e)
+            tile[tile_at(line, place + e)] =
+                line0 + line < a.lines && c + e < a.len ? to_float(v[q][e]) * a.alpha : 0.0f;
+        }
       }
     } else {
-      constexpr int V = 16 / (int)sizeof(T);  // elements of a 16-byte load
       const T* src = static_cast<const T*>(a.src);
       for (int item = tid; item < kTile * kTile / V; item += kThreads) {
         const int line = item / (kTile / V), place = item % (kTile / V) * V;

@@ -52,46 +52,58 @@ struct LeftStage {
   uint32_t scale[MX ? PASSES : 1];
   uint32_t line[TRANS ? 8 : 1][TW];
 
+  // (Where a whole step is there, all of its loads stand behind one branch: none
+  // waits for another.)
   __device__ inline void load(const Args& p, int64_t i0, int64_t k0) {
     const int t = threadIdx.x;
     if constexpr (TRANS) {
       // wave w has k = k0 + 8 w .. + 7, lane l rows MPT l .. of each
-      const int64_t i = i0 + MPT * (t % 64);
-      const int64_t left = p.m - i;
+      const int wave = __builtin_amdgcn_readfirstlane(t / 64);
+      const char* base = static_cast<const char*>(p.real) + ((k0 + 8 * wave) * p.a_cs + i0) * ES;
+      const int at = MPT * ES * (t % 64);
+      const int64_t left = p.m - i0 - MPT * (t % 64);
 #pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        const int64_t k = k0 + 8 * (t / 64) + q;
-        const char* at = static_cast<const char*>(p.real) + (k * p.a_cs + i) * ES;
+      for (int q = 0; q < 8; ++q)
 #pragma unroll
         for (int w = 0; w < TW; ++w) line[q][w] = 0;
-        if (k < p.k) {
-          if (left >= MPT) {
-            __builtin_memcpy(line[q], at, MPT * ES);
-          } else {
+      if (left >= MPT && k0 + kStepBf16 <= p.k) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) __builtin_memcpy(line[q], base + q * p.a_cs * ES + at, MPT * ES);
+      } else if (left > 0) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+          if (k0 + 8 * wave + q < p.k) {
+            const char* from = base + q * p.a_cs * ES + at;
 #pragma unroll
             for (int e = 0; e < MPT; ++e)
               if (e < left) {
-                if (ES == 4) line[q][e % TW] = reinterpret_cast<const uint32_t*>(at)[e];
-                else line[q][e / 2 % TW] |= (uint32_t) reinterpret_cast<const uint16_t*>(at)[e] << (e % 2 * 16);
+                if (ES == 4) line[q][e % TW] = reinterpret_cast<const uint32_t*>(from)[e];
+                else line[q][e / 2 % TW] |= (uint32_t) reinterpret_cast<const uint16_t*>(from)[e] << (e % 2 * 16);
               }
           }
-        }
       }
     } else {
       const int c = t % 8;
+      const int64_t k = k0 + 8 * c;
+      if constexpr (MX) {
 #pragma unroll
-      for (int q = 0; q < PASSES; ++q) {
-        const int64_t i = min(i0 + t / 8 + 64 * q, p.m - 1), k = k0 + 8 * c;
-        if constexpr (MX) {
-          code[q] = v2u{0u, 0u};
-          scale[q] = 0;
-          if (k < p.a.row_scales * kMxBlock) {
-            const uint8_t* at = p.a.data + i * p.a.row_bytes;
-            if (BITS == 4) code[q].x = *reinterpret_cast<const uint32_t*>(at + k / 2);
-            else code[q] = *reinterpret_cast<const v2u*>(at + k);
-            scale[q] = p.a.scales[i * p.a.row_scales + k / kMxBlock];
-          }
-        } else {
+        for (int q = 0; q < PASSES; ++q) {  // (a row is padded to whole steps)
+          const int64_t i = min(i0 + t / 8 + 64 * q, p.m - 1);
+          const uint8_t* at = p.a.data + i * p.a.row_bytes;
+          if (BITS == 4) code[q] = v2u{*reinterpret_cast<const uint32_t*>(at + k / 2), 0u};
+          else code[q] = *reinterpret_cast<const v2u*>(at + k);
+          scale[q] = p.a.scales[i * p.a.row_scales + k / kMxBlock];
+        }
+      } else if (k0 + kStepBf16 <= p.k) {
+#pragma unroll
+        for (int q = 0; q < PASSES; ++q) {
+          const int64_t i = min(i0 + t / 8 + 64 * q, p.m - 1);
+          __builtin_memcpy(raw[q].w, static_cast<const char*>(p.real) + (i * p.a_rs + k) * ES, sizeof raw[q].w);
+        }
+      } else {
+#pragma unroll
+        for (int q = 0; q < PASSES; ++q) {
+          const int64_t i = min(i0 + t / 8 + 64 * q, p.m - 1);
           raw[q] = load8<SRC>(static_cast<const char*>(p.real) + (i * p.a_rs + k) * ES, p.k - k);
         }
       }
@@ -169,7 +181,8 @@ struct RightStage {
   }
 };
 
-template <int SRC, bool TRANS, int BBITS, int BM, int BN, int WM>
+// AHEAD: steps whose loads are on their way at once.
+template <int SRC, bool TRANS, int BBITS, int BM, int BN, int WM, int AHEAD>
 __global__ __launch_bounds__(kLanes) void tiles_bf16(Args p, int64_t nm, int64_t nn) {
   constexpr int WN = kWaves / WM, MT = BM / WM / 16, NT = BN / WN / 16, P = parts_of(SRC);
   constexpr int BROW = kStepBf16 * BBITS / 8;
@@ -190,56 +203,61 @@ __global__ __launch_bounds__(kLanes) void tiles_bf16(Args p, int64_t nm, int64_t
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = v4f{0, 0, 0, 0};
 
-  LeftStage<SRC, TRANS, BM> ls;
-  RightStage<BBITS, BN> rs;
-  ls.load(p, i0, first * kStepBf16);
-  rs.load(p, j0, first * kStepBf16);
-  ls.store(left[0]);
-  rs.store(right[0], scales[0]);
-  if (first + 1 < last) {
-    ls.load(p, i0, (first + 1) * kStepBf16);
-    rs.load(p, j0, (first + 1) * kStepBf16);
-  }
+  LeftStage<SRC, TRANS, BM> ls[AHEAD];
+  RightStage<BBITS, BN> rs[AHEAD];
+  auto load = [&](int set, int64_t t) {
+    if (t < last) {
+      ls[set].load(p, i0, t * kStepBf16);
+      rs[set].load(p, j0, t * kStepBf16);
+    }
+  };
+  load(0, first);
+  ls[0].store(left[0]);
+  rs[0].store(right[0], scales[0]);
+#pragma unroll
+  for (int a = 1; a <= AHEAD; ++a) load(a % AHEAD, first + a);
   __syncthreads();
-  for (int64_t t = first; t < last; ++t) {
-    const int s = (int)(t - first) & 1;
-    v4u b[NT];
-    uint32_t sc[NT];
+  for (int64_t t0 = first; t0 < last; t0 += 2) {
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      const int row = wn + 16 * j + r;
-      if (BBITS == 4) {
-        const v2u d = reinterpret_cast<const v2u*>(right[s])[row * 4 + g];
-        b[j] = v4u{d.x, d.y, 0u, 0u};
-      } else {
-        b[j] = right[s][row * 4 + g];
-      }
-      sc[j] = reinterpret_cast<const uint8_t*>(scales[s])[row * 2 + g / 2];
-    }
+    for (int s = 0; s < 2; ++s) {
+      const int64_t t = t0 + s;
+      if (t >= last) break;
+      v4u b[NT];
+      uint32_t sc[NT];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      v4u w[NT];
-#pragma unroll
-      for (int j = 0; j < NT; ++j)
-        w[j] = mx_decode8_bf16<BBITS>(BBITS == 4 ? v2u{b[j][h], 0u} : v2u{b[j][2 * h], b[j][2 * h + 1]}, sc[j]);
-#pragma unroll
-      for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int x = 0; x < P; ++x) {
-          const v4u a = left[s][x * BM * 8 + chunk_at(wm + 16 * i + r, 2 * g + h)];
-#pragma unroll
-          for (int j = 0; j < NT; ++j) acc[i][j] = mfma_bf16(w[j], a, acc[i][j]);
+      for (int j = 0; j < NT; ++j) {
+        const int row = wn + 16 * j + r;
+        if (BBITS == 4) {
+          const v2u d = reinterpret_cast<const v2u*>(right[s])[row * 4 + g];
+          b[j] = v4u{d.x, d.y, 0u, 0u};
+        } else {
+          b[j] = right[s][row * 4 + g];
         }
-    }
-    if (t + 1 < last) {
-      ls.store(left[1 - s]);
-      rs.store(right[1 - s], scales[1 - s]);
-      if (t + 2 < last) {
-        ls.load(p, i0, (t + 2) * kStepBf16);
-        rs.load(p, j0, (t + 2) * kStepBf16);
+        sc[j] = reinterpret_cast<const uint8_t*>(scales[s])[row * 2 + g / 2];
       }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        v4u w[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+          w[j] = mx_decode8_bf16<BBITS>(BBITS == 4 ? v2u{b[j][h], 0u} : v2u{b[j][2 * h], b[j][2 * h + 1]}, sc[j]);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int x = 0; x < P; ++x) {
+            const v4u a = left[s][x * BM * 8 + chunk_at(wm + 16 * i + r, 2 * g + h)];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) acc[i][j] = mfma_bf16(w[j], a, acc[i][j]);
+          }
+      }
+      if (t + 1 < last) {
+        const int set = (s + 1) % AHEAD;  // (AHEAD is 1 or 2: a step's parity is its set)
+        ls[set].store(left[1 - s]);
+        rs[set].store(right[1 - s], scales[1 - s]);
+        load(set, t + 1 + AHEAD);
+      }
+      __syncthreads();
     }
-    __syncthreads();
   }
   Epilogue e = p.e;
   if (p.part) e.c = static_cast<float*>(e.c) + blockIdx.y * p.part;
@@ -387,8 +405,8 @@ hipError_t launch_bf16(const Args& p, const ProductPlan& plan, hipStream_t strea
   constexpr int BM = parts_of(SRC) == 1 ? 256 : 128;
   const int64_t nm = (p.m + plan.bm - 1) / plan.bm, nn = (p.n + plan.bn - 1) / plan.bn;
   const dim3 grid((unsigned)(nm * nn), plan.splits);
-  if (plan.bn == 256) tiles_bf16<SRC, TRANS, BBITS, BM, 256, 2><<<grid, kLanes, 0, stream>>>(p, nm, nn);
-  else tiles_bf16<SRC, TRANS, BBITS, 128, 64, 4><<<grid, kLanes, 0, stream>>>(p, nm, nn);
+  if (plan.bn == 256) tiles_bf16<SRC, TRANS, BBITS, BM, 256, 2, 1><<<grid, kLanes, 0, stream>>>(p, nm, nn);
+  else tiles_bf16<SRC, TRANS, BBITS, 128, 64, 4, 2><<<grid, kLanes, 0, stream>>>(p, nm, nn);
   return hipGetLastError();
 }
 template <int SRC, bool TRANS>
