@@ -281,12 +281,27 @@ __global__ __launch_bounds__(256) void scale_only(Epilogue e, int64_t m, int64_t
 // ---- which kernel -------------------------------------------------------------------
 constexpr size_t kPartsMax = (size_t)256 << 20;  // bytes of a split sum's parts
 
-// Splits of a sum of `steps` steps over workgroups that fill the device, when
-// `groups` of them make the tiles: not below `least` steps each.
-int splits_for(int64_t groups, int64_t want, int64_t steps, int64_t least, int64_t m, int64_t n) {
-  int64_t s = std::min(want / std::max<int64_t>(groups, 1), steps / least);
-  s = std::min<int64_t>(s, (int64_t)(kPartsMax / 4) / std::max<int64_t>(m * n, 1));
-  return (int)std::max<int64_t>(s, 1);
+int64_t up_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Most splits that the parts' memory allows.
+int64_t splits_max(int64_t m, int64_t n) {
+  return std::max<int64_t>((int64_t)(kPartsMax / 4) / std::max<int64_t>(m * n, 1), 1);
+}
+
+// Estimated time of a tiled product in us, from what MI355X measured.  A
+// workgroup's step of k takes `step` us when the CU has w of them, max(alone, w *
+// share): bfloat16, k by 64: 1.77 us for a 256x256 tile (one a CU), 0.57 a tile for
+// several of 128x128, 0.39 of 128x64, not below 0.66 (the way from memory through
+// shared memory); 4 bits, k by 256: 2.6 us at 256x256, 0.76 at 128x128, not below 1.0.
+// Joining a split sum costs a launch and its parts' way to memory and back.
+// (512x8192x8192 in bfloat16: 128x128 unsplit 88 us, 256x256 unsplit 232, split in four 86;
+// 256x8192x8192: 128x128 split in four 53, 128x64 unsplit 72; 1024^3: 128x64 13, 128x128 17.)
+double tiled_time(bool scaled, int parts, int64_t bm, int64_t bn, int64_t splits, int64_t m, int64_t n, int64_t k) {
+  const double size = (double)(bm * bn * parts) / 65536.0;
+  const double share = scaled ? 0.2 + 2.4 * size : 0.22 + 1.55 * size, alone = scaled ? 1.0 : 0.66;
+  const int64_t groups = up_div(m, bm) * up_div(n, bn) * splits, steps = up_div(up_div(k, scaled ? 256 : 64), splits);
+  const double step = std::max(alone, (double)up_div(groups, kCUs) * share);
+  return 3.0 + (double)steps * step + (splits > 1 ? 3.0 + (double)splits * m * n * 8e-6 / 4.0 : 0.0);
 }
 
 ProductPlan plan_product(int src, bool k_next, int bbits, int64_t m, int64_t n, int64_t k) {
@@ -296,24 +311,34 @@ ProductPlan plan_product(int src, bool k_next, int bbits, int64_t m, int64_t n, 
     r.bm = m <= 16 ? 16 : m <= 32 ? 32 : 64;
     // (32 columns share a slab's way through shared memory; half as many workgroups)
     r.bn = m > 4 && n >= 64 * kCUs ? 32 : 16;
-    const int64_t units = (k + 1024 / bbits - 1) / (1024 / bbits);
-    r.splits = splits_for((n + r.bn - 1) / r.bn, kCUs, units, 4 * kFewWaves, m, n);
+    const int64_t units = up_div(k, 1024 / bbits);
+    const int64_t s = std::min(kCUs / std::max<int64_t>(up_div(n, r.bn), 1), units / (4 * kFewWaves));
+    r.splits = (int)std::max<int64_t>(std::min(s, splits_max(m, n)), 1);
     return r;
   }
   // (the scaled kernel counts a tile's bytes in 32 bits)
   const bool scaled = src == SRC_MX4 && bbits == 4 && k <= 1 << 24;
   r.variant = scaled ? TILES_SCALED : TILES_BF16;
-  const int big = scaled || parts_of(src) == 1 ? 256 : 128;
-  const auto tiles = [&](int64_t bm, int64_t bn) { return (m + bm - 1) / bm * ((n + bn - 1) / bn); };
-  if (tiles(big, 256) >= kCUs / 2) {
-    r.bm = big;
-    r.bn = 256;
-  } else {
-    r.bm = 128;
-    r.bn = scaled ? 128 : 64;
+  const int parts = scaled ? 1 : parts_of(src);
+  const int64_t most = std::min({splits_max(m, n), up_div(k, scaled ? 1024 : 256), (int64_t)kCUs});
+  double best = 0;
+  for (const int bn : {256, 128, 64}) {
+    if (scaled && bn == 64) continue;
+    const int bm = bn == 256 && parts == 1 ? 256 : 128;
+    const int64_t tiles = up_div(m, bm) * up_div(n, bn);
+    // unsplit, in a few, or so that the workgroups are one to four for every CU
+    for (int64_t c = 0; c < 8; ++c) {
+      const int64_t s = c < 4 ? c + 1 : (c - 3) * kCUs / std::max<int64_t>(tiles, 1);
+      if (s < 1 || s > most) continue;
+      const double t = tiled_time(scaled, parts, bm, bn, s, m, n, k);
+      if (r.splits == 0 || t < best) {
+        best = t;
+        r.bm = bm;
+        r.bn = bn;
+        r.splits = (int)s;
+      }
+    }
   }
-  const int64_t step = scaled ? 256 : 64;
-  r.splits = splits_for(tiles(r.bm, r.bn), kCUs, (k + step - 1) / step, 4, m, n);
   return r;
 }
 
@@ -321,6 +346,7 @@ ProductPlan plan_product(int src, bool k_next, int bbits, int64_t m, int64_t n, 
 
 size_t mx_product_workspace(int64_t m, int64_t n, int64_t k) {
   size_t most = 0;
+  if (m == 0 || n == 0 || k == 0) return 0;
   for (int src : {SRC_MX4, SRC_MX8, SRC_BF16, SRC_F16, SRC_F32})
     for (int bbits : {4, 8})
       for (bool k_next : {true, false}) {

@@ -30,7 +30,7 @@ __device__ inline uint32_t magnitude(float x) { return __builtin_bit_cast(uint32
 // elements and writes them.  No shared memory.
 template <typename T, int BITS>
 __global__ __launch_bounds__(kThreads) void quantize_lines(const T* src, int64_t ld, int64_t lines, int64_t len,
-                                                           float alpha, MxView q, bool wide) {
+                                                           float alpha, MxView q) {
   const uint32_t upl = (uint32_t)(q.row_scales * 4);  // units of 8 elements of a padded line
   const int64_t units = lines * upl;
   for (int64_t u0 = (int64_t)blockIdx.x * kThreads; u0 < units; u0 += (int64_t)gridDim.x * kThreads) {
@@ -42,11 +42,9 @@ __global__ __launch_bounds__(kThreads) void quantize_lines(const T* src, int64_t
     const bool here = line < lines;
     float x[8];
     const T* p = src + line * ld + c;
-    if (here && wide && c + 8 <= len) {
+    if (here && c + 8 <= len) {
       alignas(16) T v[8];
-#pragma unroll
-      for (size_t i = 0; i < 8 * sizeof(T) / 16; ++i)
-        *reinterpret_cast<v4u*>(reinterpret_cast<char*>(v) + 16 * i) = reinterpret_cast<const v4u*>(p)[i];
+      __builtin_memcpy(v, p, sizeof v);  // (vector loads need no alignment)
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = to_float(v[i]) * alpha;
     } else {
@@ -67,24 +65,38 @@ __global__ __launch_bounds__(kThreads) void quantize_lines(const T* src, int64_t
 }
 
 // ---- either direction, any source, through a tile in shared memory -------------
-// A tile is 128 lines by 128 elements as 32-bit floats, with a gap after every
-// 32 elements and an odd line stride: lanes that read blocks along the lines
-// (four blocks of a line, then the next line) and blocks across them meet few
-// equal banks.
-constexpr int kTile = 128;
-constexpr int kTileStride = kTile + 5;
-__device__ inline int tile_at(int line, int place) { return line * kTileStride + place + place / 32; }
+// A tile is 128 lines by 128 (16-bit types, held as they are) or 64 places (held as
+// 32-bit floats): 34 KiB, so that four workgroups of a CU overlap their loads with
+// the others' arithmetic.  A gap of 4 bytes after every 32 elements and an odd number
+// of words a line let lanes that read blocks along the lines (the blocks of a line,
+// then the next line) and across them meet few equal banks.
+constexpr int kLines = 128;
+template <typename T>
+struct Tile {
+  static constexpr bool HALF = sizeof(T) == 2;
+  typedef typename std::conditional<HALF, T, float>::type S;
+  static constexpr int PLACES = HALF ? 128 : 64;
+  static constexpr int GAP = 4 / (int)sizeof(S);
+  static constexpr int STRIDE = HALF ? 138 : 67;
+  static __device__ inline int at(int line, int place) { return line * STRIDE + place + place / 32 * GAP; }
+};
 
-// One block of 32 elements out of the tile: `step` apart from x on.
-template <int BITS>
-__device__ inline void put_block(const float* tile, bool across, int line, int place, uint8_t* data, uint8_t* scale) {
+// One block of 32 elements out of the tile, of which n are the matrix's.
+template <typename T, int BITS>
+__device__ inline void put_block(const typename Tile<T>::S* tile, bool across, int line, int place, int64_t n,
+                                 float alpha, uint8_t* data, uint8_t* scale) {
   float x[32];
   uint32_t m = 0;
 #pragma unroll
   for (int i = 0; i < 32; ++i) {
-    x[i] = across ? tile[tile_at(line + i, place)] : tile[tile_at(line, place) + i];
-    m = max(m, magnitude(x[i]));
+    const float v = (float)(across ? tile[Tile<T>::at(line + i, place)] : tile[Tile<T>::at(line, place) + i]);
+    x[i] = v * alpha;
   }
+  if (n < 32)  // what pads a row is +0, whatever alpha
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x[i] = i < n ? x[i] : 0.0f;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) m = max(m, magnitude(x[i]));
   const uint32_t s = mx_scale<BITS>(m);
   v2u d[4];
 #pragma unroll
@@ -98,16 +110,20 @@ __device__ inline void put_block(const float* tile, bool across, int line, int p
   *scale = (uint8_t)s;
 }
 
-// The blocks of a tile in one direction.  `outer` counts q's rows, `inner` its columns.
-__device__ inline void put_tile(const float* tile, bool across, const MxView& q, int64_t row0, int64_t col0) {
-  for (int item = threadIdx.x; item < kTile * 4; item += kThreads) {
-    const int r = item / 4, b = item % 4;
+// The blocks of a tile in one direction: ROWS of q, BLOCKS of each.
+template <typename T, bool ACROSS>
+__device__ inline void put_tile(const typename Tile<T>::S* tile, const MxView& q, int64_t row0, int64_t col0,
+                                float alpha) {
+  constexpr int ROWS = ACROSS ? Tile<T>::PLACES : kLines, BLOCKS = (ACROSS ? kLines : Tile<T>::PLACES) / 32;
+  for (int item = threadIdx.x; item < ROWS * BLOCKS; item += kThreads) {
+    const int r = item / BLOCKS, b = item % BLOCKS;
     const int64_t row = row0 + r, col = col0 + 32 * b;
     if (row >= q.rows || col >= q.row_scales * kMxBlock) continue;
     uint8_t* scale = q.scales + row * q.row_scales + col / kMxBlock;
-    const int line = across ? 32 * b : r, place = across ? r : 32 * b;
-    if (q.bits == 4) put_block<4>(tile, across, line, place, q.data + row * q.row_bytes + col / 2, scale);
-    else put_block<8>(tile, across, line, place, q.data + row * q.row_bytes + col, scale);
+    const int line = ACROSS ? 32 * b : r, place = ACROSS ? r : 32 * b;
+    const int64_t n = q.cols - col;
+    if (q.bits == 4) put_block<T, 4>(tile, ACROSS, line, place, n, alpha, q.data + row * q.row_bytes + col / 2, scale);
+    else put_block<T, 8>(tile, ACROSS, line, place, n, alpha, q.data + row * q.row_bytes + col, scale);
   }
 }
 
@@ -127,94 +143,97 @@ struct TileArgs {
   const void* src;
   int64_t ld, lines, len, tiles_x, tiles;
   float alpha;
-  bool wide;
   MxView along, across;
 };
 
-template <typename T, bool LAYOUT>
-__global__ __launch_bounds__(kThreads) void quantize_tiles(TileArgs a, MxLayoutArgs l, MxPointers ptrs) {
-  __shared__ float tile[kTile * kTileStride];
-  __shared__ int32_t line_cls[LAYOUT ? kTile : 1], place_cls[LAYOUT ? kTile : 1];
-  __shared__ int64_t line_local[LAYOUT ? kTile : 1], place_local[LAYOUT ? kTile : 1];
-  constexpr int V = 16 / (int)sizeof(T);  // elements of a 16-byte load
+// A lane takes V neighbouring places of every LINES-th line, BATCH loads at a time;
+// those that are next to one another in memory in one load, of any alignment.
+struct Dealt {
+  MxLayoutArgs l;
+  MxPointers ptrs;
+};
+struct Plain {};
+template <typename T, typename Where>
+__global__ __launch_bounds__(kThreads) void quantize_tiles(TileArgs a, Where where) {
+  constexpr bool LAYOUT = std::is_same<Where, Dealt>::value;
+  typedef Tile<T> Ti;
+  typedef typename Ti::S S;
+  constexpr int V = 16 / (int)sizeof(T), LANES = Ti::PLACES / V, LINES = kThreads / LANES;
+  constexpr int PASSES = kLines / LINES, BATCH = PASSES < 8 ? PASSES : 8;
+  __shared__ S tile[kLines * Ti::STRIDE];
+  __shared__ int32_t line_cls[LAYOUT ? kLines : 1], place_cls[LAYOUT ? Ti::PLACES : 1];
+  __shared__ int64_t line_local[LAYOUT ? kLines : 1], place_local[LAYOUT ? Ti::PLACES : 1];
   const int tid = threadIdx.x;
+  const int place = tid % LANES * V;
   for (int64_t t = blockIdx.x; t < a.tiles; t += gridDim.x) {
-    const int64_t line0 = t / a.tiles_x * kTile, place0 = t % a.tiles_x * kTile;
-    if (LAYOUT) {
-      const bool is_line = tid < kTile;
-      const int k = tid % kTile;
-      const int64_t i = (is_line ? line0 : place0) + k;
-      if (i < (is_line ? a.lines : a.len)) {
-        if (is_line) locate(l.line, i, line_cls[k], line_local[k]);
-        else locate(l.place, i, place_cls[k], place_local[k]);
+    const int64_t line0 = t / a.tiles_x * kLines, place0 = t % a.tiles_x * Ti::PLACES;
+    const int64_t c = place0 + place;
+    bool run = c + V <= a.len;
+    if constexpr (LAYOUT) {
+      const MxLayoutArgs& l = where.l;
+      if (tid < kLines) {
+        if (line0 + tid < a.lines) locate(l.line, line0 + tid, line_cls[tid], line_local[tid]);
+      } else if (tid < kLines + Ti::PLACES) {
+        const int k = tid - kLines;
+        if (place0 + k < a.len) locate(l.place, place0 + k, place_cls[k], place_local[k]);
       }
       __syncthreads();
-      // a lane takes V neighbouring places of every 8th (16th) line; where they lie
-      // next to one another in memory, in one load.  The cell changes where a line's
-      // block does.
-      constexpr int LANES = kTile / V, ROWS = kThreads / LANES, BATCH = 8;
-      const int place = tid % LANES * V;
-      const int64_t c = place0 + place;
-      const bool run = c + V <= a.len && place_cls[place] == place_cls[place + V - 1] &&
-                       place_local[place + V - 1] == place_local[place] + V - 1;
-      int32_t last_cls = -1;
-      const T* base = nullptr;
-      int64_t ld = 0;
-      for (int first = tid / LANES; first < kTile; first += ROWS * BATCH) {
-        alignas(16) T v[BATCH][V];
+      run = run && place_cls[place] == place_cls[place + V - 1] &&
+            place_local[place + V - 1] == place_local[place] + V - 1;
+    }
+    int32_t last_cls = -1;  // the cell changes where a line's block does
+    const T* base = static_cast<const T*>(a.src) + c;
+    int64_t ld = a.ld;
+#pragma unroll 1
+    for (int first = tid / LANES; first < kLines; first += LINES * BATCH) {
+      alignas(16) T v[BATCH][V];
+      if (run) {
 #pragma unroll
         for (int q = 0; q < BATCH; ++q) {
-          const int line = first + ROWS * q;
-          if (line0 + line >= a.lines) continue;
-          if (run) {
+          const int line = first + LINES * q;
+          if (line0 + line >= a.lines) break;
+          int64_t at = line0 + line;
+          if constexpr (LAYOUT) {
             if (line_cls[line] != last_cls) {
               last_cls = line_cls[line];
-              const MxCell& cell = l.cells[(int64_t)last_cls * l.nplace + place_cls[place]];
-              base = static_cast<const T*>(ptrs.p[cell.rank]) + cell.offset + place_local[place];
+              const MxCell& cell = where.l.cells[(int64_t)last_cls * where.l.nplace + place_cls[place]];
+              base = static_cast<const T*>(where.ptrs.p[cell.rank]) + cell.offset + place_local[place];
               ld = cell.ld;
             }
-            __builtin_memcpy(v[q], base + line_local[line] * ld, sizeof v[q]);
-          } else {
-#pragma unroll
-            for (int e = 0; e < V; ++e)
-              if (c + e < a.len) {
-                const MxCell& cell = l.cells[(int64_t)line_cls[line] * l.nplace + place_cls[place + e]];
-                v[q][e] = static_cast<const T*>(
-                    ptrs.p[cell.rank])[cell.offset + line_local[line] * cell.ld + place_local[place + e]];
-              }
+            at = line_local[line];
           }
+          __builtin_memcpy(v[q], base + at * ld, sizeof v[q]);
         }
+      } else {
 #pragma unroll
         for (int q = 0; q < BATCH; ++q) {
-          const int line = first + ROWS * q;
+          const int line = first + LINES * q;
+          if (line0 + line >= a.lines) break;
 #pragma unroll
           for (int e = 0; e < V; ++e)
-            tile[tile_at(line, place + e)] =
-                line0 + line < a.lines && c + e < a.len ? to_float(v[q][e]) * a.alpha : 0.0f;
+            if (c + e < a.len) {
+              if constexpr (LAYOUT) {
+                const MxCell& cell =
+                    where.l.cells[(int64_t)line_cls[line] * where.l.nplace + place_cls[place + e]];
+                v[q][e] = static_cast<const T*>(
+                    where.ptrs.p[cell.rank])[cell.offset + line_local[line] * cell.ld + place_local[place + e]];
+              } else {
+                v[q][e] = base[(line0 + line) * ld + e];
+              }
+            }
         }
       }
-    } else {
-      const T* src = static_cast<const T*>(a.src);
-      for (int item = tid; item < kTile * kTile / V; item += kThreads) {
-        const int line = item / (kTile / V), place = item % (kTile / V) * V;
-        const int64_t c = place0 + place;
-        const T* p = src + (line0 + line) * a.ld + c;
-        if (a.wide && line0 + line < a.lines && c + V <= a.len) {
-          alignas(16) T v[V];
-          *reinterpret_cast<v4u*>(v) = *reinterpret_cast<const v4u*>(p);
 #pragma unroll
-          for (int i = 0; i < V; ++i) tile[tile_at(line, place + i)] = to_float(v[i]) * a.alpha;
-        } else {
+      for (int q = 0; q < BATCH; ++q) {
+        const int line = first + LINES * q;
+        const bool there = line0 + line < a.lines;
 #pragma unroll
-          for (int i = 0; i < V; ++i)
-            tile[tile_at(line, place + i)] =
-                line0 + line < a.lines && c + i < a.len ? to_float(p[i]) * a.alpha : 0.0f;
-        }
+        for (int e = 0; e < V; ++e) tile[Ti::at(line, place + e)] = there && c + e < a.len ? (S)v[q][e] : (S)0.0f;
       }
     }
     __syncthreads();
-    if (a.along.data) put_tile(tile, false, a.along, line0, place0);
-    if (a.across.data) put_tile(tile, true, a.across, place0, line0);
+    if (a.along.data) put_tile<T, false>(tile, a.along, line0, place0, a.alpha);
+    if (a.across.data) put_tile<T, true>(tile, a.across, place0, line0, a.alpha);
     __syncthreads();
   }
 }
@@ -224,7 +243,7 @@ __global__ __launch_bounds__(kThreads) void quantize_tiles(TileArgs a, MxLayoutA
 // elements of a row (A by rows); else the same elements of neighbouring rows (A by
 // columns), whose 64 writes of a column are next to one another.
 template <typename T, int BITS, bool ROWS>
-__global__ __launch_bounds__(kThreads) void dequantize(DequantArgs a, bool wide) {
+__global__ __launch_bounds__(kThreads) void dequantize(DequantArgs a) {
   typedef typename std::conditional<std::is_same<T, double>::value, double, float>::type W;
   T* dst = static_cast<T*>(a.dst);
   const int64_t upr = (a.q.cols + 7) / 8;
@@ -234,9 +253,9 @@ __global__ __launch_bounds__(kThreads) void dequantize(DequantArgs a, bool wide)
     // ROWS: u = row * upr + unit; else u = unit * rows + row
     const int64_t per = ROWS ? upr : a.q.rows;
     const int64_t o0 = u0 / per;
-    const int64_t in = u0 - o0 * per + threadIdx.x;
-    const int64_t over = in < per ? 0 : in / per;
-    const int64_t outer = o0 + over, inner = in - over * per;
+    const uint32_t in = (uint32_t)(u0 - o0 * per) + threadIdx.x;  // (per is below 2^31)
+    const uint32_t over = in / (uint32_t)per;
+    const int64_t outer = o0 + over, inner = in - over * (uint32_t)per;
     const int64_t row = ROWS ? outer : inner, unit = ROWS ? inner : outer;
     if (outer >= (ROWS ? a.q.rows : upr)) continue;
     v2u d = {0u, 0u};
@@ -246,21 +265,17 @@ __global__ __launch_bounds__(kThreads) void dequantize(DequantArgs a, bool wide)
     mx_decode8<BITS>(d, a.q.scales[row * a.q.row_scales + unit / 4], x);
     T* p = dst + row * a.rs + unit * 8 * a.cs;
     const int n = (int)min((int64_t)8, a.q.cols - unit * 8);
-    if (ROWS && wide && n == 8) {
+    if (ROWS && n == 8) {  // (vector accesses need no alignment)
       alignas(16) T v[8];
       if (a.beta != 0.0f) {
-#pragma unroll
-        for (size_t i = 0; i < 8 * sizeof(T) / 16; ++i)
-          *reinterpret_cast<v4u*>(reinterpret_cast<char*>(v) + 16 * i) = reinterpret_cast<const v4u*>(p)[i];
+        __builtin_memcpy(v, p, sizeof v);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = (T)(alpha * (W)x[i] + beta * (W)v[i]);
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = (T)(alpha * (W)x[i]);
       }
-#pragma unroll
-      for (size_t i = 0; i < 8 * sizeof(T) / 16; ++i)
-        reinterpret_cast<v4u*>(p)[i] = *reinterpret_cast<const v4u*>(reinterpret_cast<const char*>(v) + 16 * i);
+      __builtin_memcpy(p, v, sizeof v);
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
@@ -277,41 +292,37 @@ inline dim3 grid_for(int64_t groups) { return dim3((unsigned)std::min<int64_t>(s
 
 template <typename T>
 hipError_t quantize_plain(const QuantArgs& a, hipStream_t stream) {
-  const bool wide = (uintptr_t)a.src % 16 == 0 && a.ld * sizeof(T) % 16 == 0;
-  if (!a.across.data) {
-    const int64_t units = a.lines * a.along.row_scales * 4;
-    const dim3 grid = grid_for((units + kThreads - 1) / kThreads);
-    if (a.along.bits == 4)
-      quantize_lines<T, 4><<<grid, kThreads, 0, stream>>>(static_cast<const T*>(a.src), a.ld, a.lines, a.len, a.alpha,
-                                                          a.along, wide);
-    else
-      quantize_lines<T, 8><<<grid, kThreads, 0, stream>>>(static_cast<const T*>(a.src), a.ld, a.lines, a.len, a.alpha,
-                                                          a.along, wide);
-    return hipGetLastError();
-  }
-  return hipSuccess;
+  const int64_t units = a.lines * a.along.row_scales * 4;
+  const dim3 grid = grid_for((units + kThreads - 1) / kThreads);
+  const T* src = static_cast<const T*>(a.src);
+  if (a.along.bits == 4)
+    quantize_lines<T, 4><<<grid, kThreads, 0, stream>>>(src, a.ld, a.lines, a.len, a.alpha, a.along);
+  else
+    quantize_lines<T, 8><<<grid, kThreads, 0, stream>>>(src, a.ld, a.lines, a.len, a.alpha, a.along);
+  return hipGetLastError();
 }
 
 // Tiles that cover the source and what pads either output.
-TileArgs tiles_of(const QuantArgs& a, bool wide) {
-  int64_t nx = (a.len + kTile - 1) / kTile, ny = (a.lines + kTile - 1) / kTile;
-  if (a.along.data) nx = std::max(nx, a.along.row_scales * kMxBlock / kTile);
-  if (a.across.data) ny = std::max(ny, a.across.row_scales * kMxBlock / kTile);
-  return TileArgs{a.src, a.ld, a.lines, a.len, nx, nx * ny, a.alpha, wide, a.along, a.across};
+template <typename T>
+TileArgs tiles_of(const QuantArgs& a) {
+  constexpr int PLACES = Tile<T>::PLACES;
+  int64_t nx = (a.len + PLACES - 1) / PLACES, ny = (a.lines + kLines - 1) / kLines;
+  if (a.along.data) nx = std::max(nx, a.along.row_scales * kMxBlock / PLACES);
+  if (a.across.data) ny = std::max(ny, a.across.row_scales * kMxBlock / kLines);
+  return TileArgs{a.src, a.ld, a.lines, a.len, nx, nx * ny, a.alpha, a.along, a.across};
 }
 
 template <typename T>
 hipError_t quantize_tiled(const QuantArgs& a, hipStream_t stream) {
-  const bool wide = (uintptr_t)a.src % 16 == 0 && a.ld * sizeof(T) % 16 == 0;
-  const TileArgs t = tiles_of(a, wide);
-  quantize_tiles<T, false><<<grid_for(t.tiles), kThreads, 0, stream>>>(t, MxLayoutArgs{}, MxPointers{});
+  const TileArgs t = tiles_of<T>(a);
+  quantize_tiles<T, Plain><<<grid_for(t.tiles), kThreads, 0, stream>>>(t, Plain{});
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t quantize_dealt(const QuantArgs& a, const MxLayoutArgs& l, const MxPointers& p, hipStream_t stream) {
-  const TileArgs t = tiles_of(a, false);
-  quantize_tiles<T, true><<<grid_for(t.tiles), kThreads, 0, stream>>>(t, l, p);
+  const TileArgs t = tiles_of<T>(a);
+  quantize_tiles<T, Dealt><<<grid_for(t.tiles), kThreads, 0, stream>>>(t, Dealt{l, p});
   return hipGetLastError();
 }
 
@@ -319,12 +330,8 @@ template <typename T, int BITS>
 hipError_t dequantize_typed(const DequantArgs& a, hipStream_t stream) {
   const int64_t units = a.q.rows * ((a.q.cols + 7) / 8);
   const dim3 grid = grid_for((units + kThreads - 1) / kThreads);
-  if (a.cs == 1) {
-    const bool wide = (uintptr_t)a.dst % 16 == 0 && a.rs * sizeof(T) % 16 == 0;
-    dequantize<T, BITS, true><<<grid, kThreads, 0, stream>>>(a, wide);
-  } else {
-    dequantize<T, BITS, false><<<grid, kThreads, 0, stream>>>(a, false);
-  }
+  if (a.cs == 1) dequantize<T, BITS, true><<<grid, kThreads, 0, stream>>>(a);
+  else dequantize<T, BITS, false><<<grid, kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 

@@ -405,8 +405,14 @@ hipError_t launch_bf16(const Args& p, const ProductPlan& plan, hipStream_t strea
   constexpr int BM = parts_of(SRC) == 1 ? 256 : 128;
   const int64_t nm = (p.m + plan.bm - 1) / plan.bm, nn = (p.n + plan.bn - 1) / plan.bn;
   const dim3 grid((unsigned)(nm * nn), plan.splits);
-  if (plan.bn == 256) tiles_bf16<SRC, TRANS, BBITS, BM, 256, 2, 1><<<grid, kLanes, 0, stream>>>(p, nm, nn);
-  else tiles_bf16<SRC, TRANS, BBITS, 128, 64, 4, 2><<<grid, kLanes, 0, stream>>>(p, nm, nn);
+  if (plan.bm == BM && plan.bn == 256)
+    tiles_bf16<SRC, TRANS, BBITS, BM, 256, 2, 1><<<grid, kLanes, 0, stream>>>(p, nm, nn);
+  else if (plan.bm == 128 && plan.bn == 128)
+    tiles_bf16<SRC, TRANS, BBITS, 128, 128, 2, 1><<<grid, kLanes, 0, stream>>>(p, nm, nn);
+  else if (plan.bm != 128 || plan.bn != 64)
+    return hipErrorInvalidValue;  // not a tile of this kernel
+  else
+    tiles_bf16<SRC, TRANS, BBITS, 128, 64, 4, 2><<<grid, kLanes, 0, stream>>>(p, nm, nn);
   return hipGetLastError();
 }
 template <int SRC, bool TRANS>
@@ -433,7 +439,8 @@ hipError_t launch_tiles_bf16(int src, const Args& p, const ProductPlan& plan, hi
 hipError_t launch_tiles_scaled(const Args& p, const ProductPlan& plan, hipStream_t stream) {
   const int64_t nm = (p.m + plan.bm - 1) / plan.bm, nn = (p.n + plan.bn - 1) / plan.bn;
   const dim3 grid((unsigned)(nm * nn), plan.splits);
-  if (plan.bn == 256) tiles_scaled<256, 256, 2><<<grid, kLanes, 0, stream>>>(p, nm, nn);
+  if (plan.bm == 256 && plan.bn == 256) tiles_scaled<256, 256, 2><<<grid, kLanes, 0, stream>>>(p, nm, nn);
+  else if (plan.bm != 128 || plan.bn != 128) return hipErrorInvalidValue;  // not a tile of this kernel
   else tiles_scaled<128, 128, 2><<<grid, kLanes, 0, stream>>>(p, nm, nn);
   return hipGetLastError();
 }

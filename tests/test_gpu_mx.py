@@ -131,6 +131,23 @@ def test_every_rounding(bits):
 
 
 @pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("alpha", [-1.0, 0.0, float("inf"), float("nan")])
+def test_scalars_leave_what_pads_a_row_alone(bits, alpha):
+    x = np.abs(np.random.default_rng(9).standard_normal((37, 45))).astype(np.float32) + 1
+    with np.errstate(invalid="ignore"):
+        want = x * np.float32(alpha)
+    for dtype in ("f32", "bf16"):
+        w = want if dtype == "f32" else torch.from_numpy(x).bfloat16().float().numpy() * np.float32(alpha)
+        q, qt = filled(bits, 37, 45), filled(bits, 45, 37)
+        C.costa_mx_quantize(alpha, gpu(x, dtype), q, qt)
+        check_stored(q, w)
+        check_stored(qt, w.T)
+        q = filled(bits, 37, 45)
+        C.costa_mx_quantize(alpha, gpu(x, dtype), q)
+        check_stored(q, w)
+
+
+@pytest.mark.parametrize("bits", [4, 8])
 def test_extremes_and_what_is_no_number(bits):
     big = np.finfo(np.float32).max
     x = np.random.default_rng(3).standard_normal((16, 96)).astype(np.float32)

@@ -121,6 +121,18 @@ def test_products_of_doubles_overlaps_and_workspaces_are_refused():
     assert C._lib.costa_mx_workspace(1, 1, 1, None) == C.INVALID_VALUE
 
 
+@pytest.mark.parametrize("m", [0, 1, 64, 65, 5000, 2**31 - 1])
+@pytest.mark.parametrize("n", [0, 1, 300, 2**31 - 1])
+@pytest.mark.parametrize("k", [0, 1, 4096, 2**31 - 1])
+def test_workspaces_of_all_sizes(m, n, k):
+    """Parts of whole matrices, bounded; none for a sum over nothing."""
+    b = C.costa_mx_workspace(m, n, k)
+    assert b <= 256 << 20
+    assert b % (4 * m * n) == 0 if m and n else b == 0
+    if k <= 1:
+        assert b == 0
+
+
 def test_layouts_that_are_refused():
     L = C.Layout.block_cyclic(8, 6, 2, 2, 2, 1)
     f = lambda type, lay, bufs, q, qt=None: C._lib.costa_mx_quantize_layout(  # noqa: E731
