@@ -162,9 +162,17 @@ def _addr(x) -> int:
 _cuda = False  # whether torch has said that a device is there
 
 
+# torch's own way to the handle of a device's current stream, where this torch has it
+# (0.1 us; through the stream objects of its public interface 2.8 us)
+_raw_stream = getattr(getattr(torch, "_C", None), "_cuda_getCurrentRawStream", None)
+_raw_device = getattr(getattr(torch, "_C", None), "_cuda_getDevice", None)
+
+
 def _stream(stream) -> int:
     global _cuda
     if stream is None:
+        if _raw_stream is not None and _raw_device is not None and torch.cuda.is_initialized():
+            return int(_raw_stream(_raw_device()))
         _cuda = _cuda or torch.cuda.is_available()
         return int(torch.cuda.current_stream().cuda_stream) if _cuda else 0
     if isinstance(stream, int):

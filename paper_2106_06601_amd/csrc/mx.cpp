@@ -113,6 +113,7 @@ constexpr size_t kMxTablesMax = 64;
 struct LayoutTables {
   void* dev = nullptr;
   MxLayoutArgs args{};
+  std::vector<int32_t> rank;  // (HostTables::rank)
   bool captured = false;  // a graph reads them: kept until costa_finalize
   ~LayoutTables() {
     if (dev) (void)hipFree(dev);
@@ -129,49 +130,38 @@ TableState& table_state() {
 }
 
 // The host side of a layout's tables, by its lines (columns of a column-major
-// layout, rows of a row-major one).
+// layout, rows of a row-major one): [0] lines, [1] places.
 struct HostTables {
-  std::vector<int64_t> start[2], local[2];  // lines, places
-  std::vector<int32_t> cls[2];
+  std::vector<int64_t> start[2];
+  MxSplits splits[2] = {};
   std::vector<MxCell> cells;
+  std::vector<int32_t> rank;  // of each cell of a block-cyclic layout
   int32_t nplace = 0;
 };
 
 void fill_tables(const Layout& L, HostTables& h) {
   const bool col = L.order == COSTA_COL_MAJOR;
   const int row = col ? 1 : 0;  // which of the two the rows are
-  h.start[row] = L.rsplit;
-  h.start[1 - row] = L.csplit;
-  h.local[row].resize(L.nbr);
-  h.cls[row].resize(L.nbr);
-  h.local[1 - row].resize(L.nbc);
-  h.cls[1 - row].resize(L.nbc);
   if (L.block_cyclic) {
     // the local matrix of a process: classes are process rows and columns
-    for (int32_t b = 0; b < L.nbr; ++b) {
-      h.cls[row][b] = L.prow_of(b);
-      h.local[row][b] = (L.rb0 + b) / L.prow * L.mb + (L.r0 + L.rsplit[b]) % L.mb;
-    }
-    for (int32_t b = 0; b < L.nbc; ++b) {
-      h.cls[1 - row][b] = L.pcol_of(b);
-      h.local[1 - row][b] = (L.cb0 + b) / L.pcol * L.nb + (L.c0 + L.csplit[b]) % L.nb;
-    }
+    auto narrow = [](int64_t off, int64_t n) { return off <= (int64_t)UINT32_MAX - 1 - n ? 1 : 0; };
+    h.splits[row] = MxSplits{nullptr, 0, L.prow, L.rsrc, L.r0, L.mb, narrow(L.r0, L.nrows)};
+    h.splits[1 - row] = MxSplits{nullptr, 0, L.pcol, L.csrc, L.c0, L.nb, narrow(L.c0, L.ncols)};
     const int32_t nline = col ? L.pcol : L.prow;
     h.nplace = col ? L.prow : L.pcol;
     h.cells.resize((size_t)nline * h.nplace);
+    h.rank.resize(h.cells.size());
     for (int32_t pr = 0; pr < L.prow; ++pr)
       for (int32_t pc = 0; pc < L.pcol; ++pc) {
         const int64_t ext = col ? L.lrows[pr] : L.lcols[pc];
-        h.cells[(size_t)(col ? pc : pr) * h.nplace + (col ? pr : pc)] =
-            MxCell{0, L.lld ? L.lld : std::max<int64_t>(ext, 1), L.rank_at(pr, pc)};
+        const size_t at = (size_t)(col ? pc : pr) * h.nplace + (col ? pr : pc);
+        h.cells[at] = MxCell{0, L.lld ? L.lld : std::max<int64_t>(ext, 1), (int64_t)at};
+        h.rank[at] = L.rank_at(pr, pc);
       }
     return;
   }
-  for (int s = 0; s < 2; ++s)
-    for (size_t b = 0; b < h.cls[s].size(); ++b) {
-      h.cls[s][b] = (int32_t)b;
-      h.local[s][b] = 0;
-    }
+  h.start[row] = L.rsplit;
+  h.start[1 - row] = L.csplit;
   const int32_t nline = col ? L.nbc : L.nbr;
   h.nplace = col ? L.nbr : L.nbc;
   h.cells.resize((size_t)nline * h.nplace);
@@ -180,10 +170,12 @@ void fill_tables(const Layout& L, HostTables& h) {
       const int64_t b = L.block(bi, bj);
       h.cells[(size_t)(col ? bj : bi) * h.nplace + (col ? bi : bj)] = MxCell{L.boff[b], L.bld[b], L.owner[b]};
     }
+  for (int s = 0; s < 2; ++s) h.splits[s] = MxSplits{nullptr, (int32_t)h.start[s].size() - 1, 0, 0, 0, 0, 0};
 }
 
 // The device tables of a layout; uploaded on the first call.
-costa_status layout_tables(const Layout& L, hipStream_t stream, MxLayoutArgs& out) {
+// `p` holds the ranks' buffers and gets them in the order that the kernel looks them up.
+costa_status layout_tables(const Layout& L, hipStream_t stream, MxLayoutArgs& out, MxPointers& p) {
   int device = 0;
   HIP_OR_FAIL(hipGetDevice(&device));
   hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
@@ -211,12 +203,8 @@ costa_status layout_tables(const Layout& L, hipStream_t stream, MxLayoutArgs& ou
       if (n) std::copy_n(static_cast<const unsigned char*>(p), n, all.data() + at);
       return at;
     };
-    size_t at_start[2], at_local[2], at_cls[2];
-    for (int s = 0; s < 2; ++s) {
-      at_start[s] = put(h.start[s].data(), h.start[s].size() * sizeof(int64_t));
-      at_local[s] = put(h.local[s].data(), h.local[s].size() * sizeof(int64_t));
-      at_cls[s] = put(h.cls[s].data(), h.cls[s].size() * sizeof(int32_t));
-    }
+    size_t at_start[2];
+    for (int s = 0; s < 2; ++s) at_start[s] = put(h.start[s].data(), h.start[s].size() * sizeof(int64_t));
     const size_t at_cells = put(h.cells.data(), h.cells.size() * sizeof(MxCell));
     std::unique_ptr<LayoutTables> t(new LayoutTables());
     if (hipMalloc(&t->dev, all.size()) != hipSuccess) {
@@ -226,15 +214,19 @@ costa_status layout_tables(const Layout& L, hipStream_t stream, MxLayoutArgs& ou
     }
     HIP_OR_FAIL(hipMemcpy(t->dev, all.data(), all.size(), hipMemcpyHostToDevice));
     const unsigned char* d = static_cast<const unsigned char*>(t->dev);
-    auto splits = [&](int s) {
-      return MxSplits{reinterpret_cast<const int64_t*>(d + at_start[s]), reinterpret_cast<const int64_t*>(d + at_local[s]),
-                      reinterpret_cast<const int32_t*>(d + at_cls[s]), (int32_t)h.cls[s].size()};
-    };
-    t->args = MxLayoutArgs{splits(0), splits(1), reinterpret_cast<const MxCell*>(d + at_cells), h.nplace};
+    for (int s = 0; s < 2; ++s)
+      if (!h.start[s].empty()) h.splits[s].start = reinterpret_cast<const int64_t*>(d + at_start[s]);
+    t->args = MxLayoutArgs{h.splits[0], h.splits[1], reinterpret_cast<const MxCell*>(d + at_cells), h.nplace,
+                           L.block_cyclic ? 1 : 0};
+    t->rank = std::move(h.rank);
     it = T.tables.emplace(key, std::move(t)).first;
   }
   if (capturing) it->second->captured = true;
   out = it->second->args;
+  if (out.dealt) {  // (at most as many cells as ranks)
+    const MxPointers by_rank = p;
+    for (size_t c = 0; c < it->second->rank.size(); ++c) p.p[c] = by_rank.p[it->second->rank[c]];
+  }
   return COSTA_SUCCESS;
 }
 
@@ -366,7 +358,7 @@ extern "C" costa_status costa_mx_quantize_layout(costa_real type, float alpha, c
       return COSTA_SUCCESS;
     }
     MxLayoutArgs l{};
-    CHECKED(layout_tables(*L, stream, l));
+    CHECKED(layout_tables(*L, stream, l, p));
     HIP_OR_FAIL(launch_mx_quantize_layout(a, l, p, stream));
     return COSTA_SUCCESS;
   });

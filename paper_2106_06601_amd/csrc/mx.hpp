@@ -42,24 +42,29 @@ struct QuantArgs {
 hipError_t launch_mx_quantize(const QuantArgs& a, hipStream_t stream);
 
 // A layout's lines and elements.  Line i lies in block line `lb`, the last with
-// line_start[lb] <= i; then (class, local line) = (line_class[lb], line_local[lb]
-// + i - line_start[lb]); the same for an element's place in its line.  The cell
-// (line class, element class) gives the rank, the offset and the leading
-// dimension: the element is at offset + local line * ld + local place.
+// start[lb] <= i; then (class, local line) = (lb, i - start[lb]).  Block-cyclic
+// layouts (blk > 0) have no such arrays: of the dealt dimension, index off + i is in
+// block (off + i) / blk, whose process (shifted by src) is the class, and is the
+// process's (off + i) / (blk * np) * blk + (off + i) % blk -th.  The same for an
+// element's place in its line.  The cell (line class, place class) gives the place of
+// the pointer in the call's array, the offset and the leading dimension: the element
+// is at offset + local line * ld + local place.
 struct MxCell {
   int64_t offset, ld;
-  int64_t rank;
+  int64_t pointer;
 };
 struct MxSplits {
   const int64_t* start;  // n + 1 entries
-  const int64_t* local;  // n
-  const int32_t* cls;    // n
   int32_t n;
+  int32_t np, src;  // block-cyclic: processes, and the one that has block 0
+  int64_t off, blk;
+  int32_t narrow;  // off + i is below 2^32 - 1
 };
 struct MxLayoutArgs {
   MxSplits line, place;
   const MxCell* cells;  // line class * nplace + place class
   int32_t nplace;
+  int32_t dealt;  // block-cyclic: a cell's pointer is at the cell's own index
 };
 constexpr int kMxRanksMax = 256;
 struct MxPointers {

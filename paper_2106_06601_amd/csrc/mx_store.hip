@@ -127,16 +127,29 @@ __device__ inline void put_tile(const typename Tile<T>::S* tile, const MxView& q
   }
 }
 
-// Where an index lies in a dimension's splits: (class, local index).
+// Where an index lies in a dimension: (class, local index).
 __device__ inline void locate(const MxSplits& s, int64_t i, int32_t& cls, int64_t& local) {
+  if (s.blk > 0 && s.narrow) {  // (64-bit divisions take several times as long)
+    const uint32_t at = (uint32_t)(s.off + i), blk = (uint32_t)min(s.blk, (int64_t)0xffffffff), np = (uint32_t)s.np;
+    const uint32_t block = at / blk, round = block / np;
+    cls = (int32_t)((block - round * np + (uint32_t)s.src) % np);
+    local = (int64_t)round * blk + (at - block * blk);
+    return;
+  }
+  if (s.blk > 0) {
+    const int64_t at = s.off + i, block = at / s.blk, round = block / s.np;
+    cls = (int32_t)((block - round * s.np + s.src) % s.np);
+    local = round * s.blk + (at - block * s.blk);
+    return;
+  }
   int32_t lo = 0, hi = s.n;  // start[lo] <= i < start[hi]
   while (hi - lo > 1) {
     const int32_t mid = lo + (hi - lo) / 2;
     if (s.start[mid] <= i) lo = mid;
     else hi = mid;
   }
-  cls = s.cls[lo];
-  local = s.local[lo] + (i - s.start[lo]);
+  cls = lo;
+  local = i - s.start[lo];
 }
 
 struct TileArgs {
@@ -181,29 +194,29 @@ __global__ __launch_bounds__(kThreads) void quantize_tiles(TileArgs a, Where whe
       run = run && place_cls[place] == place_cls[place + V - 1] &&
             place_local[place + V - 1] == place_local[place] + V - 1;
     }
-    int32_t last_cls = -1;  // the cell changes where a line's block does
     const T* base = static_cast<const T*>(a.src) + c;
-    int64_t ld = a.ld;
+    const int last = (int)min((int64_t)kLines, a.lines - line0) - 1;  // (may be below 0: padding only)
 #pragma unroll 1
     for (int first = tid / LANES; first < kLines; first += LINES * BATCH) {
       alignas(16) T v[BATCH][V];
-      if (run) {
+      if (run && last >= 0) {
+        // all addresses, then all loads: none waits for another (lines past the last
+        // repeat it and are dropped below)
+        const T* from[BATCH];
 #pragma unroll
         for (int q = 0; q < BATCH; ++q) {
-          const int line = first + LINES * q;
-          if (line0 + line >= a.lines) break;
-          int64_t at = line0 + line;
+          const int line = min(first + LINES * q, last);
           if constexpr (LAYOUT) {
-            if (line_cls[line] != last_cls) {
-              last_cls = line_cls[line];
-              const MxCell& cell = where.l.cells[(int64_t)last_cls * where.l.nplace + place_cls[place]];
-              base = static_cast<const T*>(where.ptrs.p[cell.rank]) + cell.offset + place_local[place];
-              ld = cell.ld;
-            }
-            at = line_local[line];
+            const int64_t at_cell = (int64_t)line_cls[line] * where.l.nplace + place_cls[place];
+            const MxCell& cell = where.l.cells[at_cell];
+            from[q] = static_cast<const T*>(where.ptrs.p[where.l.dealt ? at_cell : cell.pointer]) + cell.offset +
+                      place_local[place] + line_local[line] * cell.ld;
+          } else {
+            from[q] = base + (line0 + line) * a.ld;
           }
-          __builtin_memcpy(v[q], base + at * ld, sizeof v[q]);
         }
+#pragma unroll
+        for (int q = 0; q < BATCH; ++q) __builtin_memcpy(v[q], from[q], sizeof v[q]);
       } else {
 #pragma unroll
         for (int q = 0; q < BATCH; ++q) {
@@ -216,9 +229,9 @@ __global__ __launch_bounds__(kThreads) void quantize_tiles(TileArgs a, Where whe
                 const MxCell& cell =
                     where.l.cells[(int64_t)line_cls[line] * where.l.nplace + place_cls[place + e]];
                 v[q][e] = static_cast<const T*>(
-                    where.ptrs.p[cell.rank])[cell.offset + line_local[line] * cell.ld + place_local[place + e]];
+                    where.ptrs.p[cell.pointer])[cell.offset + line_local[line] * cell.ld + place_local[place + e]];
               } else {
-                v[q][e] = base[(line0 + line) * ld + e];
+                v[q][e] = base[(line0 + line) * a.ld + e];
               }
             }
         }

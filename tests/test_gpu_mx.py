@@ -222,6 +222,22 @@ def test_quantize_out_of_layouts(spec, dtype):
         check_stored(qt, x.T * np.float32(0.5))
 
 
+def test_quantize_window_far_into_a_matrix():
+    """Rows past 2^32 of a block-cyclic matrix; the ranks' buffers are addressed as
+    if the whole of their local matrices were there, and only the window's part is read."""
+    nb, np_, r0, m, n = 1 << 31, 2, (1 << 32) + 77, 100, 70
+    whole = C.Layout.block_cyclic(1 << 33, n, nb, 32, np_, 1, "row", "row")
+    L = whole.submatrix(r0, 0, m, n)
+    x = np.random.default_rng(8).standard_normal((m, n)).astype(np.float32)
+    t = gpu(x)
+    # row r0 + i is in block 2, process 0's second: its local row nb + 77 + i
+    at = t.data_ptr() - (nb + 77) * n * 4
+    q, qt = filled(8, m, n), filled(4, n, m)
+    C.costa_mx_quantize_layout("f32", 1.0, L, [at, 16], q, qt)
+    check_stored(q, x)
+    check_stored(qt, x.T)
+
+
 def _splits(L, spec, rng):
     """The splits of a test's layout, from its recipe."""
     kind, m, n = spec[:3]
