@@ -217,23 +217,25 @@ __global__ __launch_bounds__(kThreads) void quantize_tiles(TileArgs a, Where whe
         }
 #pragma unroll
         for (int q = 0; q < BATCH; ++q) __builtin_memcpy(v[q], from[q], sizeof v[q]);
-      } else {
+      } else if (last >= 0) {  // across an edge of a block or of the matrix: place by place
 #pragma unroll
-        for (int q = 0; q < BATCH; ++q) {
-          const int line = first + LINES * q;
-          if (line0 + line >= a.lines) break;
+        for (int e = 0; e < V; ++e) {
+          if (c + e >= a.len) continue;
+          const T* from[BATCH];
 #pragma unroll
-          for (int e = 0; e < V; ++e)
-            if (c + e < a.len) {
-              if constexpr (LAYOUT) {
-                const MxCell& cell =
-                    where.l.cells[(int64_t)line_cls[line] * where.l.nplace + place_cls[place + e]];
-                v[q][e] = static_cast<const T*>(
-                    where.ptrs.p[cell.pointer])[cell.offset + line_local[line] * cell.ld + place_local[place + e]];
-              } else {
-                v[q][e] = base[(line0 + line) * a.ld + e];
-              }
+          for (int q = 0; q < BATCH; ++q) {
+            const int line = min(first + LINES * q, last);
+            if constexpr (LAYOUT) {
+              const int64_t at_cell = (int64_t)line_cls[line] * where.l.nplace + place_cls[place + e];
+              const MxCell& cell = where.l.cells[at_cell];
+              from[q] = static_cast<const T*>(where.ptrs.p[where.l.dealt ? at_cell : cell.pointer]) + cell.offset +
+                        place_local[place + e] + line_local[line] * cell.ld;
+            } else {
+              from[q] = base + (line0 + line) * a.ld + e;
             }
+          }
+#pragma unroll
+          for (int q = 0; q < BATCH; ++q) v[q][e] = *from[q];
         }
       }
 #pragma unroll
