@@ -10,6 +10,7 @@ Importing this module fails loudly when the library has not been built.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from array import array as _array
 from typing import List, Optional, Sequence
@@ -602,6 +603,7 @@ def costa_mx_dequantize(alpha: float, Q: MxMatrix, beta: float, A, stream=None) 
     _check(_lib.costa_mx_dequantize(alpha, _mx(Q), beta, _matrix(A), _stream(stream)), "costa_mx_dequantize")
 
 
+@functools.lru_cache(maxsize=4096)  # (a function of the sizes)
 def costa_mx_workspace(m: int, n: int, k: int) -> int:
     b = ctypes.c_size_t()
     _check(_lib.costa_mx_workspace(m, n, k, ctypes.byref(b)), "costa_mx_workspace")

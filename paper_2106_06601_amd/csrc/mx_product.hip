@@ -153,10 +153,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_rows(Args p, int splits, i
         if (i + 1 < MT) left.load(p, 16 * (i + 1), u * UNIT + h * kSlab, a_end);
         else if (h + 1 < SLABS) left.load(p, 0, u * UNIT + (h + 1) * kSlab, a_end);
         else if (to_go > 1) left.load(p, 0, next * UNIT, a_end);
-        // (a wave's accesses to shared memory take effect in their order)
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        wave_fence();
 #pragma unroll
         for (int l = 0; l < LOADS; ++l)
 #pragma unroll
@@ -169,9 +166,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_rows(Args p, int splits, i
               for (int j = 0; j < NT; ++j) acc[i][j] = mfma_bf16(e[j][l][q], a, acc[i][j]);
             }
           }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        wave_fence();
       }
     }
     u = next;
@@ -193,14 +188,16 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_rows(Args p, int splits, i
   if (wave != 0) return;
   Epilogue e = p.e;
   if (p.part) e.c = static_cast<float*>(e.c) + (int64_t)(blockIdx.x % splits) * p.part;
-  // lane l has row l % 16 of C and columns 4 (l / 16) .. + 3 of each 16 x 16 piece
+  // lane l has row l % 16 of C and columns 4 (l / 16) .. + 3 of each 16 x 16 piece; the
+  // pieces go through shared memory so that the code that stores them stands there once
 #pragma unroll
-  for (int i = 0; i < MT; ++i)
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      const int64_t row = 16 * i + r, col = j0 + 16 * j + 4 * g;
-      if (row < p.m) put_four(e, row, col, acc[i][j], (int)min((int64_t)4, p.n - col));
-    }
+  for (int t = 0; t < MT * NT; ++t) red[0][t][lane] = acc[t / NT][t % NT];
+  wave_fence();
+#pragma unroll 1
+  for (int t = 0; t < MT * NT; ++t) {
+    const int64_t row = 16 * (t / NT) + r, col = j0 + 16 * (t % NT) + 4 * g;
+    if (row < p.m) put_four(e, row, col, red[0][t][lane], (int)min((int64_t)4, p.n - col));
+  }
 }
 
 template <int SRC, int BBITS, int MT>
@@ -247,7 +244,7 @@ __global__ __launch_bounds__(256) void join_parts(Epilogue e, const float* parts
   const int mine = threadIdx.x / UNITS, at = threadIdx.x % UNITS;
   for (int64_t u0 = (int64_t)blockIdx.x * UNITS; u0 < units; u0 += (int64_t)gridDim.x * UNITS) {
     const int64_t u = u0 + at;
-    const int64_t i = u / upr, j = (u - i * upr) * 4;
+    const int64_t i = ((u | upr) >> 32) == 0 ? (int64_t)((uint32_t)u / (uint32_t)upr) : u / upr, j = (u - i * upr) * 4;
     const int c = u < units ? (int)min((int64_t)4, n - j) : 0;
     v4f acc = {0, 0, 0, 0};
     const float* p = parts + i * n + j;

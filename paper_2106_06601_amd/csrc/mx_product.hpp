@@ -60,6 +60,14 @@ __device__ inline void put_four(const Epilogue& e, int64_t i, int64_t j, v4f acc
   else put_typed<_Float16>(e, i, j, acc, n);
 }
 
+// A wave's accesses to shared memory take effect in their order: this keeps the
+// compiler to it, between lanes that write and others that read.
+__device__ inline void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // Arguments of the product kernels.
 struct Args {
   int64_t m, n, k;

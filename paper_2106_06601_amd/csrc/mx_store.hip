@@ -17,6 +17,13 @@ __device__ inline float to_float(T v) {
   return (float)v;
 }
 
+// a / b of a non-negative a; in 32 bits where they do (64-bit divisions take several
+// times as long).
+__device__ inline int64_t quotient(int64_t a, int64_t b) {
+  if (((a | b) >> 32) == 0) return (int64_t)((uint32_t)a / (uint32_t)b);
+  return a / b;
+}
+
 // The largest of four neighbouring lanes.
 __device__ inline uint32_t quad_max(uint32_t v) {
   v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true));  // lanes 1 0 3 2
@@ -34,7 +41,7 @@ __global__ __launch_bounds__(kThreads) void quantize_lines(const T* src, int64_t
   const uint32_t upl = (uint32_t)(q.row_scales * 4);  // units of 8 elements of a padded line
   const int64_t units = lines * upl;
   for (int64_t u0 = (int64_t)blockIdx.x * kThreads; u0 < units; u0 += (int64_t)gridDim.x * kThreads) {
-    const int64_t line0 = u0 / upl;
+    const int64_t line0 = quotient(u0, upl);
     const uint32_t in = (uint32_t)(u0 - line0 * upl) + threadIdx.x;
     const int64_t line = line0 + in / upl;
     const uint32_t unit = in % upl;
@@ -179,7 +186,7 @@ __global__ __launch_bounds__(kThreads) void quantize_tiles(TileArgs a, Where whe
   const int tid = threadIdx.x;
   const int place = tid % LANES * V;
   for (int64_t t = blockIdx.x; t < a.tiles; t += gridDim.x) {
-    const int64_t line0 = t / a.tiles_x * kLines, place0 = t % a.tiles_x * Ti::PLACES;
+    const int64_t ty = quotient(t, a.tiles_x), line0 = ty * kLines, place0 = (t - ty * a.tiles_x) * Ti::PLACES;
     const int64_t c = place0 + place;
     bool run = c + V <= a.len;
     if constexpr (LAYOUT) {
@@ -267,7 +274,7 @@ __global__ __launch_bounds__(kThreads) void dequantize(DequantArgs a) {
   for (int64_t u0 = (int64_t)blockIdx.x * kThreads; u0 < units; u0 += (int64_t)gridDim.x * kThreads) {
     // ROWS: u = row * upr + unit; else u = unit * rows + row
     const int64_t per = ROWS ? upr : a.q.rows;
-    const int64_t o0 = u0 / per;
+    const int64_t o0 = quotient(u0, per);
     const uint32_t in = (uint32_t)(u0 - o0 * per) + threadIdx.x;  // (per is below 2^31)
     const uint32_t over = in / (uint32_t)per;
     const int64_t outer = o0 + over, inner = in - over * (uint32_t)per;

@@ -19,13 +19,49 @@ constexpr int kLanes = 64 * kWaves;
 // Tile (tm, tn) of workgroup b of a launch over nm x nn tiles.  Workgroups go
 // round the 8 XCDs in turn; each XCD gets a run of neighbouring tiles (8 tile
 // rows wide, by columns), whose operands its L2 holds.
-__device__ inline void tile_of(int64_t b, int64_t nm, int64_t nn, int64_t& tm, int64_t& tn) {
-  const int64_t total = nm * nn, per = total / 8, more = total % 8, x = b % 8;
-  const int64_t t = x * per + min(x, more) + b / 8;
-  const int64_t group = t / (8 * nn), rows = min((int64_t)8, nm - group * 8), in = t - group * 8 * nn;
+__device__ inline void tile_of(uint32_t b, uint32_t nm, uint32_t nn, int64_t& tm, int64_t& tn) {
+  const uint32_t total = nm * nn, per = total / 8, more = total % 8, x = b % 8;
+  const uint32_t t = x * per + min(x, more) + b / 8;
+  const uint32_t group = t / (8 * nn), rows = min(8u, nm - group * 8), in = t - group * 8 * nn;
   // (the division runs on vector registers: both are the wave's, not a lane's)
-  tm = __builtin_amdgcn_readfirstlane((int)(group * 8 + in % rows));
-  tn = __builtin_amdgcn_readfirstlane((int)(in / rows));
+  tm = __builtin_amdgcn_readfirstlane(group * 8 + in % rows);
+  tn = __builtin_amdgcn_readfirstlane(in / rows);
+}
+
+// Part y of `parts` of a sum's steps.
+__device__ inline void steps_of(uint32_t steps, uint32_t y, uint32_t parts, int64_t& first, int64_t& last) {
+  const uint32_t per = steps / parts, more = steps % parts;
+  first = __builtin_amdgcn_readfirstlane(y * per + min(y, more));
+  last = __builtin_amdgcn_readfirstlane((y + 1) * per + min(y + 1, more));
+}
+
+// A wave's part of C, rows i0 .. and columns j0 .., through a piece of shared memory
+// (the operands are done with): whole rows are written at a time, and the code that
+// rounds and stores stands there twice and not for each of the MT x NT pieces, where
+// fetching it cost small products more than running it.
+template <int MT, int NT>
+__device__ inline void put_wave(const Args& p, const v4f (&acc)[MT][NT], v4u* shared, int wave, int64_t i0,
+                                int64_t j0) {
+  constexpr int ROWS = 16, COLS = NT * 16, STRIDE = COLS / 4 + 1;  // 16-byte units: neighbouring rows, other banks
+  constexpr int LANES = COLS / 4, PER = 64 / LANES;               // lanes a row, rows at a time
+  v4f* const mine = reinterpret_cast<v4f*>(shared) + wave * ROWS * STRIDE;
+  const int lane = threadIdx.x % 64, r = lane % 16, g = lane / 16;
+  Epilogue e = p.e;
+  if (p.part) e.c = static_cast<float*>(e.c) + blockIdx.y * p.part;
+  const int64_t col = j0 + lane % LANES * 4;
+  const int n = (int)max((int64_t)0, min((int64_t)4, p.n - col));
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j) mine[r * STRIDE + 4 * j + g] = acc[i][j];
+    wave_fence();
+#pragma unroll 1
+    for (int q = 0; q < ROWS; q += PER) {
+      const int64_t row = i0 + 16 * i + q + lane / LANES;
+      if (row < p.m) put_four(e, row, col, mine[(q + lane / LANES) * STRIDE + lane % LANES], n);
+    }
+    wave_fence();
+  }
 }
 
 // ---- plain (or decoded) left operand: bfloat16 instructions --------------------------
@@ -183,7 +219,7 @@ struct RightStage {
 
 // AHEAD: steps whose loads are on their way at once.
 template <int SRC, bool TRANS, int BBITS, int BM, int BN, int WM, int AHEAD>
-__global__ __launch_bounds__(kLanes) void tiles_bf16(Args p, int64_t nm, int64_t nn) {
+__global__ __launch_bounds__(kLanes) void tiles_bf16(Args p, uint32_t nm, uint32_t nn) {
   constexpr int WN = kWaves / WM, MT = BM / WM / 16, NT = BN / WN / 16, P = parts_of(SRC);
   constexpr int BROW = kStepBf16 * BBITS / 8;
   __shared__ v4u left[2][P * BM * 8];
@@ -194,8 +230,8 @@ __global__ __launch_bounds__(kLanes) void tiles_bf16(Args p, int64_t nm, int64_t
   int64_t tm, tn;
   tile_of(blockIdx.x, nm, nn, tm, tn);
   const int64_t i0 = tm * BM, j0 = tn * BN;
-  const int64_t steps = (p.k + kStepBf16 - 1) / kStepBf16;
-  const int64_t first = steps * blockIdx.y / gridDim.y, last = steps * (blockIdx.y + 1) / gridDim.y;
+  int64_t first, last;
+  steps_of((uint32_t)((p.k + kStepBf16 - 1) / kStepBf16), blockIdx.y, gridDim.y, first, last);
 
   v4f acc[MT][NT];
 #pragma unroll
@@ -259,18 +295,7 @@ __global__ __launch_bounds__(kLanes) void tiles_bf16(Args p, int64_t nm, int64_t
       __syncthreads();
     }
   }
-  Epilogue e = p.e;
-  if (p.part) e.c = static_cast<float*>(e.c) + blockIdx.y * p.part;
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int64_t row = i0 + wm + 16 * i + r;
-    if (row < p.m)
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        const int64_t col = j0 + wn + 16 * j + 4 * g;
-        put_four(e, row, col, acc[i][j], (int)max((int64_t)0, min((int64_t)4, p.n - col)));
-      }
-  }
+  put_wave<MT, NT>(p, acc, &left[0][0], wave, i0 + wm, j0 + wn);
 }
 
 // ---- both operands in 4 bits: the scaled instructions -----------------------------------
@@ -320,7 +345,7 @@ __device__ inline v8i operand4(v4u d) {  // the instruction reads four of the ei
 }
 
 template <int BM, int BN, int WM>
-__global__ __launch_bounds__(kLanes) void tiles_scaled(Args p, int64_t nm, int64_t nn) {
+__global__ __launch_bounds__(kLanes) void tiles_scaled(Args p, uint32_t nm, uint32_t nn) {
   constexpr int WN = kWaves / WM, MT = BM / WM / 16, NT = BN / WN / 16;
   __shared__ v4u left[2][BM * kRowChunks];
   __shared__ v4u right[2][BN * kRowChunks];
@@ -330,8 +355,8 @@ __global__ __launch_bounds__(kLanes) void tiles_scaled(Args p, int64_t nm, int64
   int64_t tm, tn;
   tile_of(blockIdx.x, nm, nn, tm, tn);
   const int64_t i0 = tm * BM, j0 = tn * BN;
-  const int64_t steps = (p.k + kStep4 - 1) / kStep4;
-  const int64_t first = steps * blockIdx.y / gridDim.y, last = steps * (blockIdx.y + 1) / gridDim.y;
+  int64_t first, last;
+  steps_of((uint32_t)((p.k + kStep4 - 1) / kStep4), blockIdx.y, gridDim.y, first, last);
 
   v4f acc[MT][NT];
 #pragma unroll
@@ -383,28 +408,28 @@ __global__ __launch_bounds__(kLanes) void tiles_scaled(Args p, int64_t nm, int64
         for (int j = 0; j < NT; ++j)
           acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j], a, acc[i][j], 4, 4, 0, sb[j], 0, sa);
       }
+      // the first three rows' operands are read ahead, then one for every half row of
+      // instructions (8192^3: 341 us in the compiler's own order, 333 so)
+      __builtin_amdgcn_sched_group_barrier(0x100, 2 * NT + 6, 0);  // reads of shared memory
+#pragma unroll
+      for (int i = 0; i < 2 * MT; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, NT / 2, 0);  // matrix instructions
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
     }
     if (t + 1 < last) arrive(1 - s);
   }
-  Epilogue e = p.e;
-  if (p.part) e.c = static_cast<float*>(e.c) + blockIdx.y * p.part;
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int64_t row = i0 + wm + 16 * i + r;
-    if (row < p.m)
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        const int64_t col = j0 + wn + 16 * j + 4 * g;
-        put_four(e, row, col, acc[i][j], (int)max((int64_t)0, min((int64_t)4, p.n - col)));
-      }
-  }
+  __syncthreads();
+  put_wave<MT, NT>(p, acc, &left[0][0], wave, i0 + wm, j0 + wn);
 }
 
 template <int SRC, bool TRANS, int BBITS>
 hipError_t launch_bf16(const Args& p, const ProductPlan& plan, hipStream_t stream) {
   constexpr int BM = parts_of(SRC) == 1 ? 256 : 128;
-  const int64_t nm = (p.m + plan.bm - 1) / plan.bm, nn = (p.n + plan.bn - 1) / plan.bn;
-  const dim3 grid((unsigned)(nm * nn), plan.splits);
+  // (C would not fit the device's memory with 2^32 tiles)
+  const uint32_t nm = (uint32_t)((p.m + plan.bm - 1) / plan.bm), nn = (uint32_t)((p.n + plan.bn - 1) / plan.bn);
+  if ((int64_t)nm * nn > 1 << 22) return hipErrorInvalidValue;
+  const dim3 grid(nm * nn, plan.splits);
   if (plan.bm == BM && plan.bn == 256)
     tiles_bf16<SRC, TRANS, BBITS, BM, 256, 2, 1><<<grid, kLanes, 0, stream>>>(p, nm, nn);
   else if (plan.bm == 128 && plan.bn == 128)
@@ -437,8 +462,10 @@ hipError_t launch_tiles_bf16(int src, const Args& p, const ProductPlan& plan, hi
 }
 
 hipError_t launch_tiles_scaled(const Args& p, const ProductPlan& plan, hipStream_t stream) {
-  const int64_t nm = (p.m + plan.bm - 1) / plan.bm, nn = (p.n + plan.bn - 1) / plan.bn;
-  const dim3 grid((unsigned)(nm * nn), plan.splits);
+  // (C would not fit the device's memory with 2^32 tiles)
+  const uint32_t nm = (uint32_t)((p.m + plan.bm - 1) / plan.bm), nn = (uint32_t)((p.n + plan.bn - 1) / plan.bn);
+  if ((int64_t)nm * nn > 1 << 22) return hipErrorInvalidValue;
+  const dim3 grid(nm * nn, plan.splits);
   if (plan.bm == 256 && plan.bn == 256) tiles_scaled<256, 256, 2><<<grid, kLanes, 0, stream>>>(p, nm, nn);
   else if (plan.bm != 128 || plan.bn != 128) return hipErrorInvalidValue;  // not a tile of this kernel
   else tiles_scaled<128, 128, 2><<<grid, kLanes, 0, stream>>>(p, nm, nn);
