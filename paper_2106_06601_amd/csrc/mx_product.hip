@@ -53,14 +53,17 @@ struct FewSlab {
           scale[q] = p.a.scales[row * p.a.row_scales + k / kMxBlock];
         }
       } else {
-        const char* at = static_cast<const char*>(p.real) + (row * p.a_rs + k) * bytes_of(SRC);
-        if (k0 + kSlab <= end) __builtin_memcpy(raw[q].w, at, sizeof raw[q].w);
-        else raw[q] = load8<SRC>(at, end - k);
+        const char* line = static_cast<const char*>(p.real) + row * p.a_rs * bytes_of(SRC);
+        load8<SRC>(raw[q], line, k, end);
       }
     }
   }
-  __device__ inline void store(const Args& p, int64_t row0, v4u* slab) const {
+  __device__ inline void store(const Args& p, int64_t row0, int64_t k0, int64_t end, v4u* slab) {
     const int lane = threadIdx.x % 64;
+    if constexpr (!MX)
+      if (k0 + kSlab > end)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) place8<SRC>(raw[q], k0 + 8 * (lane % 16), end);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       if (q > 0 && row0 + 4 * q >= p.m) continue;
@@ -126,14 +129,16 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_rows(Args p, int splits, i
   }
   for (uint32_t to_go = turns; to_go > 0; --to_go) {
     turn = turn + 1 < turns ? turn + 1 : 0;
-    const int64_t next = first + turn * step;
+    // (the last turn loads its own piece again, from the cache: without a branch, the
+    // compiler can count the loads on their way and waits for no more than it needs)
+    const int64_t next = to_go > 1 ? first + turn * step : u;
     v4u w[NT][2];
     uint32_t t[NT][2];
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int h = 0; h < 2; ++h) w[j][h] = b[j][h], t[j][h] = s[j][h];
-    if (to_go > 1) load(next);
+    load(next);
 #pragma unroll
     for (int h = 0; h < SLABS; ++h) {
       v4u e[NT][LOADS][STEPS];  // the slab's part of B, decoded
@@ -149,10 +154,10 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_rows(Args p, int splits, i
           }
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
-        left.store(p, 16 * i, slab);
+        left.store(p, 16 * i, u * UNIT + h * kSlab, a_end, slab);
         if (i + 1 < MT) left.load(p, 16 * (i + 1), u * UNIT + h * kSlab, a_end);
         else if (h + 1 < SLABS) left.load(p, 0, u * UNIT + (h + 1) * kSlab, a_end);
-        else if (to_go > 1) left.load(p, 0, next * UNIT, a_end);
+        else left.load(p, 0, next * UNIT, a_end);
         wave_fence();
 #pragma unroll
         for (int l = 0; l < LOADS; ++l)
@@ -233,6 +238,42 @@ hipError_t launch_few(int src, const Args& p, const ProductPlan& plan, hipStream
   }
 }
 
+// ---- what has too little for vector loads --------------------------------------------
+// Sums of fewer than 8 elements of a plain operand.  A lane makes one element of C.
+template <int SRC, int BBITS>
+__global__ __launch_bounds__(256) void thin(Args p) {
+  for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < p.m * p.n; u += (int64_t)gridDim.x * 256) {
+    const int64_t i = u / p.n, j = u - i * p.n;
+    v2u d = {0u, 0u};
+    if (BBITS == 4) d.x = *reinterpret_cast<const uint32_t*>(p.b.data + j * p.b.row_bytes);
+    else d = *reinterpret_cast<const v2u*>(p.b.data + j * p.b.row_bytes);
+    float b[8], sum = 0.0f;
+    mx_decode8<BBITS>(d, p.b.scales[j * p.b.row_scales], b);
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      if (q < p.k) {
+        const int64_t at = i * p.a_rs + q * p.a_cs;
+        const float a = SRC == SRC_BF16  ? (float)static_cast<const __bf16*>(p.real)[at]
+                        : SRC == SRC_F16 ? (float)static_cast<const _Float16*>(p.real)[at]
+                                         : static_cast<const float*>(p.real)[at];
+        sum += a * b[q];
+      }
+    put_four(p.e, i, j, v4f{sum, 0, 0, 0}, 1);
+  }
+}
+template <int SRC>
+hipError_t launch_thin_src(const Args& p, hipStream_t stream) {
+  const dim3 grid((unsigned)std::min<int64_t>((p.m * p.n + 255) / 256, 1 << 20));
+  if (p.b.bits == 4) thin<SRC, 4><<<grid, 256, 0, stream>>>(p);
+  else thin<SRC, 8><<<grid, 256, 0, stream>>>(p);
+  return hipGetLastError();
+}
+hipError_t launch_thin(int src, const Args& p, hipStream_t stream) {
+  if (src == SRC_BF16) return launch_thin_src<SRC_BF16>(p, stream);
+  if (src == SRC_F16) return launch_thin_src<SRC_F16>(p, stream);
+  return launch_thin_src<SRC_F32>(p, stream);
+}
+
 // ---- the parts of a split sum, in their order -------------------------------------
 // LANES lanes share four elements of C, each adding every LANES-th part; their sums
 // are then added in turn.
@@ -303,6 +344,11 @@ double tiled_time(bool scaled, int parts, int64_t bm, int64_t bn, int64_t splits
 
 ProductPlan plan_product(int src, bool k_next, int bbits, int64_t m, int64_t n, int64_t k) {
   ProductPlan r{};
+  if (src != SRC_MX4 && src != SRC_MX8 && k < 8) {
+    r.variant = THIN;
+    r.splits = 1;
+    return r;
+  }
   if (m <= 64 && k_next) {
     r.variant = FEW_ROWS;
     r.bm = m <= 16 ? 16 : m <= 32 ? 32 : 64;
@@ -378,7 +424,8 @@ hipError_t launch_mx_product(const ProductArgs& a, hipStream_t stream) {
   } else {
     plan.splits = 1;
   }
-  hipError_t err = plan.variant == FEW_ROWS     ? launch_few(src, p, plan, stream)
+  hipError_t err = plan.variant == THIN         ? launch_thin(src, p, stream)
+                   : plan.variant == FEW_ROWS   ? launch_few(src, p, plan, stream)
                    : plan.variant == TILES_BF16 ? launch_tiles_bf16(src, p, plan, stream)
                                                 : launch_tiles_scaled(p, plan, stream);
   if (err != hipSuccess || plan.splits == 1) return err;

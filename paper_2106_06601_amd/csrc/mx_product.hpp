@@ -78,29 +78,36 @@ struct Args {
   int64_t part;  // elements between the parts of a split sum (0: not split)
 };
 
-// Eight consecutive elements of a line of a plain matrix at p, of which n
-// (at most 8) are there; the rest zero.  Vector loads need no alignment.
+// Eight consecutive elements of a line of a plain matrix.  Vector loads need no alignment.
 template <int SRC>
 struct Raw8 {
   uint32_t w[2 * bytes_of(SRC)];
 };
+// Elements k .. k + 7 of a line of len >= 8 elements that begins at `line`: the load is of
+// the line's last eight where fewer are left (always one load, so that none waits for
+// another), and place8 moves them into place, with zeros behind.
 template <int SRC>
-__device__ inline Raw8<SRC> load8(const char* p, int64_t n) {
-  Raw8<SRC> r;
-  if (n >= 8) {
-    __builtin_memcpy(r.w, p, sizeof r.w);
-  } else if (bytes_of(SRC) == 4) {
+__device__ inline void load8(Raw8<SRC>& r, const char* line, int64_t k, int64_t len) {
+  __builtin_memcpy(r.w, line + min(k, len - 8) * bytes_of(SRC), sizeof r.w);
+}
+template <int SRC>
+__device__ inline void place8(Raw8<SRC>& r, int64_t k, int64_t len) {
+  const uint32_t s = (uint32_t)max((int64_t)0, min(k - (len - 8), (int64_t)8));  // elements to drop
+  if constexpr (bytes_of(SRC) == 4) {
 #pragma unroll
-    for (int q = 0; q < 8; ++q) r.w[q % (2 * bytes_of(SRC))] = q < n ? reinterpret_cast<const uint32_t*>(p)[q] : 0u;
+    for (int q = 0; q < 8; ++q) r.w[q] = s >= 8 ? 0u : r.w[q];
+#pragma unroll
+    for (int by = 4; by > 0; by /= 2)
+#pragma unroll
+      for (int q = 0; q < 8; ++q) r.w[q] = (s & by) ? (q + by < 8 ? r.w[(q + by) % 8] : 0u) : r.w[q];
   } else {
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const uint32_t lo = 2 * q < n ? reinterpret_cast<const uint16_t*>(p)[2 * q] : 0u;
-      const uint32_t hi = 2 * q + 1 < n ? reinterpret_cast<const uint16_t*>(p)[2 * q + 1] : 0u;
-      r.w[q] = lo | hi << 16;
-    }
+    uint64_t lo = r.w[0] | (uint64_t)r.w[1] << 32, hi = r.w[2] | (uint64_t)r.w[3] << 32;
+    if (s & 4) lo = hi, hi = 0;
+    const uint32_t bits = 16 * (s & 3);
+    if (bits) lo = lo >> bits | hi << (64 - bits), hi >>= bits;
+    if (s >= 8) lo = 0, hi = 0;
+    r.w[0] = (uint32_t)lo, r.w[1] = (uint32_t)(lo >> 32), r.w[2] = (uint32_t)hi, r.w[3] = (uint32_t)(hi >> 32);
   }
-  return r;
 }
 
 // bfloat16 parts of eight elements: each takes the leading 8 bits that are left
@@ -163,7 +170,7 @@ __device__ inline v4f mfma_bf16(v4u a, v4u b, v4f c) {
 }
 
 // How a product runs; a function of sizes and types alone.
-enum Variant : int { FEW_ROWS, TILES_BF16, TILES_SCALED };
+enum Variant : int { FEW_ROWS, TILES_BF16, TILES_SCALED, THIN };
 struct ProductPlan {
   Variant variant;
   int bm, bn;   // tile of C (rows, columns)

@@ -140,7 +140,8 @@ struct LeftStage {
 #pragma unroll
         for (int q = 0; q < PASSES; ++q) {
           const int64_t i = min(i0 + t / 8 + 64 * q, p.m - 1);
-          raw[q] = load8<SRC>(static_cast<const char*>(p.real) + (i * p.a_rs + k) * ES, p.k - k);
+          load8<SRC>(raw[q], static_cast<const char*>(p.real) + i * p.a_rs * ES, k, p.k);
+          place8<SRC>(raw[q], k, p.k);
         }
       }
     }

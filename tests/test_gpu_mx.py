@@ -297,7 +297,7 @@ def check_product(got, a, b, alpha, beta, c0, out):
 
 PRODUCTS = [(1, 1, 1), (1, 16, 32), (1, 130, 500), (3, 17, 33), (16, 16, 128), (17, 100, 257), (40, 300, 129),
             (64, 64, 4096), (65, 33, 2000), (128, 128, 256), (130, 260, 384), (257, 255, 640), (300, 513, 1000),
-            (513, 300, 96), (7, 1024, 8192), (260, 20, 5000)]
+            (513, 300, 96), (7, 1024, 8192), (260, 20, 5000), (70, 40, 5), (5, 300, 7), (130, 70, 8)]
 
 
 @pytest.mark.parametrize("m,n,k", PRODUCTS, ids=str)
