@@ -84,8 +84,10 @@ struct LeftStage {
   static constexpr int TW = (MPT * ES + 3) / 4;
 
   Raw8<SRC> raw[TRANS || MX ? 1 : PASSES];
-  v2u code[MX ? PASSES : 1];
-  uint32_t scale[MX ? PASSES : 1];
+  // few-bit operands: sixteen elements of a lane at a time, half a block
+  static constexpr int HALVES = BM / 128;
+  v4u code[MX ? HALVES : 1];
+  uint32_t scale[MX ? HALVES : 1];
   uint32_t line[TRANS ? 8 : 1][TW];
 
   // (Where a whole step is there, all of its loads stand behind one branch: none
@@ -123,12 +125,16 @@ struct LeftStage {
       const int64_t k = k0 + 8 * c;
       if constexpr (MX) {
 #pragma unroll
-        for (int q = 0; q < PASSES; ++q) {  // (a row is padded to whole steps)
-          const int64_t i = min(i0 + t / 8 + 64 * q, p.m - 1);
-          const uint8_t* at = p.a.data + i * p.a.row_bytes;
-          if (BITS == 4) code[q] = v2u{*reinterpret_cast<const uint32_t*>(at + k / 2), 0u};
-          else code[q] = *reinterpret_cast<const v2u*>(at + k);
-          scale[q] = p.a.scales[i * p.a.row_scales + k / kMxBlock];
+        for (int q = 0; q < HALVES; ++q) {  // (a row is padded to whole steps)
+          const int64_t i = min(i0 + t / 4 + 128 * q, p.m - 1), k16 = k0 + 16 * (t % 4);
+          const uint8_t* at = p.a.data + i * p.a.row_bytes + k16 * BITS / 8;
+          if constexpr (BITS == 4) {
+            const v2u d = *reinterpret_cast<const v2u*>(at);
+            code[q] = v4u{d.x, 0u, d.y, 0u};
+          } else {
+            code[q] = *reinterpret_cast<const v4u*>(at);
+          }
+          scale[q] = p.a.scales[i * p.a.row_scales + k16 / kMxBlock];
         }
       } else if (k0 + kStepBf16 <= p.k) {
 #pragma unroll
@@ -172,12 +178,18 @@ struct LeftStage {
 #pragma unroll
         for (int x = 0; x < P; ++x) stage[x * BM * 8 + chunk_at(MPT * (t % 64) + e, t / 64)] = out[x];
       }
+    } else if constexpr (MX) {
+#pragma unroll
+      for (int q = 0; q < HALVES; ++q)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          stage[chunk_at(t / 4 + 128 * q, 2 * (t % 4) + h)] =
+              mx_decode8_bf16<BITS>(v2u{code[q][2 * h], code[q][2 * h + 1]}, scale[q]);
     } else {
 #pragma unroll
       for (int q = 0; q < PASSES; ++q) {
         v4u out[P];
-        if constexpr (MX) out[0] = mx_decode8_bf16<BITS>(code[q], scale[q]);
-        else raw_parts<SRC>(raw[q], out);
+        raw_parts<SRC>(raw[q], out);
 #pragma unroll
         for (int x = 0; x < P; ++x) stage[x * BM * 8 + chunk_at(t / 8 + 64 * q, t % 8)] = out[x];
       }
@@ -196,14 +208,14 @@ struct RightStage {
     const int t = threadIdx.x;
 #pragma unroll
     for (int q = 0; q < PASSES; ++q) {
-      const int at = t + q * kLanes;
-      if (BN * CHUNKS % kLanes == 0 || at < BN * CHUNKS) {
-        const int64_t j = min(j0 + at / CHUNKS, p.n - 1);
-        data[q] = *reinterpret_cast<const v4u*>(p.b.data + j * p.b.row_bytes + k0 * BBITS / 8 + at % CHUNKS * 16);
-      }
+      const int at = (t + q * kLanes) % (BN * CHUNKS);  // (lanes past the tile repeat others' loads)
+      const int64_t j = min(j0 + at / CHUNKS, p.n - 1);
+      data[q] = *reinterpret_cast<const v4u*>(p.b.data + j * p.b.row_bytes + k0 * BBITS / 8 + at % CHUNKS * 16);
     }
-    if (t < BN) {
-      const int64_t j = min(j0 + t, p.n - 1);
+    // (every lane in the small tiles, where a branch costs a wait for all loads: 1041x1999x2501 of 8 by 4 bits
+    // 43 us with, 37 without; in the large ones the loads cost more than the branch: 470 and 478 us)
+    if (BN < 256 || t < BN) {
+      const int64_t j = min(j0 + t % BN, p.n - 1);
       scale = *reinterpret_cast<const uint16_t*>(p.b.scales + j * p.b.row_scales + k0 / kMxBlock);
     }
   }
