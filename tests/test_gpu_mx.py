@@ -551,3 +551,16 @@ def test_offsets_past_32_bits():
     c = torch.empty(80, rows, device="cuda")
     C.costa_mx_product_real(1.0, "N", big, q, 0.0, c)
     check_product(c[:, -3:], big.cpu().double().numpy(), F.decode(*want, 8, cols), 1.0, 0.0, None, "f32")
+
+
+def test_example_trains():
+    """The example's loss falls to what 4-bit weights leave: their rounding error is up to a
+    quarter of a value (1 to 1.5 of a step of 0.5 .. and so on), so under a tenth of the first loss."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "few_bit_layer.py")
+    spec = importlib.util.spec_from_file_location("few_bit_layer", path)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    losses = mod.train(tokens=2048, inputs=384, outputs=250, steps=8)
+    assert losses[-1] < losses[0] / 10, losses
