@@ -363,7 +363,8 @@ ProductPlan plan_product(int src, bool k_next, int bbits, int64_t m, int64_t n, 
   const bool scaled = src == SRC_MX4 && bbits == 4 && k <= 1 << 24;
   r.variant = scaled ? TILES_SCALED : TILES_BF16;
   const int parts = scaled ? 1 : parts_of(src);
-  const int64_t most = std::min({splits_max(m, n), up_div(k, scaled ? 1024 : 256), (int64_t)kCUs});
+  // (two steps of k each, at least)
+  const int64_t most = std::min({splits_max(m, n), up_div(k, scaled ? 512 : 128), (int64_t)kCUs});
   double best = 0;
   for (const int bn : {256, 128, 64}) {
     if (scaled && bn == 64) continue;
@@ -371,8 +372,8 @@ ProductPlan plan_product(int src, bool k_next, int bbits, int64_t m, int64_t n, 
     const int64_t tiles = up_div(m, bm) * up_div(n, bn);
     // unsplit, in a few, or so that the workgroups are one to four for every CU
     for (int64_t c = 0; c < 8; ++c) {
-      const int64_t s = c < 4 ? c + 1 : (c - 3) * kCUs / std::max<int64_t>(tiles, 1);
-      if (s < 1 || s > most) continue;
+      const int64_t s = std::min(c < 4 ? c + 1 : (c - 3) * kCUs / std::max<int64_t>(tiles, 1), most);
+      if (s < 1) continue;
       const double t = tiled_time(scaled, parts, bm, bn, s, m, n, k);
       if (r.splits == 0 || t < best) {
         best = t;
