@@ -73,7 +73,8 @@ __device__ inline void put_wave(const Args& p, const v4f (&acc)[MT][NT], v4u* sh
 constexpr int kStepBf16 = 64;
 __device__ inline int chunk_at(int row, int chunk) { return row * 8 + (chunk ^ ((row ^ row >> 3) & 7)); }
 
-template <int SRC, bool TRANS, int BM>
+// EDGE: a transposed operand's last lane may have fewer rows than MPT.
+template <int SRC, bool TRANS, int BM, bool EDGE>
 struct LeftStage {
   static constexpr bool MX = SRC == SRC_MX4 || SRC == SRC_MX8;
   static constexpr int BITS = SRC == SRC_MX4 ? 4 : 8;
@@ -89,6 +90,7 @@ struct LeftStage {
   v4u code[MX ? HALVES : 1];
   uint32_t scale[MX ? HALVES : 1];
   uint32_t line[TRANS ? 8 : 1][TW];
+  bool moved;  // (transposed) the last lane's rows are not in place yet
 
   // (Where a whole step is there, all of its loads stand behind one branch: none
   // waits for another.)
@@ -98,20 +100,27 @@ struct LeftStage {
       // wave w has k = k0 + 8 w .. + 7, lane l rows MPT l .. of each
       const int wave = __builtin_amdgcn_readfirstlane(t / 64);
       const char* base = static_cast<const char*>(p.real) + ((k0 + 8 * wave) * p.a_cs + i0) * ES;
-      const int at = MPT * ES * (t % 64);
-      const int64_t left = p.m - i0 - MPT * (t % 64);
+      moved = false;
+      if (!EDGE && k0 + kStepBf16 <= p.k) {
+        if (MPT * (t % 64) < p.m - i0)
 #pragma unroll
-      for (int q = 0; q < 8; ++q)
+          for (int q = 0; q < 8; ++q) __builtin_memcpy(line[q], base + q * p.a_cs * ES + MPT * ES * (t % 64), MPT * ES);
+      } else if (EDGE && p.m >= MPT && k0 + kStepBf16 <= p.k) {
+        // the last lane with rows reads the matrix's last MPT, as do those past it
+        // (whose results are not stored); store() moves what it read into place.
+        // (803x236 over 66454 in float: 211 us row by row, 142 so)
+        moved = true;
+        const char* at = base + min((int64_t)MPT * (t % 64), p.m - i0 - MPT) * ES;
 #pragma unroll
-        for (int w = 0; w < TW; ++w) line[q][w] = 0;
-      if (left >= MPT && k0 + kStepBf16 <= p.k) {
+        for (int q = 0; q < 8; ++q) __builtin_memcpy(line[q], at + q * p.a_cs * ES, MPT * ES);
+      } else {  // the last of k, or fewer rows than a lane takes: one by one
+        const int64_t left = p.m - i0 - MPT * (t % 64);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) __builtin_memcpy(line[q], base + q * p.a_cs * ES + at, MPT * ES);
-      } else if (left > 0) {
+        for (int q = 0; q < 8; ++q) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q)
+          for (int w = 0; w < TW; ++w) line[q][w] = 0;
           if (k0 + 8 * wave + q < p.k) {
-            const char* from = base + q * p.a_cs * ES + at;
+            const char* from = base + (q * p.a_cs + MPT * (t % 64)) * ES;
 #pragma unroll
             for (int e = 0; e < MPT; ++e)
               if (e < left) {
@@ -119,6 +128,7 @@ struct LeftStage {
                 else line[q][e / 2 % TW] |= (uint32_t) reinterpret_cast<const uint16_t*>(from)[e] << (e % 2 * 16);
               }
           }
+        }
       }
     } else {
       const int c = t % 8;
@@ -154,9 +164,22 @@ struct LeftStage {
   }
 
   // stage: P planes of BM x 8 chunks
-  __device__ inline void store(v4u* stage) const {
+  __device__ inline void store(const Args& p, int64_t i0, v4u* stage) {
     const int t = threadIdx.x;
     if constexpr (TRANS) {
+      if (EDGE && moved) {
+        const uint32_t drop = (uint32_t)max((int64_t)0, MPT * (t % 64) - (p.m - i0 - MPT));
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          if constexpr (TW == 1) {
+            line[q][0] >>= 16 * (drop & 1);
+          } else {
+            const uint64_t v = (line[q][0] | (uint64_t)line[q][1] << 32) >> (8 * ES * (drop % MPT));
+            line[q][0] = (uint32_t)v;
+            line[q][1] = (uint32_t)(v >> 32);
+          }
+        }
+      }
 #pragma unroll
       for (int e = 0; e < MPT; ++e) {
         v4u out[P];
@@ -231,7 +254,7 @@ struct RightStage {
 };
 
 // AHEAD: steps whose loads are on their way at once.
-template <int SRC, bool TRANS, int BBITS, int BM, int BN, int WM, int AHEAD>
+template <int SRC, bool TRANS, int BBITS, int BM, int BN, int WM, int AHEAD, bool EDGE>
 __global__ __launch_bounds__(kLanes) void tiles_bf16(Args p, uint32_t nm, uint32_t nn) {
   constexpr int WN = kWaves / WM, MT = BM / WM / 16, NT = BN / WN / 16, P = parts_of(SRC);
   constexpr int BROW = kStepBf16 * BBITS / 8;
@@ -252,7 +275,7 @@ __global__ __launch_bounds__(kLanes) void tiles_bf16(Args p, uint32_t nm, uint32
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = v4f{0, 0, 0, 0};
 
-  LeftStage<SRC, TRANS, BM> ls[AHEAD];
+  LeftStage<SRC, TRANS, BM, EDGE> ls[AHEAD];
   RightStage<BBITS, BN> rs[AHEAD];
   auto load = [&](int set, int64_t t) {
     if (t < last) {
@@ -261,7 +284,7 @@ __global__ __launch_bounds__(kLanes) void tiles_bf16(Args p, uint32_t nm, uint32
     }
   };
   load(0, first);
-  ls[0].store(left[0]);
+  ls[0].store(p, i0, left[0]);
   rs[0].store(right[0], scales[0]);
 #pragma unroll
   for (int a = 1; a <= AHEAD; ++a) load(a % AHEAD, first + a);
@@ -301,7 +324,7 @@ __global__ __launch_bounds__(kLanes) void tiles_bf16(Args p, uint32_t nm, uint32
       }
       if (t + 1 < last) {
         const int set = (s + 1) % AHEAD;  // (AHEAD is 1 or 2: a step's parity is its set)
-        ls[set].store(left[1 - s]);
+        ls[set].store(p, i0, left[1 - s]);
         rs[set].store(right[1 - s], scales[1 - s]);
         load(set, t + 1 + AHEAD);
       }
@@ -443,14 +466,23 @@ hipError_t launch_bf16(const Args& p, const ProductPlan& plan, hipStream_t strea
   const uint32_t nm = (uint32_t)((p.m + plan.bm - 1) / plan.bm), nn = (uint32_t)((p.n + plan.bn - 1) / plan.bn);
   if ((int64_t)nm * nn > 1 << 22) return hipErrorInvalidValue;
   const dim3 grid(nm * nn, plan.splits);
-  if (plan.bm == BM && plan.bn == 256)
-    tiles_bf16<SRC, TRANS, BBITS, BM, 256, 2, 1><<<grid, kLanes, 0, stream>>>(p, nm, nn);
-  else if (plan.bm == 128 && plan.bn == 128)
-    tiles_bf16<SRC, TRANS, BBITS, 128, 128, 2, 1><<<grid, kLanes, 0, stream>>>(p, nm, nn);
+  if (plan.bm == BM && plan.bn == 256) {
+    // (transposed operands: a kernel of its own where every lane has all of its rows or none.
+    // 4096x4096 over 16384 in bfloat16 takes 470 us, with the other kernel 511; 803x236 over 66454 takes 77 us with
+    // the other one, with its last lane's rows one by one 96)
+    if constexpr (TRANS) {
+      if (p.m % (BM / 64) == 0) {
+        tiles_bf16<SRC, TRANS, BBITS, BM, 256, 2, 1, false><<<grid, kLanes, 0, stream>>>(p, nm, nn);
+        return hipGetLastError();
+      }
+    }
+    tiles_bf16<SRC, TRANS, BBITS, BM, 256, 2, 1, true><<<grid, kLanes, 0, stream>>>(p, nm, nn);
+  } else if (plan.bm == 128 && plan.bn == 128)
+    tiles_bf16<SRC, TRANS, BBITS, 128, 128, 2, 1, true><<<grid, kLanes, 0, stream>>>(p, nm, nn);
   else if (plan.bm != 128 || plan.bn != 64)
     return hipErrorInvalidValue;  // not a tile of this kernel
   else
-    tiles_bf16<SRC, TRANS, BBITS, 128, 64, 4, 2><<<grid, kLanes, 0, stream>>>(p, nm, nn);
+    tiles_bf16<SRC, TRANS, BBITS, 128, 64, 4, 2, true><<<grid, kLanes, 0, stream>>>(p, nm, nn);
   return hipGetLastError();
 }
 template <int SRC, bool TRANS>
