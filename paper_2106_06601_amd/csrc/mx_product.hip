@@ -21,7 +21,10 @@ constexpr int kCUs = 256;
 // shared memory of its own.  (Read in that order straight from memory, a load
 // touches 64 pieces of 16 bytes, and the left operand costs more than B.)  The next piece of
 // B and the next slab are on their way meanwhile.  The waves' sums are joined
-// through shared memory, pairwise, in a fixed order.
+// through shared memory, pairwise, in a fixed order.  Measured, B in 4 bits: one row
+// of bfloat16 by 8192x8192 13 us (35.7 MB of B, 2.7 TB/s; a launch and the first loads
+// take about 5 us of any call, past them B comes at 4.5 TB/s), 13 rows of float16 by 20000x4095
+// 24 us, 64 rows of bfloat16 by 8192x8192 40 us, of float 91 (three parts).
 constexpr int kFewWaves = 4;
 constexpr int kSlab = 128;
 
@@ -274,7 +277,7 @@ hipError_t launch_thin(int src, const Args& p, hipStream_t stream) {
   return launch_thin_src<SRC_F32>(p, stream);
 }
 
-// ---- the parts of a split sum, in their order -------------------------------------
+// ---- the parts of a split sum, in a fixed order -------------------------------------
 // LANES lanes share four elements of C, each adding every LANES-th part; their sums
 // are then added in turn.
 template <int LANES>

@@ -69,7 +69,16 @@ __device__ inline void put_wave(const Args& p, const v4f (&acc)[MT][NT], v4u* sh
 // chunks (8 elements) permuted within a row so that lanes on neighbouring rows meet
 // different banks; the right tile as stored, decoded on the way to the matrix
 // instruction (16 elements of a row a lane and step, 8 for each of two
-// instructions; the left operand is read in the same order of k).
+// instructions; the left operand is read in the same order of k).  A few-bit tile in
+// shared memory is a quarter or half of what it is decoded, and decoding costs 8
+// conversions for 4 * MT matrix instructions.
+//
+// Measured: 2048x8192x8192 of bfloat16 by 4 bits 217 to 235 us (1.17 to 1.27 PFLOP/s; the
+// library's product of two bfloat16 matrices reaches 1.47 at 8192^3), 4096x4096 over 16384
+// transposed by 8 bits 470 to 515 us (1.07 to 1.17).  The matrix units are busy half of the
+// time, at 2.0 to 2.1 GHz; a third stage, reading further ahead and wave priorities changed
+// nothing.  256x256 tiles for one bfloat16 part (8 waves of 128x64: 128 registers of sums), 128x256
+// for two and three, whose parts fill the shared memory; smaller tiles where those are few.
 constexpr int kStepBf16 = 64;
 __device__ inline int chunk_at(int row, int chunk) { return row * 8 + (chunk ^ ((row ^ row >> 3) & 7)); }
 
@@ -339,7 +348,10 @@ __global__ __launch_bounds__(kLanes) void tiles_bf16(Args p, uint32_t nm, uint32
 // rounded into a 32-bit sum.  (The same instruction on 8-bit elements drops what is
 // some 2^-13 of its largest product: 1.5e-5 of a product of normal matrices, more
 // where a few columns stand out; those products take the bfloat16 kernel.)  k goes
-// by 256, so that a step's row is 128 bytes.
+// by 256, so that a step's row is 128 bytes.  Measured at 8192^3: 296 to 333 us, 3.3 to 3.7
+// PFLOP/s (the library's 8-bit product reaches 2.7); the matrix units are busy 41% of the time at
+// 2.0 GHz, and the waves wait a third of theirs, mostly for the next stage.  With the stage
+// loaded to registers first the tile's registers did not suffice (1914 us).
 constexpr int kStep4 = 256;
 constexpr int kRowChunks = 8;  // 16-byte chunks of a step's row
 __device__ inline int code_at(int row, int chunk) { return row * kRowChunks + (chunk ^ (row & 7)); }
