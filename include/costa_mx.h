@@ -88,7 +88,7 @@ costa_status costa_mx_sizes(costa_mx_format format, int64_t rows, int64_t cols, 
 /* Q <- mx(alpha * B) and QT <- mx(alpha * B^T), either of them or (one read of
  * B) both; the other is NULL.  Q has B's shape, QT the transposed one; their
  * formats may differ.  x = alpha * b: b rounded to a 32-bit float, then the
- * product rounded (alpha == 1: no rounding).  Errors: INVALID_VALUE for null
+ * product rounded (alpha == 1: no rounding).  B, Q and QT must not overlap.  Errors: INVALID_VALUE for null
  * or misaligned pointers, unknown types, a leading dimension that is too
  * small, neither Q nor QT; SHAPE_MISMATCH; NOT_SUPPORTED for dimensions above
  * 2^31 - 1 (as in every call here). */
@@ -119,7 +119,7 @@ costa_status costa_mx_dequantize(float alpha, const costa_mx* Q, float beta, con
  * are exact and summed in 32 bits; alpha and beta apply in 32 bits, C is rounded
  * once.  (With an 8-bit operand the values enter as bfloat16, which holds all of
  * them but those below 2^-133: blocks whose largest magnitude is under 2^-116.)
- * C must not overlap A or B.
+ * C must not overlap A or B, nor the workspace any of them.
  * beta == 0: C is not read.  k == 0: C <- beta * C.
  * workspace: device memory for the parts of a sum that is split over several
  * workgroups (calls with few rows or columns and a long sum), 16-byte aligned,

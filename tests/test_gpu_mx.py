@@ -495,6 +495,35 @@ def test_captured_calls():
     assert e.value.status == C.NOT_SUPPORTED
 
 
+def test_tables_of_many_layouts():
+    """More layouts than the library keeps tables of; a captured call's stay for its replays."""
+    L = C.Layout.block_cyclic(100, 90, 16, 32, 2, 2)
+    bufs = [torch.randn(L.local_elems(r)).cuda() for r in range(4)]
+    q, want = C.MxMatrix.empty(8, 100, 90), C.MxMatrix.empty(8, 100, 90)
+    C.costa_mx_quantize_layout("f32", 1.0, L, bufs, want)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        C.costa_mx_quantize_layout("f32", 1.0, L, bufs, q)
+    x = torch.randn(60, 70)
+    for k in range(150):
+        M = C.Layout.general(60, 70, [0, 1 + k % 59, 60], [0, 1 + k % 69, 70], [0, 1, 2, 0], 3, "row")
+        parts = [torch.zeros(max(1, M.local_elems(r))).cuda() for r in range(3)]
+        for bi, (r0, r1) in enumerate(((0, 1 + k % 59), (1 + k % 59, 60))):
+            for bj, (c0, c1) in enumerate(((0, 1 + k % 69), (1 + k % 69, 70))):
+                o, off, ld = C.costa_layout_block(M.handle, bi, bj)
+                torch.as_strided(parts[o], (r1 - r0, c1 - c0), (ld, 1), off).copy_(x[r0:r1, c0:c1])
+        m = filled(4, 60, 70)
+        C.costa_mx_quantize_layout("f32", 1.0, M, parts, m)
+        check_stored(m, x.numpy())
+    for _ in range(3):
+        q.data.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(q.data, want.data) and torch.equal(q.scales, want.scales)
+
+
 # ---------------------------------------------------------------------------
 # gradients
 # ---------------------------------------------------------------------------

@@ -150,6 +150,16 @@ def test_layouts_that_are_refused():
     assert f(F32, many.handle, [BUF] * 257, Q(rows=600)) == C.NOT_SUPPORTED
 
 
+@pytest.mark.spawns
+def test_header_is_plain_c(tmp_path):
+    import subprocess
+    src = tmp_path / "t.c"
+    src.write_text('#include "costa_mx.h"\nint main(void) { costa_mx q = {COSTA_MX_E2M1, 1, 1, 0, 0}; return (int)q.rows - 1; }\n')
+    rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Wextra", "-Werror", "-D__HIP_PLATFORM_AMD__", "-fsyntax-only", "-I",
+                    os.path.join(ROOT, "include"), "-I", os.path.join(rocm, "include"), str(src)], check=True)
+
+
 def test_python_views_are_checked():
     import torch
     with pytest.raises(ValueError):  # host memory never reaches a kernel
