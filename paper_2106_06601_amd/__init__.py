@@ -613,17 +613,18 @@ def costa_mx_workspace(m: int, n: int, k: int) -> int:
 def _product_workspace(m: int, n: int, k: int, workspace, device, stream):
     """(address, bytes, tensor to keep until the call returns) of a product's
     workspace: the caller's uint8 tensor, or one from torch's allocator.  That
-    one belongs to torch's current stream; it is marked as used on `stream`
-    where the call runs on another."""
+    one comes from the pool of the stream that the call runs on: a block of
+    another stream's may still have work of that stream queued on it."""
     if workspace is None:
         n = costa_mx_workspace(m, n, k)
         if n == 0:
             return None, 0, None
-        workspace = torch.empty(n, dtype=torch.uint8, device=device)
-        if stream is not None:
-            at = _stream(stream)
-            if at != torch.cuda.current_stream().cuda_stream:
-                workspace.record_stream(torch.cuda.ExternalStream(at) if at else torch.cuda.default_stream())
+        at = None if stream is None else _stream(stream)
+        if at is None or at == torch.cuda.current_stream().cuda_stream:
+            workspace = torch.empty(n, dtype=torch.uint8, device=device)
+        else:
+            with torch.cuda.stream(torch.cuda.ExternalStream(at) if at else torch.cuda.default_stream()):
+                workspace = torch.empty(n, dtype=torch.uint8, device=device)
     elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or not workspace.is_cuda:
         raise ValueError("workspace: a contiguous uint8 tensor on the GPU is needed")
     return workspace.data_ptr() or None, workspace.numel(), workspace
