@@ -173,17 +173,17 @@ void fill_tables(const Layout& L, HostTables& h) {
   for (int s = 0; s < 2; ++s) h.splits[s] = MxSplits{nullptr, (int32_t)h.start[s].size() - 1, 0, 0, 0, 0, 0};
 }
 
-// The device tables of a layout; uploaded on the first call.
+// The device tables of a layout; uploaded on the first call.  The caller holds T.mu
+// until the kernel that reads them is enqueued: a call that starts the tables over
+// waits for kernels that are, not for one that is yet to be.
 // `p` holds the ranks' buffers and gets them in the order that the kernel looks them up.
-costa_status layout_tables(const Layout& L, hipStream_t stream, MxLayoutArgs& out, MxPointers& p) {
+costa_status layout_tables(TableState& T, const Layout& L, hipStream_t stream, MxLayoutArgs& out, MxPointers& p) {
   int device = 0;
   HIP_OR_FAIL(hipGetDevice(&device));
   hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
   bool capturing = false;
   if (hipStreamIsCapturing(stream, &cs) == hipSuccess) capturing = cs == hipStreamCaptureStatusActive;
   else (void)hipGetLastError();  // the null stream, while another stream captures
-  TableState& T = table_state();
-  std::lock_guard<std::mutex> lock(T.mu);
   const std::pair<int, uint64_t> key(device, L.id);
   auto it = T.tables.find(key);
   if (it == T.tables.end()) {
@@ -358,7 +358,9 @@ extern "C" costa_status costa_mx_quantize_layout(costa_real type, float alpha, c
       return COSTA_SUCCESS;
     }
     MxLayoutArgs l{};
-    CHECKED(layout_tables(*L, stream, l, p));
+    TableState& T = table_state();
+    std::lock_guard<std::mutex> lock(T.mu);
+    CHECKED(layout_tables(T, *L, stream, l, p));
     HIP_OR_FAIL(launch_mx_quantize_layout(a, l, p, stream));
     return COSTA_SUCCESS;
   });

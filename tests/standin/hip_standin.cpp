@@ -26,6 +26,7 @@
 #include <vector>
 
 #include "../../paper_2106_06601_amd/csrc/index_math.hpp"
+#include "../../paper_2106_06601_amd/csrc/mx.hpp"
 
 using namespace costa;
 
@@ -61,6 +62,7 @@ std::map<const void*, std::pair<size_t, void*>> symbols;
 std::string faults;
 hipError_t last = hipSuccess;
 bool implicit_refused = false;  // a blocking stream captures: the null stream reports it
+void (*before_launch)() = nullptr;  // a test's, called once, by a launch before it is enqueued
 
 hipError_t err(hipError_t e) {
   if (e != hipSuccess) last = e;
@@ -245,6 +247,7 @@ void standin_tile_walk(int32_t lanes, int32_t tid, int32_t len, int64_t ld, int3
   if (lanes == kSmallTileLanes) walk(TileWalk<kSmallTileLanes>(tid, len, ld, ls, lc));
   else walk(TileWalk<kThreadsPerTask>(tid, len, ld, ls, lc));
 }
+void standin_before_launch(void (*f)()) { before_launch = f; }
 void standin_refuse_implicit(int on) { implicit_refused = on != 0; }
 const char* standin_faults() {
   static std::string out;
@@ -421,6 +424,11 @@ void __hipRegisterVar(void**, void* var, char*, char*, int, size_t size, int, in
 
 hipError_t hipLaunchKernel(const void* f, dim3 grid, dim3, void** args, size_t, hipStream_t stream) {
   const std::string name = kernels[f];
+  if (before_launch) {
+    void (*const call)() = before_launch;
+    before_launch = nullptr;
+    call();
+  }
   if (name.find("costa_mover") != std::string::npos || name.find("costa_tiles") != std::string::npos) {
     const ArgTable table = arg<ArgTable>(args, 0);
     const Piece* pieces = arg<const Piece*>(args, 1);
@@ -439,6 +447,15 @@ hipError_t hipLaunchKernel(const void* f, dim3 grid, dim3, void** args, size_t, 
   } else if (name.find("costa_volume_dealt") != std::string::npos) {
     const VolumeDealtArgs a = arg<VolumeDealtArgs>(args, 0);
     add(at(stream), [=] { volume(a); });
+  } else if (name.find("quantize_tiles") != std::string::npos && name.find("Dealt") != std::string::npos) {
+    // (its arithmetic is not run: what it reads of the layout's tables has to be there)
+    const MxLayoutArgs l = arg<MxLayoutArgs>(args, 1);
+    add(at(stream), [=] {
+      if (!holds(memory, l.cells, (size_t)l.nplace * sizeof(MxCell))) fault("a layout's cells that are gone");
+      for (const MxSplits* q : {&l.line, &l.place})
+        if (q->start && !holds(memory, q->start, (size_t)(q->n + 1) * sizeof(int64_t)))
+          fault("a layout's splits that are gone");
+    });
   } else {
     fault("a kernel that the stand-in does not run: " + name);
   }
