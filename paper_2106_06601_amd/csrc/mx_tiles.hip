@@ -8,6 +8,7 @@
 // l % 16 of C and four neighbouring columns, which makes wide stores.
 #include <algorithm>
 
+#include "index_math.hpp"
 #include "mx_product.hpp"
 
 namespace costa {
@@ -16,16 +17,13 @@ namespace {
 constexpr int kWaves = 8;
 constexpr int kLanes = 64 * kWaves;
 
-// Tile (tm, tn) of workgroup b of a launch over nm x nn tiles.  Workgroups go
-// round the 8 XCDs in turn; each XCD gets a run of neighbouring tiles (8 tile
-// rows wide, by columns), whose operands its L2 holds.
-__device__ inline void tile_of(uint32_t b, uint32_t nm, uint32_t nn, int64_t& tm, int64_t& tn) {
-  const uint32_t total = nm * nn, per = total / 8, more = total % 8, x = b % 8;
-  const uint32_t t = x * per + min(x, more) + b / 8;
-  const uint32_t group = t / (8 * nn), rows = min(8u, nm - group * 8), in = t - group * 8 * nn;
+// This workgroup's tile.
+__device__ inline void my_tile(const TileRange& r, int64_t& tm, int64_t& tn) {
+  uint32_t m, n;
+  xcd_tile(blockIdx.x, gridDim.x, r, m, n);
   // (the division runs on vector registers: both are the wave's, not a lane's)
-  tm = __builtin_amdgcn_readfirstlane(group * 8 + in % rows);
-  tn = __builtin_amdgcn_readfirstlane(in / rows);
+  tm = __builtin_amdgcn_readfirstlane(m);
+  tn = __builtin_amdgcn_readfirstlane(n);
 }
 
 // Part y of `parts` of a sum's steps.
@@ -264,7 +262,7 @@ struct RightStage {
 
 // AHEAD: steps whose loads are on their way at once.
 template <int SRC, bool TRANS, int BBITS, int BM, int BN, int WM, int AHEAD, bool EDGE>
-__global__ __launch_bounds__(kLanes) void tiles_bf16(Args p, uint32_t nm, uint32_t nn) {
+__global__ __launch_bounds__(kLanes) void tiles_bf16(Args p, TileRange range) {
   constexpr int WN = kWaves / WM, MT = BM / WM / 16, NT = BN / WN / 16, P = parts_of(SRC);
   constexpr int BROW = kStepBf16 * BBITS / 8;
   __shared__ v4u left[2][P * BM * 8];
@@ -273,7 +271,7 @@ __global__ __launch_bounds__(kLanes) void tiles_bf16(Args p, uint32_t nm, uint32
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, g = lane / 16;
   const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
   int64_t tm, tn;
-  tile_of(blockIdx.x, nm, nn, tm, tn);
+  my_tile(range, tm, tn);
   const int64_t i0 = tm * BM, j0 = tn * BN;
   int64_t first, last;
   steps_of((uint32_t)((p.k + kStepBf16 - 1) / kStepBf16), blockIdx.y, gridDim.y, first, last);
@@ -393,7 +391,7 @@ __device__ inline v8i operand4(v4u d) {  // the instruction reads four of the ei
 }
 
 template <int BM, int BN, int WM>
-__global__ __launch_bounds__(kLanes) void tiles_scaled(Args p, uint32_t nm, uint32_t nn) {
+__global__ __launch_bounds__(kLanes) void tiles_scaled(Args p, TileRange range) {
   constexpr int WN = kWaves / WM, MT = BM / WM / 16, NT = BN / WN / 16;
   __shared__ v4u left[2][BM * kRowChunks];
   __shared__ v4u right[2][BN * kRowChunks];
@@ -401,7 +399,7 @@ __global__ __launch_bounds__(kLanes) void tiles_scaled(Args p, uint32_t nm, uint
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, g = lane / 16;
   const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
   int64_t tm, tn;
-  tile_of(blockIdx.x, nm, nn, tm, tn);
+  my_tile(range, tm, tn);
   const int64_t i0 = tm * BM, j0 = tn * BN;
   int64_t first, last;
   steps_of((uint32_t)((p.k + kStep4 - 1) / kStep4), blockIdx.y, gridDim.y, first, last);
@@ -471,31 +469,45 @@ __global__ __launch_bounds__(kLanes) void tiles_scaled(Args p, uint32_t nm, uint
   put_wave<MT, NT>(p, acc, &left[0][0], wave, i0 + wm, j0 + wn);
 }
 
+// Launches the tiles of C in slices that a grid holds.
+template <typename F>
+hipError_t launch_slices(const Args& p, const ProductPlan& plan, F launch) {
+  const int64_t nm = (p.m + plan.bm - 1) / plan.bm, nn = (p.n + plan.bn - 1) / plan.bn;
+  // (a C of 16 TiB and more: either dimension is below 2^31)
+  if (nm * nn > kTilesMax) throw LimitExceeded("a product of more than 2^31 - 1 tiles");
+  for (int64_t first = 0; first < nm * nn; first += kTileSlice) {
+    launch(dim3((unsigned)std::min(kTileSlice, nm * nn - first), plan.splits),
+           TileRange{(uint32_t)nm, (uint32_t)nn, (uint32_t)first});
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 template <int SRC, bool TRANS, int BBITS>
 hipError_t launch_bf16(const Args& p, const ProductPlan& plan, hipStream_t stream) {
   constexpr int BM = parts_of(SRC) == 1 ? 256 : 128;
-  // (C would not fit the device's memory with 2^32 tiles)
-  const uint32_t nm = (uint32_t)((p.m + plan.bm - 1) / plan.bm), nn = (uint32_t)((p.n + plan.bn - 1) / plan.bn);
-  if ((int64_t)nm * nn > 1 << 22) return hipErrorInvalidValue;
-  const dim3 grid(nm * nn, plan.splits);
-  if (plan.bm == BM && plan.bn == 256) {
-    // (transposed operands: a kernel of its own where every lane has all of its rows or none.
-    // 4096x4096 over 16384 in bfloat16 takes 470 us, with the other kernel 511; 803x236 over 66454 takes 77 us with
-    // the other one, with its last lane's rows one by one 96)
-    if constexpr (TRANS) {
-      if (p.m % (BM / 64) == 0) {
-        tiles_bf16<SRC, TRANS, BBITS, BM, 256, 2, 1, false><<<grid, kLanes, 0, stream>>>(p, nm, nn);
-        return hipGetLastError();
-      }
-    }
-    tiles_bf16<SRC, TRANS, BBITS, BM, 256, 2, 1, true><<<grid, kLanes, 0, stream>>>(p, nm, nn);
-  } else if (plan.bm == 128 && plan.bn == 128)
-    tiles_bf16<SRC, TRANS, BBITS, 128, 128, 2, 1, true><<<grid, kLanes, 0, stream>>>(p, nm, nn);
-  else if (plan.bm != 128 || plan.bn != 64)
+  const bool wide = plan.bm == BM && plan.bn == 256;
+  if (!wide && (plan.bm != 128 || (plan.bn != 128 && plan.bn != 64)))
     return hipErrorInvalidValue;  // not a tile of this kernel
-  else
-    tiles_bf16<SRC, TRANS, BBITS, 128, 64, 4, 2, true><<<grid, kLanes, 0, stream>>>(p, nm, nn);
-  return hipGetLastError();
+  return launch_slices(p, plan, [&](dim3 grid, TileRange range) {
+    if (wide) {
+      // (transposed operands: a kernel of its own where every lane has all of its rows or none.
+      // 4096x4096 over 16384 in bfloat16 takes 470 us, with the other kernel 511; 803x236 over 66454 takes 77 us with
+      // the other one, with its last lane's rows one by one 96)
+      if constexpr (TRANS) {
+        if (p.m % (BM / 64) == 0) {
+          tiles_bf16<SRC, TRANS, BBITS, BM, 256, 2, 1, false><<<grid, kLanes, 0, stream>>>(p, range);
+          return;
+        }
+      }
+      tiles_bf16<SRC, TRANS, BBITS, BM, 256, 2, 1, true><<<grid, kLanes, 0, stream>>>(p, range);
+    } else if (plan.bn == 128) {
+      tiles_bf16<SRC, TRANS, BBITS, 128, 128, 2, 1, true><<<grid, kLanes, 0, stream>>>(p, range);
+    } else {
+      tiles_bf16<SRC, TRANS, BBITS, 128, 64, 4, 2, true><<<grid, kLanes, 0, stream>>>(p, range);
+    }
+  });
 }
 template <int SRC, bool TRANS>
 hipError_t launch_bf16_bits(const Args& p, const ProductPlan& plan, hipStream_t stream) {
@@ -519,14 +531,12 @@ hipError_t launch_tiles_bf16(int src, const Args& p, const ProductPlan& plan, hi
 }
 
 hipError_t launch_tiles_scaled(const Args& p, const ProductPlan& plan, hipStream_t stream) {
-  // (C would not fit the device's memory with 2^32 tiles)
-  const uint32_t nm = (uint32_t)((p.m + plan.bm - 1) / plan.bm), nn = (uint32_t)((p.n + plan.bn - 1) / plan.bn);
-  if ((int64_t)nm * nn > 1 << 22) return hipErrorInvalidValue;
-  const dim3 grid(nm * nn, plan.splits);
-  if (plan.bm == 256 && plan.bn == 256) tiles_scaled<256, 256, 2><<<grid, kLanes, 0, stream>>>(p, nm, nn);
-  else if (plan.bm != 128 || plan.bn != 128) return hipErrorInvalidValue;  // not a tile of this kernel
-  else tiles_scaled<128, 128, 2><<<grid, kLanes, 0, stream>>>(p, nm, nn);
-  return hipGetLastError();
+  const bool wide = plan.bm == 256 && plan.bn == 256;
+  if (!wide && (plan.bm != 128 || plan.bn != 128)) return hipErrorInvalidValue;  // not a tile of this kernel
+  return launch_slices(p, plan, [&](dim3 grid, TileRange range) {
+    if (wide) tiles_scaled<256, 256, 2><<<grid, kLanes, 0, stream>>>(p, range);
+    else tiles_scaled<128, 128, 2><<<grid, kLanes, 0, stream>>>(p, range);
+  });
 }
 
 }  // namespace costa

@@ -62,6 +62,11 @@ std::map<const void*, std::pair<size_t, void*>> symbols;
 std::string faults;
 hipError_t last = hipSuccess;
 bool implicit_refused = false;  // a blocking stream captures: the null stream reports it
+struct TileLaunch {
+  TileRange range;
+  uint32_t tiles, splits;
+};
+std::vector<TileLaunch> tile_launches;  // of products
 void (*before_launch)() = nullptr;  // a test's, called once, by a launch before it is enqueued
 
 hipError_t err(hipError_t e) {
@@ -246,6 +251,17 @@ void standin_tile_walk(int32_t lanes, int32_t tid, int32_t len, int64_t ld, int3
   };
   if (lanes == kSmallTileLanes) walk(TileWalk<kSmallTileLanes>(tid, len, ld, ls, lc));
   else walk(TileWalk<kThreadsPerTask>(tid, len, ld, ls, lc));
+}
+// The launches of product tiles since the last call: nm, nn, first, tiles, splits of each.
+int standin_tile_launches(uint32_t* out, int most) {
+  const int n = (int)tile_launches.size();
+  if (n <= most && n) std::memcpy(out, tile_launches.data(), n * sizeof(TileLaunch));
+  tile_launches.clear();
+  return n;
+}
+void standin_xcd_tiles(uint32_t nm, uint32_t nn, uint32_t first, uint32_t n, uint32_t b0, uint32_t count, uint32_t* tm,
+                       uint32_t* tn) {
+  for (uint32_t k = 0; k < count; ++k) xcd_tile(b0 + k, n, TileRange{nm, nn, first}, tm[k], tn[k]);
 }
 void standin_before_launch(void (*f)()) { before_launch = f; }
 void standin_refuse_implicit(int on) { implicit_refused = on != 0; }
@@ -456,6 +472,8 @@ hipError_t hipLaunchKernel(const void* f, dim3 grid, dim3, void** args, size_t, 
         if (q->start && !holds(memory, q->start, (size_t)(q->n + 1) * sizeof(int64_t)))
           fault("a layout's splits that are gone");
     });
+  } else if (name.find("tiles_bf16") != std::string::npos || name.find("tiles_scaled") != std::string::npos) {
+    tile_launches.push_back({arg<TileRange>(args, 1), grid.x, grid.y});  // (not run)
   } else {
     fault("a kernel that the stand-in does not run: " + name);
   }
