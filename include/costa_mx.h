@@ -119,7 +119,8 @@ costa_status costa_mx_dequantize(float alpha, const costa_mx* Q, float beta, con
  * are exact and summed in 32 bits; alpha and beta apply in 32 bits, C is rounded
  * once.  (With an 8-bit operand the values enter as bfloat16, which holds all of
  * them but those below 2^-133: blocks whose largest magnitude is under 2^-116.)
- * C must not overlap A or B, nor the workspace any of them.
+ * C must not overlap A or B, nor the workspace any of them (elements count, not what
+ * lies between them: slices of one buffer may be side by side).
  * beta == 0: C is not read.  k == 0: C <- beta * C.  NOT_SUPPORTED for a C of
  * more than 2^31 - 1 of the kernels' tiles (16 TiB and more).
  * workspace: device memory for the parts of a sum that is split over several

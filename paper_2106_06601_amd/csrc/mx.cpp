@@ -10,6 +10,7 @@
 
 #include "mx.hpp"
 #include "plan.hpp"
+#include "spans.hpp"
 
 namespace costa {
 namespace {
@@ -230,19 +231,15 @@ costa_status layout_tables(TableState& T, const Layout& L, hipStream_t stream, M
   return COSTA_SUCCESS;
 }
 
-// Whether [p, p + bytes) meets the elements of the matrix a.
-bool overlaps(const void* p, int64_t bytes, const costa_matrix& a) {
-  if (!p || bytes <= 0 || a.rows == 0 || a.cols == 0) return false;
-  const int64_t line = a.order == COSTA_COL_MAJOR ? a.rows : a.cols, lines = a.order == COSTA_COL_MAJOR ? a.cols : a.rows;
-  const uintptr_t b0 = (uintptr_t)p, c0 = (uintptr_t)a.data;
-  const uintptr_t c1 = c0 + (uintptr_t)(((lines - 1) * a.ld + line) * real_size(a.type));
-  return b0 < c1 && c0 < b0 + (uintptr_t)bytes;
+// The memory of a matrix's elements, and of a buffer of `bytes`.
+Span span_of(const costa_matrix& a) {
+  if (a.rows == 0 || a.cols == 0) return Span{0, 0, 0, 0};
+  const int64_t es = real_size(a.type), line = a.order == COSTA_COL_MAJOR ? a.rows : a.cols;
+  return Span{(uintptr_t)a.data, line * es, a.ld * es, a.order == COSTA_COL_MAJOR ? a.cols : a.rows};
 }
-int64_t matrix_bytes(const costa_matrix& a) {
-  if (a.rows == 0 || a.cols == 0) return 0;
-  const int64_t line = a.order == COSTA_COL_MAJOR ? a.rows : a.cols, lines = a.order == COSTA_COL_MAJOR ? a.cols : a.rows;
-  return ((lines - 1) * a.ld + line) * real_size(a.type);
-}
+Span span_of(const void* p, int64_t bytes) { return Span{(uintptr_t)p, p ? bytes : 0, bytes, 1}; }
+Span data_of(const MxView& q) { return span_of(q.data, q.rows * q.row_bytes); }
+Span scales_of(const MxView& q) { return span_of(q.scales, q.rows * q.row_scales); }
 
 // The part of a product's checks and arguments that both entry points share.
 costa_status product_common(int64_t m, int64_t k, const costa_mx* B, const costa_matrix* C, float alpha, float beta,
@@ -253,9 +250,10 @@ costa_status product_common(int64_t m, int64_t k, const costa_mx* B, const costa
   if (C->rows != m || C->cols != B->rows) return fail(COSTA_ERROR_SHAPE_MISMATCH, "C is not the shape of A B^T");
   if (workspace && (uintptr_t)workspace % 16 != 0)
     return fail(COSTA_ERROR_INVALID_VALUE, "the workspace is not 16-byte aligned");
-  if (overlaps(B->data, p.b.rows * p.b.row_bytes, *C) || overlaps(B->scales, p.b.rows * p.b.row_scales, *C))
+  const Span c = span_of(*C);
+  if (spans_meet(data_of(p.b), c) || spans_meet(scales_of(p.b), c))
     return fail(COSTA_ERROR_INVALID_VALUE, "C overlaps B");
-  if (workspace && workspace_bytes <= (size_t)INT64_MAX && overlaps(workspace, (int64_t)workspace_bytes, *C))
+  if (spans_meet(span_of(workspace, (int64_t)std::min(workspace_bytes, (size_t)INT64_MAX)), c))
     return fail(COSTA_ERROR_INVALID_VALUE, "C overlaps the workspace");
   p.m = m;
   p.n = B->rows;
@@ -392,7 +390,7 @@ extern "C" costa_status costa_mx_product(float alpha, const costa_mx* A, const c
     ProductArgs p{};
     CHECKED(check_mx("A", A, p.amx));
     CHECKED(product_common(A->rows, A->cols, B, C, alpha, beta, workspace, workspace_bytes, p));
-    if (overlaps(A->data, p.amx.rows * p.amx.row_bytes, *C) || overlaps(A->scales, p.amx.rows * p.amx.row_scales, *C))
+    if (spans_meet(data_of(p.amx), span_of(*C)) || spans_meet(scales_of(p.amx), span_of(*C)))
       return fail(COSTA_ERROR_INVALID_VALUE, "C overlaps A");
     if (p.m == 0 || p.n == 0) return COSTA_SUCCESS;
     HIP_OR_FAIL(launch_mx_product(p, stream));
@@ -410,7 +408,7 @@ extern "C" costa_status costa_mx_product_real(float alpha, costa_op op, const co
     const bool tr = op != COSTA_OP_N;
     CHECKED(product_common(tr ? A->cols : A->rows, tr ? A->rows : A->cols, B, C, alpha, beta, workspace,
                            workspace_bytes, p));
-    if (overlaps(A->data, matrix_bytes(*A), *C)) return fail(COSTA_ERROR_INVALID_VALUE, "C overlaps A");
+    if (spans_meet(span_of(*A), span_of(*C))) return fail(COSTA_ERROR_INVALID_VALUE, "C overlaps A");
     if (p.m == 0 || p.n == 0) return COSTA_SUCCESS;
     const int64_t rs = A->order == COSTA_ROW_MAJOR ? A->ld : 1, cs = A->order == COSTA_ROW_MAJOR ? 1 : A->ld;
     p.real = A->data;
