@@ -88,9 +88,10 @@ costa_status costa_mx_sizes(costa_mx_format format, int64_t rows, int64_t cols, 
 /* Q <- mx(alpha * B) and QT <- mx(alpha * B^T), either of them or (one read of
  * B) both; the other is NULL.  Q has B's shape, QT the transposed one; their
  * formats may differ.  x = alpha * b: b rounded to a 32-bit float, then the
- * product rounded (alpha == 1: no rounding).  B, Q and QT must not overlap.  Errors: INVALID_VALUE for null
- * or misaligned pointers, unknown types, a leading dimension that is too
- * small, neither Q nor QT; SHAPE_MISMATCH; NOT_SUPPORTED for dimensions above
+ * product rounded (alpha == 1: no rounding).  B, Q and QT must not overlap.
+ * Errors: INVALID_VALUE for null or misaligned pointers, unknown types, a
+ * leading dimension that is too small, operands that overlap, neither Q nor
+ * QT; SHAPE_MISMATCH; NOT_SUPPORTED for dimensions above
  * 2^31 - 1 (as in every call here). */
 costa_status costa_mx_quantize(float alpha, const costa_matrix* B, const costa_mx* Q, const costa_mx* QT,
                                hipStream_t stream);
@@ -98,7 +99,8 @@ costa_status costa_mx_quantize(float alpha, const costa_matrix* B, const costa_m
 /* The same out of the blocks of a distributed matrix: B_local[r] is the buffer
  * of rank r of layout B (as in costa_transform(); a rank that owns nothing may
  * pass NULL), its elements of type `type`.  The blocks of 32 are those of the
- * whole matrix, whatever blocks the layout cuts it into.
+ * whole matrix, whatever blocks the layout cuts it into.  (That B's buffers do
+ * not overlap Q and QT is not checked.)
  * The first call for a layout on a device uploads the layout's tables (device
  * memory, kept until costa_finalize(); the tables of up to 64 layouts, then all
  * of them start over but for those that captured calls read): such a call
@@ -110,7 +112,8 @@ costa_status costa_mx_quantize_layout(costa_real type, float alpha, costa_layout
 
 /* A <- alpha * Q^ + beta * A, Q^ the values that Q stands for, A of the same
  * shape.  In 32 bits (A of type F64: in 64), rounded once to A's type; a
- * product by alpha == 1 or beta == 1 is exact; beta == 0: A is not read. */
+ * product by alpha == 1 or beta == 1 is exact; beta == 0: A is not read.
+ * A must not overlap Q. */
 costa_status costa_mx_dequantize(float alpha, const costa_mx* Q, float beta, const costa_matrix* A,
                                  hipStream_t stream);
 

@@ -2,6 +2,7 @@
 // checks, the tables of distributed layouts, launches.
 #include <algorithm>
 #include <climits>
+#include <initializer_list>
 #include <map>
 #include <memory>
 #include <mutex>
@@ -88,6 +89,24 @@ costa_status check_matrix(const char* what, const costa_matrix* a, bool f64) {
   return COSTA_SUCCESS;
 }
 
+// The memory of a matrix's elements, and of a buffer of `bytes`.
+Span span_of(const costa_matrix& a) {
+  if (a.rows == 0 || a.cols == 0) return Span{0, 0, 0, 0};
+  const int64_t es = real_size(a.type), line = a.order == COSTA_COL_MAJOR ? a.rows : a.cols;
+  return Span{(uintptr_t)a.data, line * es, a.ld * es, a.order == COSTA_COL_MAJOR ? a.cols : a.rows};
+}
+Span span_of(const void* p, int64_t bytes) { return Span{(uintptr_t)p, p ? bytes : 0, bytes, 1}; }
+Span data_of(const MxView& q) { return span_of(q.data, q.rows * q.row_bytes); }
+Span scales_of(const MxView& q) { return span_of(q.scales, q.rows * q.row_scales); }
+
+// INVALID_VALUE where two of the buffers have a byte in common, `what` they are.
+costa_status check_apart(const char* what, std::initializer_list<Span> one, std::initializer_list<Span> other) {
+  for (const Span& x : one)
+    for (const Span& y : other)
+      if (spans_meet(x, y)) return fail(COSTA_ERROR_INVALID_VALUE, what);
+  return COSTA_SUCCESS;
+}
+
 // Q and QT of a rows x cols source; at least one of them.
 costa_status check_outputs(int64_t rows, int64_t cols, const costa_mx* Q, const costa_mx* QT, MxView& q, MxView& qt) {
   if (!Q && !QT) return fail(COSTA_ERROR_INVALID_VALUE, "neither Q nor QT");
@@ -102,7 +121,9 @@ costa_status check_outputs(int64_t rows, int64_t cols, const costa_mx* Q, const 
     if (QT->rows != cols || QT->cols != rows)
       return fail(COSTA_ERROR_SHAPE_MISMATCH, "QT is not the shape of the transposed B");
   }
-  return COSTA_SUCCESS;
+  CHECKED(check_apart("Q overlaps itself", {data_of(q)}, {scales_of(q)}));
+  CHECKED(check_apart("QT overlaps itself", {data_of(qt)}, {scales_of(qt)}));
+  return check_apart("Q overlaps QT", {data_of(q), scales_of(q)}, {data_of(qt), scales_of(qt)});
 }
 
 // ---------------------------------------------------------------------------
@@ -231,18 +252,8 @@ costa_status layout_tables(TableState& T, const Layout& L, hipStream_t stream, M
   return COSTA_SUCCESS;
 }
 
-// The memory of a matrix's elements, and of a buffer of `bytes`.
-Span span_of(const costa_matrix& a) {
-  if (a.rows == 0 || a.cols == 0) return Span{0, 0, 0, 0};
-  const int64_t es = real_size(a.type), line = a.order == COSTA_COL_MAJOR ? a.rows : a.cols;
-  return Span{(uintptr_t)a.data, line * es, a.ld * es, a.order == COSTA_COL_MAJOR ? a.cols : a.rows};
-}
-Span span_of(const void* p, int64_t bytes) { return Span{(uintptr_t)p, p ? bytes : 0, bytes, 1}; }
-Span data_of(const MxView& q) { return span_of(q.data, q.rows * q.row_bytes); }
-Span scales_of(const MxView& q) { return span_of(q.scales, q.rows * q.row_scales); }
-
 // The part of a product's checks and arguments that both entry points share.
-costa_status product_common(int64_t m, int64_t k, const costa_mx* B, const costa_matrix* C, float alpha, float beta,
+costa_status product_common(std::initializer_list<Span> a, int64_t m, int64_t k, const costa_mx* B, const costa_matrix* C, float alpha, float beta,
                             void* workspace, size_t workspace_bytes, ProductArgs& p) {
   CHECKED(check_mx("B", B, p.b));
   CHECKED(check_matrix("C", C, false));
@@ -250,11 +261,12 @@ costa_status product_common(int64_t m, int64_t k, const costa_mx* B, const costa
   if (C->rows != m || C->cols != B->rows) return fail(COSTA_ERROR_SHAPE_MISMATCH, "C is not the shape of A B^T");
   if (workspace && (uintptr_t)workspace % 16 != 0)
     return fail(COSTA_ERROR_INVALID_VALUE, "the workspace is not 16-byte aligned");
-  const Span c = span_of(*C);
-  if (spans_meet(data_of(p.b), c) || spans_meet(scales_of(p.b), c))
-    return fail(COSTA_ERROR_INVALID_VALUE, "C overlaps B");
-  if (spans_meet(span_of(workspace, (int64_t)std::min(workspace_bytes, (size_t)INT64_MAX)), c))
-    return fail(COSTA_ERROR_INVALID_VALUE, "C overlaps the workspace");
+  const Span c = span_of(*C), w = span_of(workspace, (int64_t)std::min(workspace_bytes, (size_t)INT64_MAX));
+  CHECKED(check_apart("C overlaps B", {c}, {data_of(p.b), scales_of(p.b)}));
+  CHECKED(check_apart("C overlaps the workspace", {c}, {w}));
+  CHECKED(check_apart("B overlaps the workspace", {w}, {data_of(p.b), scales_of(p.b)}));
+  CHECKED(check_apart("C overlaps A", {c}, a));
+  CHECKED(check_apart("A overlaps the workspace", {w}, a));
   p.m = m;
   p.n = B->rows;
   p.k = k;
@@ -301,6 +313,8 @@ extern "C" costa_status costa_mx_quantize(float alpha, const costa_matrix* B, co
     QuantArgs a{};
     MxView q, qt;
     CHECKED(check_outputs(B->rows, B->cols, Q, QT, q, qt));
+    CHECKED(check_apart("B overlaps Q", {span_of(*B)}, {data_of(q), scales_of(q)}));
+    CHECKED(check_apart("B overlaps QT", {span_of(*B)}, {data_of(qt), scales_of(qt)}));
     if (B->rows == 0 || B->cols == 0) return COSTA_SUCCESS;
     const bool row = B->order == COSTA_ROW_MAJOR;
     a.lines = row ? B->rows : B->cols;
@@ -371,6 +385,7 @@ extern "C" costa_status costa_mx_dequantize(float alpha, const costa_mx* Q, floa
     CHECKED(check_mx("Q", Q, d.q));
     CHECKED(check_matrix("A", A, true));
     if (A->rows != Q->rows || A->cols != Q->cols) return fail(COSTA_ERROR_SHAPE_MISMATCH, "A is not the shape of Q");
+    CHECKED(check_apart("A overlaps Q", {span_of(*A)}, {data_of(d.q), scales_of(d.q)}));
     if (A->rows == 0 || A->cols == 0) return COSTA_SUCCESS;
     d.dst = A->data;
     d.rs = A->order == COSTA_ROW_MAJOR ? A->ld : 1;
@@ -389,9 +404,8 @@ extern "C" costa_status costa_mx_product(float alpha, const costa_mx* A, const c
   return guarded([&]() -> costa_status {
     ProductArgs p{};
     CHECKED(check_mx("A", A, p.amx));
-    CHECKED(product_common(A->rows, A->cols, B, C, alpha, beta, workspace, workspace_bytes, p));
-    if (spans_meet(data_of(p.amx), span_of(*C)) || spans_meet(scales_of(p.amx), span_of(*C)))
-      return fail(COSTA_ERROR_INVALID_VALUE, "C overlaps A");
+    CHECKED(product_common({data_of(p.amx), scales_of(p.amx)}, A->rows, A->cols, B, C, alpha, beta, workspace,
+                           workspace_bytes, p));
     if (p.m == 0 || p.n == 0) return COSTA_SUCCESS;
     HIP_OR_FAIL(launch_mx_product(p, stream));
     return COSTA_SUCCESS;
@@ -406,9 +420,8 @@ extern "C" costa_status costa_mx_product_real(float alpha, costa_op op, const co
     if (op != COSTA_OP_N && op != COSTA_OP_T && op != COSTA_OP_C) return fail(COSTA_ERROR_INVALID_VALUE, "unknown op");
     CHECKED(check_matrix("A", A, false));
     const bool tr = op != COSTA_OP_N;
-    CHECKED(product_common(tr ? A->cols : A->rows, tr ? A->rows : A->cols, B, C, alpha, beta, workspace,
+    CHECKED(product_common({span_of(*A)}, tr ? A->cols : A->rows, tr ? A->rows : A->cols, B, C, alpha, beta, workspace,
                            workspace_bytes, p));
-    if (spans_meet(span_of(*A), span_of(*C))) return fail(COSTA_ERROR_INVALID_VALUE, "C overlaps A");
     if (p.m == 0 || p.n == 0) return COSTA_SUCCESS;
     const int64_t rs = A->order == COSTA_ROW_MAJOR ? A->ld : 1, cs = A->order == COSTA_ROW_MAJOR ? 1 : A->ld;
     p.real = A->data;

@@ -92,3 +92,55 @@ def test_long_lines_far_apart(standin):
     b.data = FAR  # where a row of C begins
     assert status_of(S, a, M(1, ROW, m, 4, big, BASE + 32), b) == S.C.INVALID_VALUE
     assert S.C.costa_last_error() == "C overlaps B"
+
+
+def test_every_pair_of_operands_is_checked(standin):
+    """Each buffer of a call laid over each other one that the call may not share it with."""
+    S = standin
+    C, M, bad = S.C, S.C.CostaMatrix, S.C.INVALID_VALUE
+
+    def mx(fmt, rows, cols, at):
+        return C.CostaMx(fmt, rows, cols, at, at + (1 << 20))
+
+    def message(what, status):
+        S.faults()
+        S.lib.standin_tile_launches(None, 0)
+        assert status == bad and "overlap" in C.costa_last_error(), (what, status, C.costa_last_error())
+
+    # quantise: B, Q and QT, each with two buffers of the few-bit ones
+    for what in ("B Q.data", "B Q.scales", "B QT.data", "B QT.scales", "Q.data QT.data", "Q.data QT.scales",
+                 "Q.scales QT.data", "Q.scales QT.scales", "Q.data Q.scales", "QT.data QT.scales"):
+        held = {"B": M(1, ROW, 40, 70, 70, BASE), "Q": mx(0, 40, 70, 2 * BASE), "QT": mx(1, 70, 40, 3 * BASE)}
+        assert C._lib.costa_mx_quantize(1.0, *map(ref, held.values()), None) == C.SUCCESS
+        one, two = what.split()
+        at = held["B"].data if one == "B" else getattr(held[one.split(".")[0]], one.split(".")[1])
+        name, field = two.split(".")
+        setattr(held[name], field, at + 16)
+        message(what, C._lib.costa_mx_quantize(1.0, *map(ref, held.values()), None))
+    for field in ("data", "scales"):
+        q = mx(1, 40, 70, 2 * BASE)
+        assert C._lib.costa_mx_dequantize(1.0, ref(q), 0.0, ref(M(1, ROW, 40, 70, 70, BASE)), None) == C.SUCCESS
+        message(field, C._lib.costa_mx_dequantize(1.0, ref(q), 0.0, ref(M(1, ROW, 40, 70, 70, getattr(q, field))), None))
+    # products: the workspace
+    a, b, few, c = M(1, ROW, 5, 64, 64, BASE), mx(0, 9, 64, 2 * BASE), mx(1, 5, 64, 3 * BASE), M(1, ROW, 5, 9, 9, 4 * BASE)
+    for at in (5 * BASE, a.data, b.data, b.scales, c.data):
+        st = C._lib.costa_mx_product_real(1.0, 0, ref(a), ref(b), 0.0, ref(c), at, 64, None)
+        if at == 5 * BASE:
+            assert st == C.SUCCESS
+        else:
+            message(at, st)
+    for at in (few.data, few.scales):
+        message(at, C._lib.costa_mx_product(1.0, ref(few), ref(b), 0.0, ref(c), at, 64, None))
+    S.faults()
+
+
+def test_a_row_of_a_store_in_the_gaps_of_a_matrix(standin):
+    """What lies between a strided matrix's lines is not the matrix's."""
+    S = standin
+    C = S.C
+    b = C.CostaMatrix(1, ROW, 1, 40, 4096, BASE)
+    for rows, at, want in ((1, 160, C.SUCCESS), (1, 144, C.INVALID_VALUE), (2, 160, C.SUCCESS), (2, 16384 - 112, C.INVALID_VALUE)):
+        b.rows = rows
+        q = C.CostaMx(0, rows, 40, BASE + at, FAR)
+        assert C._lib.costa_mx_quantize(1.0, ref(b), ref(q), None, None) == want, (rows, at)
+    S.faults()
