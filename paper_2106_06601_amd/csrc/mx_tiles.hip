@@ -380,7 +380,7 @@ struct CodeStage {
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                    :
                    : "s"(to), "v"(offset[c]), "s"(from)
-                   : "memory");
+                   : "m0", "memory");
     }
   }
 };
