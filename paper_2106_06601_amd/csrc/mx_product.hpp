@@ -2,13 +2,10 @@
 #pragma once
 
 #include "mx_device.hpp"
+#include "mx_plan.hpp"
 
 namespace costa {
 
-// Kinds of left operands.
-enum Source : int { SRC_MX4, SRC_MX8, SRC_BF16, SRC_F16, SRC_F32 };
-// bfloat16 parts that hold an element of each.
-constexpr int parts_of(int src) { return src == SRC_F32 ? 3 : src == SRC_F16 ? 2 : 1; }
 constexpr int bytes_of(int src) { return src == SRC_F32 ? 4 : 2; }  // of plain elements
 
 // Where the sums go: C, or a part's place in the workspace.
@@ -169,13 +166,6 @@ __device__ inline v4f mfma_bf16(v4u a, v4u b, v4f c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
 }
 
-// How a product runs; a function of sizes and types alone.
-enum Variant : int { FEW_ROWS, TILES_BF16, TILES_SCALED, THIN };
-struct ProductPlan {
-  Variant variant;
-  int bm, bn;   // tile of C (rows, columns)
-  int splits;   // workgroups that share a tile's sum
-};
 hipError_t launch_tiles_bf16(int src, const Args& p, const ProductPlan& plan, hipStream_t stream);
 hipError_t launch_tiles_scaled(const Args& p, const ProductPlan& plan, hipStream_t stream);
 

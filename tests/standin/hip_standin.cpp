@@ -27,6 +27,7 @@
 
 #include "../../paper_2106_06601_amd/csrc/index_math.hpp"
 #include "../../paper_2106_06601_amd/csrc/mx.hpp"
+#include "../../paper_2106_06601_amd/csrc/mx_plan.hpp"
 
 using namespace costa;
 
@@ -258,6 +259,11 @@ int standin_tile_launches(uint32_t* out, int most) {
   if (n <= most && n) std::memcpy(out, tile_launches.data(), n * sizeof(TileLaunch));
   tile_launches.clear();
   return n;
+}
+// The rule of products: variant, bm, bn, splits.
+void standin_plan(int src, int k_next, int bbits, int64_t m, int64_t n, int64_t k, int32_t* out) {
+  const ProductPlan p = plan_product(src, k_next != 0, bbits, m, n, k);
+  out[0] = p.variant, out[1] = p.bm, out[2] = p.bn, out[3] = p.splits;
 }
 void standin_xcd_tiles(uint32_t nm, uint32_t nn, uint32_t first, uint32_t n, uint32_t b0, uint32_t count, uint32_t* tm,
                        uint32_t* tn) {
