@@ -310,8 +310,10 @@ __global__ __launch_bounds__(256) void join_parts(Epilogue e, const float* parts
   }
 }
 
-// C <- beta * C: a sum over nothing.
+// C <- beta * C: a sum over nothing.  (alpha times it would be NaN for an alpha that is
+// not finite, and -0 for a negative one.)
 __global__ __launch_bounds__(256) void scale_only(Epilogue e, int64_t m, int64_t n) {
+  e.alpha = 1.0f;
   for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < m * n; u += (int64_t)gridDim.x * 256)
     put_four(e, u / n, u % n, v4f{0, 0, 0, 0}, 1);
 }
