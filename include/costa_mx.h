@@ -24,6 +24,9 @@
  * where mx(X^T) in 8 bits is the activation's checkpoint: the blocks run along
  * the tokens, the direction the gradient sums over.  One quantise call writes
  * mx(B) and mx(B^T).  Quantisation passes gradients through unchanged.
+ * (mx(W^T) is rounded in blocks along the outputs, mx(W) in blocks along the
+ * inputs: dX is the derivative of a layer with the former's weights, off that of
+ * Y by what the two roundings differ by.)
  *
  * Conventions are those of costa.h: every call returns a costa_status, details
  * from costa_last_error(); calls are asynchronous on `stream`, on the current
