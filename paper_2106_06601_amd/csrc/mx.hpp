@@ -83,7 +83,7 @@ struct DequantArgs {
 };
 hipError_t launch_mx_dequantize(const DequantArgs& a, hipStream_t stream);
 
-// ---- products (mx_product.hip) -------------------------------------------------
+// ---- products (mx_plan.hpp, mx_product.hip, mx_tiles.hip) -------------------------------------------------
 // C (m x n) <- alpha * A B^T + beta * C over k; A microscaled (mx.data set) or
 // plain with element (i, l) at real[i*rs + l*cs].
 struct ProductArgs {
@@ -104,7 +104,7 @@ size_t mx_product_workspace(int64_t m, int64_t n, int64_t k);
 hipError_t launch_mx_product(const ProductArgs& a, hipStream_t stream);
 
 // ---- entry points (mx.cpp) -------------------------------------------------------
-// Frees the layout tables (called by costa_finalize, which has waited for the device).
+// Frees the layout tables (called by costa_finalize); waits for the kernels that read them.
 void release_mx_tables();
 
 }  // namespace costa

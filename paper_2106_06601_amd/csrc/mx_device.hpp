@@ -17,26 +17,6 @@ typedef short v2s __attribute__((ext_vector_type(2)));
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 
-// Element types of plain matrices by their costa_real value.
-template <int TYPE>
-struct Real;
-template <>
-struct Real<COSTA_REAL_F64> {
-  typedef double T;
-};
-template <>
-struct Real<COSTA_REAL_F32> {
-  typedef float T;
-};
-template <>
-struct Real<COSTA_REAL_BF16> {
-  typedef __bf16 T;
-};
-template <>
-struct Real<COSTA_REAL_F16> {
-  typedef _Float16 T;
-};
-
 // The scale byte of a block from the bits of its largest magnitude.  Integers
 // order the bits as the magnitudes, NaN above infinity above the finite ones.
 template <int BITS>

@@ -35,7 +35,11 @@ inline int64_t splits_max(int64_t m, int64_t n) {
 // share): bfloat16, k by 64: 1.77 us for a 256x256 tile (one a CU), 0.57 a tile for
 // several of 128x128, 0.39 of 128x64, not below 0.66 (the way from memory through
 // shared memory); 4 bits, k by 256: 2.6 us at 256x256, 0.76 at 128x128, not below 1.0.
-// Joining a split sum costs a launch and its parts' way to memory and back.
+// Joining a split sum costs a launch and its parts' way to memory and back.  (It ranks
+// tiles and splits of one call; as a time it holds for bfloat16 rows with k next to one
+// another and for 4 bits.  A transposed float operand's step takes about twice as long: 35 us
+// estimated, 66 measured for 100x64 over 524288; with an 8-bit operand, 29 and 31 to 38 for
+// 1041x1999x2501.)
 // (512x8192x8192 in bfloat16: 128x128 unsplit 88 us, 256x256 unsplit 232, split in four 86;
 // 256x8192x8192: 128x128 split in four 53, 128x64 unsplit 72; 1024^3: 128x64 13, 128x128 17.)
 inline double tiled_time(bool scaled, int parts, int64_t bm, int64_t bn, int64_t splits, int64_t m, int64_t n, int64_t k) {

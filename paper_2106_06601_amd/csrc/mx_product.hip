@@ -19,10 +19,12 @@ namespace {
 // shared memory of its own.  (Read in that order straight from memory, a load
 // touches 64 pieces of 16 bytes, and the left operand costs more than B.)  The next piece of
 // B and the next slab are on their way meanwhile.  The waves' sums are joined
-// through shared memory, pairwise, in a fixed order.  Measured, B in 4 bits: one row
-// of bfloat16 by 8192x8192 13 us (35.7 MB of B, 2.7 TB/s; a launch and the first loads
-// take about 5 us of any call, past them B comes at 4.5 TB/s), 13 rows of float16 by 20000x4095
-// 24 us, 64 rows of bfloat16 by 8192x8192 40 us, of float 91 (three parts).
+// through shared memory, pairwise, in a fixed order.  Measured, B in 4 bits, out of
+// memory (32 matrices in turn) and, the same one again and again, out of the last-level
+// cache: one row of bfloat16 by 8192x8192 (35.7 MB of B) 15.7 us, 2.3 TB/s, and 12.5
+// us, 2.9 TB/s (a launch and the first loads take about 5 us of any call); 13 rows of
+// float16 by 20000x4095 26.6 and 24.0 us; 64 rows of bfloat16 by 8192x8192 38 and 35
+// us, of float 91 cached (three parts).
 constexpr int kSlab = 128;
 
 // A slab: lane l has, of rows l / 16 + 4 q, the eight elements 8 (l % 16) ..

@@ -1,9 +1,10 @@
 // Products of microscaled matrices in tiles of C, with both operands staged in
 // shared memory.
 //
-// Both kernels run 8 waves on a tile and keep two stages of k: while the matrix
-// instructions work on one, the next one's loads are on their way to registers;
-// they are then written to the other stage, one barrier a step.  The operands
+// Both kernels run 8 waves on a tile and keep two stages of k, one barrier a step:
+// while the matrix instructions work on one stage, the next one's loads are on
+// their way, to registers (and are then written to the other stage) or, where both
+// operands are in 4 bits, straight to the other stage.  The operands
 // of a matrix instruction are passed with B first: lane l then ends up with row
 // l % 16 of C and four neighbouring columns, which makes wide stores.
 #include <algorithm>

@@ -28,7 +28,7 @@ sys.path[:0] = [{tests!r}, {root!r}]
 import standin
 standin.build = lambda: {lib!r}
 import pytest
-sys.exit(pytest.main([*{modules!r}, "-q", "-x", "-p", "no:cacheprovider", "-k", "not plain_c and not all_sizes"]))
+sys.exit(pytest.main([*{modules!r}, "-q", "-x", "-p", "no:cacheprovider", "-k", "not plain_c"]))
 """
 
 
