@@ -28,26 +28,6 @@ COSTA_BOTH int32_t xcd_order(int32_t b, int32_t n, int32_t run) {
   return start + idx;
 }
 
-// The tiles of a matrix, nm rows of nn of them (below 2^31 in all), of which a launch
-// takes those from `first` on, as many as it has workgroups.
-struct TileRange {
-  uint32_t nm, nn, first;
-};
-constexpr int64_t kTilesMax = INT32_MAX;
-constexpr int64_t kTileSlice = (int64_t)1 << 22;  // workgroups of a launch: below 2^32 lanes
-
-// Tile (tm, tn) of workgroup b of a launch of n.  Workgroups go round the 8 XCDs in
-// turn; each XCD gets a run of neighbouring tiles (8 tile rows wide, by columns), whose
-// operands its L2 holds.
-COSTA_BOTH void xcd_tile(uint32_t b, uint32_t n, const TileRange& r, uint32_t& tm, uint32_t& tn) {
-  const uint32_t per = n / 8, more = n % 8, x = b % 8;
-  const uint32_t t = r.first + x * per + (x < more ? x : more) + b / 8;
-  const uint32_t group = t / (8 * r.nn), left = r.nm - group * 8, rows = left < 8u ? left : 8u;
-  const uint32_t in = t - group * 8 * r.nn;
-  tm = group * 8 + in % rows;
-  tn = in / rows;
-}
-
 // 1 / x to within one ulp: the hardware's estimate; on the host, where tests run
 // this code, the quotient moved by `reciprocal_ulps`.
 #if !defined(__HIP_DEVICE_COMPILE__)

@@ -9,7 +9,6 @@
 // l % 16 of C and four neighbouring columns, which makes wide stores.
 #include <algorithm>
 
-#include "index_math.hpp"
 #include "mx_product.hpp"
 
 namespace costa {
@@ -18,13 +17,16 @@ namespace {
 constexpr int kWaves = 8;
 constexpr int kLanes = 64 * kWaves;
 
-// This workgroup's tile.
-__device__ inline void my_tile(const TileRange& r, int64_t& tm, int64_t& tn) {
-  uint32_t m, n;
-  xcd_tile(blockIdx.x, gridDim.x, r, m, n);
+// Tile (tm, tn) of workgroup b of a launch over nm x nn tiles.  Workgroups go
+// round the 8 XCDs in turn; each XCD gets a run of neighbouring tiles (8 tile
+// rows wide, by columns), whose operands its L2 holds.
+__device__ inline void tile_of(uint32_t b, uint32_t nm, uint32_t nn, int64_t& tm, int64_t& tn) {
+  const uint32_t total = nm * nn, per = total / 8, more = total % 8, x = b % 8;
+  const uint32_t t = x * per + min(x, more) + b / 8;
+  const uint32_t group = t / (8 * nn), rows = min(8u, nm - group * 8), in = t - group * 8 * nn;
   // (the division runs on vector registers: both are the wave's, not a lane's)
-  tm = __builtin_amdgcn_readfirstlane(m);
-  tn = __builtin_amdgcn_readfirstlane(n);
+  tm = __builtin_amdgcn_readfirstlane(group * 8 + in % rows);
+  tn = __builtin_amdgcn_readfirstlane(in / rows);
 }
 
 // Part y of `parts` of a sum's steps.
@@ -263,7 +265,7 @@ struct RightStage {
 
 // AHEAD: steps whose loads are on their way at once.
 template <int SRC, bool TRANS, int BBITS, int BM, int BN, int WM, int AHEAD, bool EDGE>
-__global__ __launch_bounds__(kLanes) void tiles_bf16(Args p, TileRange range) {
+__global__ __launch_bounds__(kLanes) void tiles_bf16(Args p, uint32_t nm, uint32_t nn) {
   constexpr int WN = kWaves / WM, MT = BM / WM / 16, NT = BN / WN / 16, P = parts_of(SRC);
   constexpr int BROW = kStepBf16 * BBITS / 8;
   __shared__ v4u left[2][P * BM * 8];
@@ -272,7 +274,7 @@ __global__ __launch_bounds__(kLanes) void tiles_bf16(Args p, TileRange range) {
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, g = lane / 16;
   const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
   int64_t tm, tn;
-  my_tile(range, tm, tn);
+  tile_of(blockIdx.x, nm, nn, tm, tn);
   const int64_t i0 = tm * BM, j0 = tn * BN;
   int64_t first, last;
   steps_of((uint32_t)((p.k + kStepBf16 - 1) / kStepBf16), blockIdx.y, gridDim.y, first, last);
@@ -392,7 +394,7 @@ __device__ inline v8i operand4(v4u d) {  // the instruction reads four of the ei
 }
 
 template <int BM, int BN, int WM>
-__global__ __launch_bounds__(kLanes) void tiles_scaled(Args p, TileRange range) {
+__global__ __launch_bounds__(kLanes) void tiles_scaled(Args p, uint32_t nm, uint32_t nn) {
   constexpr int WN = kWaves / WM, MT = BM / WM / 16, NT = BN / WN / 16;
   __shared__ v4u left[2][BM * kRowChunks];
   __shared__ v4u right[2][BN * kRowChunks];
@@ -400,7 +402,7 @@ __global__ __launch_bounds__(kLanes) void tiles_scaled(Args p, TileRange range) 
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, g = lane / 16;
   const int wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
   int64_t tm, tn;
-  my_tile(range, tm, tn);
+  tile_of(blockIdx.x, nm, nn, tm, tn);
   const int64_t i0 = tm * BM, j0 = tn * BN;
   int64_t first, last;
   steps_of((uint32_t)((p.k + kStep4 - 1) / kStep4), blockIdx.y, gridDim.y, first, last);
@@ -470,18 +472,36 @@ __global__ __launch_bounds__(kLanes) void tiles_scaled(Args p, TileRange range) 
   put_wave<MT, NT>(p, acc, &left[0][0], wave, i0 + wm, j0 + wn);
 }
 
-// Launches the tiles of C in slices that a grid holds.
+constexpr int64_t kTilesMax = INT32_MAX;
+constexpr int64_t kTileSlice = (int64_t)1 << 22;  // workgroups of a launch: below 2^32 lanes
+
+// Launches the tiles of C, in slices of whole rows or columns of tiles where a grid does
+// not hold them all: each a product of its own.  (The kernels take no part in this: an
+// offset among their arguments changed how the compiler ordered one of them, 1041x1999x2501
+// of 8 by 4 bits 43.0 us without, 45.3 with.)
 template <typename F>
-hipError_t launch_slices(const Args& p, const ProductPlan& plan, F launch) {
+hipError_t launch_slices(const Args& p, const ProductPlan& plan, int elem_bytes, F launch) {
   const int64_t nm = (p.m + plan.bm - 1) / plan.bm, nn = (p.n + plan.bn - 1) / plan.bn;
   // (a C of 16 TiB and more: either dimension is below 2^31)
   if (nm * nn > kTilesMax) throw LimitExceeded("a product of more than 2^31 - 1 tiles");
-  for (int64_t first = 0; first < nm * nn; first += kTileSlice) {
-    launch(dim3((unsigned)std::min(kTileSlice, nm * nn - first), plan.splits),
-           TileRange{(uint32_t)nm, (uint32_t)nn, (uint32_t)first});
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
+  const int64_t cols = std::min(nn, kTileSlice), rows = std::min(nm, kTileSlice / cols);
+  for (int64_t tm = 0; tm < nm; tm += rows)
+    for (int64_t tn = 0; tn < nn; tn += cols) {
+      const int64_t i = tm * plan.bm, j = tn * plan.bn;
+      Args q = p;
+      q.m = q.a.rows = std::min(rows * plan.bm, p.m - i);
+      q.n = q.b.rows = std::min(cols * plan.bn, p.n - j);
+      if (p.real) q.real = static_cast<const char*>(p.real) + i * p.a_rs * elem_bytes;
+      q.a.data += i * p.a.row_bytes;
+      q.a.scales += i * p.a.row_scales;
+      q.b.data += j * p.b.row_bytes;
+      q.b.scales += j * p.b.row_scales;
+      q.e.c = static_cast<char*>(p.e.c) + (i * p.e.rs + j * p.e.cs) * (p.e.type == COSTA_REAL_F32 ? 4 : 2);
+      const uint32_t tall = (uint32_t)std::min(rows, nm - tm), wide = (uint32_t)std::min(cols, nn - tn);
+      launch(dim3(tall * wide, plan.splits), q, tall, wide);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
   return hipSuccess;
 }
 
@@ -491,22 +511,22 @@ hipError_t launch_bf16(const Args& p, const ProductPlan& plan, hipStream_t strea
   const bool wide = plan.bm == BM && plan.bn == 256;
   if (!wide && (plan.bm != 128 || (plan.bn != 128 && plan.bn != 64)))
     return hipErrorInvalidValue;  // not a tile of this kernel
-  return launch_slices(p, plan, [&](dim3 grid, TileRange range) {
+  return launch_slices(p, plan, bytes_of(SRC), [&](dim3 grid, const Args& q, uint32_t nm, uint32_t nn) {
     if (wide) {
       // (transposed operands: a kernel of its own where every lane has all of its rows or none.
       // 4096x4096 over 16384 in bfloat16 takes 470 us, with the other kernel 511; 803x236 over 66454 takes 77 us with
       // the other one, with its last lane's rows one by one 96)
       if constexpr (TRANS) {
-        if (p.m % (BM / 64) == 0) {
-          tiles_bf16<SRC, TRANS, BBITS, BM, 256, 2, 1, false><<<grid, kLanes, 0, stream>>>(p, range);
+        if (q.m % (BM / 64) == 0) {
+          tiles_bf16<SRC, TRANS, BBITS, BM, 256, 2, 1, false><<<grid, kLanes, 0, stream>>>(q, nm, nn);
           return;
         }
       }
-      tiles_bf16<SRC, TRANS, BBITS, BM, 256, 2, 1, true><<<grid, kLanes, 0, stream>>>(p, range);
+      tiles_bf16<SRC, TRANS, BBITS, BM, 256, 2, 1, true><<<grid, kLanes, 0, stream>>>(q, nm, nn);
     } else if (plan.bn == 128) {
-      tiles_bf16<SRC, TRANS, BBITS, 128, 128, 2, 1, true><<<grid, kLanes, 0, stream>>>(p, range);
+      tiles_bf16<SRC, TRANS, BBITS, 128, 128, 2, 1, true><<<grid, kLanes, 0, stream>>>(q, nm, nn);
     } else {
-      tiles_bf16<SRC, TRANS, BBITS, 128, 64, 4, 2, true><<<grid, kLanes, 0, stream>>>(p, range);
+      tiles_bf16<SRC, TRANS, BBITS, 128, 64, 4, 2, true><<<grid, kLanes, 0, stream>>>(q, nm, nn);
     }
   });
 }
@@ -534,9 +554,9 @@ hipError_t launch_tiles_bf16(int src, const Args& p, const ProductPlan& plan, hi
 hipError_t launch_tiles_scaled(const Args& p, const ProductPlan& plan, hipStream_t stream) {
   const bool wide = plan.bm == 256 && plan.bn == 256;
   if (!wide && (plan.bm != 128 || plan.bn != 128)) return hipErrorInvalidValue;  // not a tile of this kernel
-  return launch_slices(p, plan, [&](dim3 grid, TileRange range) {
-    if (wide) tiles_scaled<256, 256, 2><<<grid, kLanes, 0, stream>>>(p, range);
-    else tiles_scaled<128, 128, 2><<<grid, kLanes, 0, stream>>>(p, range);
+  return launch_slices(p, plan, 0, [&](dim3 grid, const Args& q, uint32_t nm, uint32_t nn) {
+    if (wide) tiles_scaled<256, 256, 2><<<grid, kLanes, 0, stream>>>(q, nm, nn);
+    else tiles_scaled<128, 128, 2><<<grid, kLanes, 0, stream>>>(q, nm, nn);
   });
 }
 

@@ -27,7 +27,7 @@
 
 #include "../../paper_2106_06601_amd/csrc/index_math.hpp"
 #include "../../paper_2106_06601_amd/csrc/mx.hpp"
-#include "../../paper_2106_06601_amd/csrc/mx_plan.hpp"
+#include "../../paper_2106_06601_amd/csrc/mx_product.hpp"
 
 using namespace costa;
 
@@ -64,8 +64,8 @@ std::string faults;
 hipError_t last = hipSuccess;
 bool implicit_refused = false;  // a blocking stream captures: the null stream reports it
 struct TileLaunch {
-  TileRange range;
-  uint32_t tiles, splits;
+  int64_t m, n, nm, nn, tiles, splits;
+  int64_t a, b, b_scales, c;  // where each operand begins
 };
 std::vector<TileLaunch> tile_launches;  // of products
 void (*before_launch)() = nullptr;  // a test's, called once, by a launch before it is enqueued
@@ -253,8 +253,8 @@ void standin_tile_walk(int32_t lanes, int32_t tid, int32_t len, int64_t ld, int3
   if (lanes == kSmallTileLanes) walk(TileWalk<kSmallTileLanes>(tid, len, ld, ls, lc));
   else walk(TileWalk<kThreadsPerTask>(tid, len, ld, ls, lc));
 }
-// The launches of product tiles since the last call: nm, nn, first, tiles, splits of each.
-int standin_tile_launches(uint32_t* out, int most) {
+// The launches of product tiles since the last call.
+int standin_tile_launches(int64_t* out, int most) {
   const int n = (int)tile_launches.size();
   if (n <= most && n) std::memcpy(out, tile_launches.data(), n * sizeof(TileLaunch));
   tile_launches.clear();
@@ -264,10 +264,6 @@ int standin_tile_launches(uint32_t* out, int most) {
 void standin_plan(int src, int k_next, int bbits, int64_t m, int64_t n, int64_t k, int32_t* out) {
   const ProductPlan p = plan_product(src, k_next != 0, bbits, m, n, k);
   out[0] = p.variant, out[1] = p.bm, out[2] = p.bn, out[3] = p.splits;
-}
-void standin_xcd_tiles(uint32_t nm, uint32_t nn, uint32_t first, uint32_t n, uint32_t b0, uint32_t count, uint32_t* tm,
-                       uint32_t* tn) {
-  for (uint32_t k = 0; k < count; ++k) xcd_tile(b0 + k, n, TileRange{nm, nn, first}, tm[k], tn[k]);
 }
 void standin_before_launch(void (*f)()) { before_launch = f; }
 void standin_refuse_implicit(int on) { implicit_refused = on != 0; }
@@ -479,7 +475,10 @@ hipError_t hipLaunchKernel(const void* f, dim3 grid, dim3, void** args, size_t, 
           fault("a layout's splits that are gone");
     });
   } else if (name.find("tiles_bf16") != std::string::npos || name.find("tiles_scaled") != std::string::npos) {
-    tile_launches.push_back({arg<TileRange>(args, 1), grid.x, grid.y});  // (not run)
+    const Args p = arg<Args>(args, 0);  // (not run)
+    tile_launches.push_back({p.m, p.n, arg<uint32_t>(args, 1), arg<uint32_t>(args, 2), grid.x, grid.y,
+                             (int64_t)(p.real ? (uintptr_t)p.real : (uintptr_t)p.a.data), (int64_t)(uintptr_t)p.b.data,
+                             (int64_t)(uintptr_t)p.b.scales, (int64_t)(uintptr_t)p.e.c});
   } else {
     fault("a kernel that the stand-in does not run: " + name);
   }
