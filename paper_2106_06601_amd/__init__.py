@@ -593,6 +593,9 @@ def costa_mx_quantize(alpha: float, B, Q: Optional[MxMatrix] = None, QT: Optiona
 def costa_mx_quantize_layout(type: str, alpha: float, B, B_local: Sequence, Q: Optional[MxMatrix] = None,
                              QT: Optional[MxMatrix] = None, stream=None) -> None:
     """The same out of the ranks' buffers of layout B; type: "f64", "f32", "bf16" or "f16"."""
+    P = B.nranks if isinstance(B, Layout) else costa_layout_info(_h(B))["nranks"]
+    if len(B_local) < P:
+        raise ValueError(f"{len(B_local)} buffers for a layout of {P} ranks")
     keep: List = []
     _check(_lib.costa_mx_quantize_layout(REALS[type], alpha, _h(B), _pointers(B_local, keep), _mx(Q), _mx(QT),
                                          _stream(stream)), "costa_mx_quantize_layout")

@@ -56,3 +56,14 @@ def test_a_product_without_split_takes_nothing(pools):
     assert C.costa_mx_workspace(5, 7, 1) == 0
     assert C._product_workspace(5, 7, 1, None, "cuda", 0x2000) == (None, 0, None)
     assert pools.taken == []
+
+
+def test_a_buffer_for_every_rank_is_asked_for():
+    """The library reads an address for each rank of the layout."""
+    L = C.Layout.block_cyclic(8, 6, 2, 2, 2, 2)
+    for layout in (L, L.handle):
+        for bufs in ([], [1 << 20], [1 << 20] * 3):
+            with pytest.raises(ValueError, match="buffers"):
+                C.costa_mx_quantize_layout("f32", 1.0, layout, bufs)
+        with pytest.raises(C.CostaError):  # neither Q nor QT
+            C.costa_mx_quantize_layout("f32", 1.0, layout, [1 << 20] * 4)
