@@ -1,7 +1,7 @@
 """Python binding of the MI355X layout-transform library (``libcosta_mi355x.so``).
 
 Argument marshalling only: every function calls the C ABI of
-``include/costa.h`` with the same name; all work runs in the library's HIP
+``include/costa.h`` (costa_mx.h, costa_layer.h) with the same name; all work runs in the library's HIP
 kernels and host planner.  Device buffers are passed as ``torch`` tensors (or
 raw integer addresses); torch is used for nothing else, except that it is
 imported before the library so that the process holds a single HIP runtime.
@@ -86,6 +86,11 @@ class CostaMx(ctypes.Structure):
     _fields_ = [("format", ctypes.c_int), ("rows", _i64), ("cols", _i64), ("data", _vp), ("scales", _vp)]
 
 
+class CostaMxAdapters(ctypes.Structure):
+    _fields_ = [("count", _i32), ("rank", _i32), ("A", _P(CostaMatrix)), ("B", _P(CostaMatrix)), ("ranks", _vp),
+                ("scales", _vp)]
+
+
 _SIGS = {
     "costa_layout_create": [_i64, _i64, _i32, _vp, _i32, _vp, _vp, _i32, ctypes.c_int, _vp, _vp, _P(_vp)],
     "costa_layout_create_block_cyclic": [_i64, _i64, _i64, _i64, _i32, _i32, ctypes.c_int, ctypes.c_int, _P(_vp)],
@@ -129,6 +134,9 @@ _SIGS = {
     "costa_mx_product_real": [ctypes.c_float, ctypes.c_int, _P(CostaMatrix), _P(CostaMx), ctypes.c_float,
                               _P(CostaMatrix), _vp, ctypes.c_size_t, _vp],
     "costa_mx_workspace": [_i64, _i64, _i64, _P(ctypes.c_size_t)],
+    "costa_mx_norm": [ctypes.c_float, *[_P(CostaMatrix)] * 5, _P(CostaMx), _vp, _vp],
+    "costa_mx_norm_backward": [*[_P(CostaMatrix)] * 3, _vp, *[_P(CostaMatrix)] * 3, _vp, ctypes.c_size_t, _vp],
+    "costa_mx_norm_workspace": [_i64, _i64, _P(ctypes.c_size_t), _P(ctypes.c_size_t)],
 }
 for _name, _args in _SIGS.items():
     _f = getattr(_lib, _name)
@@ -613,13 +621,12 @@ def costa_mx_workspace(m: int, n: int, k: int) -> int:
     return b.value
 
 
-def _product_workspace(m: int, n: int, k: int, workspace, device, stream):
-    """(address, bytes, tensor to keep until the call returns) of a product's
-    workspace: the caller's uint8 tensor, or one from torch's allocator.  That
+def _workspace(n: int, workspace, device, stream):
+    """(address, bytes, tensor to keep until the call returns) of a workspace of n
+    bytes: the caller's uint8 tensor, or one from torch's allocator.  That
     one comes from the pool of the stream that the call runs on: a block of
     another stream's may still have work of that stream queued on it."""
     if workspace is None:
-        n = costa_mx_workspace(m, n, k)
         if n == 0:
             return None, 0, None
         at = None if stream is None else _stream(stream)
@@ -631,6 +638,11 @@ def _product_workspace(m: int, n: int, k: int, workspace, device, stream):
     elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or not workspace.is_cuda:
         raise ValueError("workspace: a contiguous uint8 tensor on the GPU is needed")
     return workspace.data_ptr() or None, workspace.numel(), workspace
+
+
+def _product_workspace(m: int, n: int, k: int, workspace, device, stream):
+    """_workspace() of a product."""
+    return _workspace(costa_mx_workspace(m, n, k) if workspace is None else 0, workspace, device, stream)
 
 
 def costa_mx_product(alpha: float, A: MxMatrix, B: MxMatrix, beta: float, C, workspace=None, stream=None) -> None:
@@ -648,6 +660,60 @@ def costa_mx_product_real(alpha: float, op: str, A, B: MxMatrix, beta: float, C,
     at, size, _keep = _product_workspace(m, B.rows, k, workspace, C.device, stream)
     _check(_lib.costa_mx_product_real(alpha, OPS[op], _matrix(A), _mx(B), beta, _matrix(C), at, size,
                                       _stream(stream)), "costa_mx_product_real")
+
+
+# ---------------------------------------------------------------------------
+# the operators around products (include/costa_layer.h)
+# ---------------------------------------------------------------------------
+def _opt(t):
+    return None if t is None else _matrix(t)
+
+
+def _line(t):
+    """A vector as a matrix of one row."""
+    if t is None:
+        return None
+    if t.dim() != 1 or not t.is_contiguous():
+        raise ValueError("a contiguous 1-D tensor is needed")
+    return _matrix(t.view(1, -1))
+
+
+def _vector(t, dtype, n, what: str):
+    """The address of a contiguous vector of n elements on the GPU."""
+    if t is None:
+        return None
+    if t.dtype != dtype or not t.is_contiguous() or not t.is_cuda or t.numel() != n:
+        raise ValueError(f"{what}: {n} contiguous elements of {dtype} on the GPU are needed")
+    return t.data_ptr() or None
+
+
+def costa_mx_norm(eps: float, X, W=None, R=None, H=None, Y=None, Q: Optional[MxMatrix] = None, rstd=None,
+                  stream=None) -> None:
+    """h = X + R, s = 1 / sqrt(mean(h^2) + eps) of each row, y = h s W: H <- h, Y <- y,
+    Q <- mx(y), rstd <- s, those that are given.  2-D tensors; W a vector, rstd one of floats."""
+    _check(_lib.costa_mx_norm(eps, _matrix(X), _line(W), _opt(R), _opt(H), _opt(Y), _mx(Q),
+                              _vector(rstd, torch.float32, X.shape[0], "rstd"), _stream(stream)), "costa_mx_norm")
+
+
+@functools.lru_cache(maxsize=4096)
+def _two_sizes(name: str, *sizes):
+    least, most = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(getattr(_lib, name)(*sizes, ctypes.byref(least), ctypes.byref(most)), name)
+    return least.value, most.value
+
+
+def costa_mx_norm_workspace(rows: int, cols: int):
+    """(least, most) bytes of costa_mx_norm_backward() with dW."""
+    return _two_sizes("costa_mx_norm_workspace", rows, cols)
+
+
+def costa_mx_norm_backward(dY, H, W, rstd, dX, dH=None, dW=None, workspace=None, stream=None) -> None:
+    """dX <- the gradient of x (and r), dH added; dW <- that of W (a vector)."""
+    need = costa_mx_norm_workspace(*dY.shape)[1] if dW is not None and workspace is None else 0
+    at, size, _keep = _workspace(need, workspace, dY.device, stream)
+    _check(_lib.costa_mx_norm_backward(_matrix(dY), _matrix(H), _line(W),
+                                       _vector(rstd, torch.float32, dY.shape[0], "rstd"), _opt(dH), _matrix(dX),
+                                       _line(dW), at, size, _stream(stream)), "costa_mx_norm_backward")
 
 
 def costa_set_workspace_limit(nbytes: int) -> None:

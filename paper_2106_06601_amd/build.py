@@ -26,7 +26,8 @@ COMMON = ["-O3", "-fPIC", "-std=c++17", "-ffp-contract=off",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
           "-Wall", "-Wno-unused-function"]
 SOURCES = ["layout.cpp", "lap.cpp", "plan.cpp", "api.cpp", "scalapack.cpp", "kernels.hip",
-           "mx.cpp", "mx_store.hip", "mx_product.hip", "mx_tiles.hip"]
+           "mx.cpp", "mx_store.hip", "mx_product.hip", "mx_tiles.hip",
+           "mx_layer.cpp", "mx_norm.hip"]
 
 
 def _run(cmd):

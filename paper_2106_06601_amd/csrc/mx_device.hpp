@@ -30,6 +30,14 @@ __device__ inline uint32_t mx_scale(uint32_t amax_bits) {
 // exponent field only, so 0 is 2^-127 and 255 NaN.
 __device__ inline float mx_scale_float(uint32_t s) { return __builtin_bit_cast(float, s << 23); }
 
+// The largest of four neighbouring lanes.
+__device__ inline uint32_t quad_max(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true));  // lanes 1 0 3 2
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true));  // lanes 2 3 0 1
+}
+
+__device__ inline uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }
+
 // Eight elements in the format, divided by the scale; zeros for a block of NaN.
 // (Rounding to 4 bits saturates by itself; past 448 the 8-bit conversion would
 // give NaN, so it is clamped first.)

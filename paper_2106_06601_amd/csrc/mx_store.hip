@@ -24,14 +24,6 @@ __device__ inline int64_t quotient(int64_t a, int64_t b) {
   return a / b;
 }
 
-// The largest of four neighbouring lanes.
-__device__ inline uint32_t quad_max(uint32_t v) {
-  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true));  // lanes 1 0 3 2
-  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true));  // lanes 2 3 0 1
-}
-
-__device__ inline uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }
-
 // ---- blocks along the lines of a plain matrix -------------------------------
 // A lane takes 8 elements, four lanes a block; a wave reads 512 consecutive
 // elements and writes them.  No shared memory.  Bound by memory: 16384^2 floats to 4

@@ -1,0 +1,282 @@
+"""Root-mean-square norms on the GPU against the formula in 64 bits.
+
+Bounds.  h: one rounding of x + r in 32 bits and one to its type (none to F32): U = 2^-24
+plus the type's half step of |h|.  s: the sum of squares is in 64 bits, one rounding to 32
+bits, after the sum x + r of 2^-24: relative 3 * 2^-24.  y = h s w: those of h and s and two
+products': 8 * 2^-24 of |y|, and the type's half step.  mx(y): what two roundings apart
+can do: the formula applied to y (1 +- 8 * 2^-24) gives the same code, or the neighbouring
+one; checked as: the stored value lies between the values that the two ends are stored as, where both
+have the same scale.  dx = s (g - u c) + dh: each of the terms' magnitudes with 12 * 2^-24, c
+with 8 * 2^-24 of mean |g u| (its sum is in 64 bits), and the half step.  dw: rows / parts
+additions in 32 bits in a workgroup (at most 24 rows each, tested up to 700 rows) and 64-bit ones:
+(rows + 4) * 2^-24 of sum |dy u|, and the half step.
+"""
+import numpy as np
+import pytest
+import torch
+
+import mx_formula as F
+
+C = pytest.importorskip("paper_2106_06601_amd")
+pytestmark = pytest.mark.gpu
+
+TORCH = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+HALF = {"f32": 2.0**-24, "bf16": 2.0**-8, "f16": 2.0**-11}  # half of torch.finfo(t).eps
+TINY = {"f32": 2.0**-149, "bf16": 2.0**-133, "f16": 2.0**-25}
+U = 2.0**-24
+EPS = 1e-5
+
+SHAPES = [(1, 1), (2, 3), (1, 7), (5, 8), (3, 9), (4, 255), (7, 256), (6, 513), (5, 1023), (3, 2048), (9, 2501), (2, 4096),
+          (3, 8191), (2, 16384), (2, 16400), (1, 32768), (2, 33001)]
+
+
+def put(x, dtype, ld=None):
+    """x on the GPU with rows `ld` apart, garbage between."""
+    rows, cols = x.shape
+    ld = ld or cols
+    flat = torch.full((rows * ld + 5,), 77.0, dtype=TORCH[dtype]).cuda()
+    t = flat[3:3 + rows * ld].view(rows, ld)[:, :cols] if ld > cols else flat[3:3 + rows * cols].view(rows, cols)
+    t.copy_(x)
+    return t
+
+
+def wide(t):
+    return t.detach().to(torch.float64).cpu().numpy()
+
+
+def inputs(rng, m, n, dtype, res, wtype):
+    x = torch.from_numpy(rng.standard_normal((m, n)) * np.exp2(rng.integers(-4, 5, (m, 1)))).to(TORCH[dtype])
+    r = torch.from_numpy(rng.standard_normal((m, n))).to(TORCH[dtype]) if res else None
+    w = torch.from_numpy(1 + 0.3 * rng.standard_normal(n)).to(TORCH[wtype]) if wtype else None
+    return x, r, w
+
+
+def formula(x, r, w):
+    h = wide(x) + (0 if r is None else wide(r))
+    s = 1 / np.sqrt((h * h).mean(1) + float(np.float32(EPS)))
+    return h, s, h * s[:, None] * (1 if w is None else wide(w))
+
+
+def between(q, y, bits):
+    """q's values are those of y, or of what is a few roundings beside it.  (How many blocks'
+    largest value lies that near a power of two, so that either scale will do, is no matter of
+    the kernel's: in the row 3 of (6, 513), bf16 with a residual, one is 2 (1 - 3 * 2^-24).)"""
+    data, scales = q
+    got = F.decode(data, scales, bits, y.shape[1])
+    ends, same = [], True
+    for f in (1 - 8 * U, 1 + 8 * U):
+        d, s = F.encode((y * f).astype(np.float32), bits)
+        ends.append(F.decode(d, s, bits, y.shape[1]))
+        same = same & (s == scales) if isinstance(same, np.ndarray) else s == scales
+    lo, hi = np.minimum(*ends), np.maximum(*ends)
+    known = np.repeat(same, 32, axis=1)[:, :y.shape[1]]
+    assert ((lo <= got) & (got <= hi) | ~known).all()
+    # a scale that differs is that of one of the ends
+    either = np.zeros(scales.shape, bool)
+    for f in (1 - 8 * U, 1 + 8 * U):
+        either |= F.encode((y * f).astype(np.float32), bits)[1] == scales
+    assert either.all()
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("dtype,wtype", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("f16", "f16"), ("f16", "f32"), ("bf16", None)])
+@pytest.mark.parametrize("res", [False, True])
+def test_norm(shape, dtype, wtype, res):
+    m, n = shape
+    rng = np.random.default_rng(m * 100003 + n)
+    x, r, w = inputs(rng, m, n, dtype, res, wtype)
+    h, s, y = formula(x, r, w)
+    for bits, ld in ((8, n), (4, n + 3)):
+        xt, rt = put(x, dtype, ld), None if r is None else put(r, dtype, ld)
+        H, Y, rstd = put(x * 0, dtype, ld), put(x * 0, dtype, n + 1), torch.zeros(m).cuda()
+        d, sc = C.costa_mx_sizes(bits, m, n)
+        data, scales = (torch.full((k + 64,), 0xA5, dtype=torch.uint8).cuda() for k in (d, sc))
+        q = C.MxMatrix(bits, m, n, data, scales)
+        C.costa_mx_norm(EPS, xt, None if w is None else w.cuda(), R=rt, H=H, Y=Y, Q=q, rstd=rstd)
+        assert (np.abs(wide(H) - h) <= (HALF[dtype] + U) * np.abs(h) + TINY[dtype]).all()
+        assert (np.abs(wide(rstd) - s) <= 3 * U * s).all()
+        assert (np.abs(wide(Y) - y) <= (HALF[dtype] + 8 * U) * np.abs(y) + TINY[dtype]).all()
+        data, scales = data.cpu().numpy(), scales.cpu().numpy()
+        assert (data[d:] == 0xA5).all() and (scales[sc:] == 0xA5).all()
+        data, scales = data[:d].reshape(m, -1), scales[:sc].reshape(m, -1)
+        between((data, scales), y, bits)
+        pad = -(-n // 32) * 32
+        assert not data[:, pad * bits // 8:].any() and not scales[:, pad // 32:].any()
+        # each result alone is the same
+        for name in ("H", "Y", "Q", "rstd"):
+            one = {"H": torch.zeros_like(H), "Y": torch.zeros_like(Y), "Q": C.MxMatrix.empty(bits, m, n),
+                   "rstd": torch.zeros_like(rstd)}[name]
+            C.costa_mx_norm(EPS, xt, None if w is None else w.cuda(), R=rt, **{name: one})
+            want = {"H": H, "Y": Y, "rstd": rstd}.get(name)
+            if want is not None:
+                assert torch.equal(one, want)
+            else:
+                assert (one.data[:d].cpu().numpy().reshape(m, -1) == data).all()
+        # in place
+        for into in (xt, rt):
+            if into is not None:
+                kept = into.clone()
+                C.costa_mx_norm(EPS, xt, None if w is None else w.cuda(), R=rt, H=into)
+                assert torch.equal(into, H)
+                into.copy_(kept)
+
+
+@pytest.mark.parametrize("shape", SHAPES + [(700, 33), (300, 257), (130, 2055), (65, 5000)], ids=str)
+@pytest.mark.parametrize("dtype,wtype", [("f32", "f32"), ("bf16", "f32"), ("f16", "f16"), ("bf16", None)])
+@pytest.mark.parametrize("res", [False, True])
+def test_norm_backward(shape, dtype, wtype, res):
+    m, n = shape
+    rng = np.random.default_rng(m * 100003 + n + 1)
+    hx, dh, w = inputs(rng, m, n, dtype, res, wtype)
+    dy = torch.from_numpy(rng.standard_normal((m, n))).to(TORCH[dtype])
+    h, s, _ = formula(hx, None, w)
+    rstd = torch.from_numpy(s.astype(np.float32)).cuda()
+    s = wide(rstd)[:, None]
+    g = wide(dy) * (1 if w is None else wide(w))
+    u = h * s
+    c = (g * u).mean(1, keepdims=True)
+    add = 0 if dh is None else wide(dh)
+    dx, dw = s * (g - u * c) + add, (wide(dy) * u).sum(0)
+    off = (12 * U) * (s * (np.abs(g) + np.abs(u * c)) + np.abs(add)) + 8 * U * s * np.abs(u) * np.abs(g * u).mean(1, keepdims=True)
+    DY, H, DH = put(dy, dtype, n + 2), put(hx, dtype, n), None if dh is None else put(dh, dtype, n + 1)
+    W = None if w is None else w.cuda()
+    DX = put(dy * 0, dtype, n + 2)
+    least, most = C.costa_mx_norm_workspace(m, n)
+    assert least <= most
+    for dwtype, size in (("f32", None), (dtype, least), ("f32", (least + most) // 2)):
+        DW = torch.full((n,), 7.0, dtype=TORCH[dwtype]).cuda()
+        ws = None if size is None else torch.full((size,), 0xFF, dtype=torch.uint8).cuda()
+        C.costa_mx_norm_backward(DY, H, W, rstd, DX, dH=DH, dW=DW, workspace=ws)
+        assert (np.abs(wide(DX) - dx) <= off + HALF[dtype] * np.abs(dx) + TINY[dtype]).all()
+        bound = (m + 4) * U * np.abs(wide(dy) * u).sum(0)
+        assert (np.abs(wide(DW) - dw) <= bound + HALF[dwtype] * np.abs(dw) + TINY[dwtype]).all()
+    alone = torch.zeros_like(DX)
+    C.costa_mx_norm_backward(DY, H, W, rstd, alone, dH=DH)
+    assert torch.equal(alone, DX)
+    for into in (DY, DH):  # in place
+        if into is not None:
+            kept = into.clone()
+            C.costa_mx_norm_backward(DY, H, W, rstd, into, dH=DH)
+            assert torch.equal(into, DX)
+            into.copy_(kept)
+
+
+def test_norm_gradients_are_the_forward_s_differences():
+    """Central differences of f = sum(dy y) in float: f's second differences at step d are of
+    order d^2, its roundings 2^-24 of its terms over d: both far below 1e-2 of the gradient's size."""
+    rng = np.random.default_rng(3)
+    m, n = 3, 40
+    x, r, w = (torch.from_numpy(rng.standard_normal(k).astype(np.float32)).cuda() for k in ((m, n), (m, n), n))
+    dy = torch.from_numpy(rng.standard_normal((m, n)).astype(np.float32)).cuda()
+    H, Y, rstd = torch.zeros_like(x), torch.zeros_like(x), torch.zeros(m).cuda()
+
+    def f(x, w):
+        C.costa_mx_norm(EPS, x, w, R=r, Y=Y)
+        return float((Y.double() * dy.double()).sum())
+
+    C.costa_mx_norm(EPS, x, w, R=r, H=H, rstd=rstd)
+    DX, DW = torch.zeros_like(x), torch.zeros_like(w)
+    C.costa_mx_norm_backward(dy, H, w, rstd, DX, dW=DW)
+    for t, grad in ((x, DX), (w, DW)):
+        for at in range(0, t.numel(), 7):
+            step = torch.zeros_like(t).view(-1)
+            step[at] = 2.0**-7
+            step = step.view(t.shape)
+            up = f(*(v + step if v is t else v for v in (x, w)))
+            down = f(*(v - step if v is t else v for v in (x, w)))
+            assert abs((up - down) / 2.0**-6 - float(grad.view(-1)[at])) < 1e-2
+
+
+def test_magnitudes_that_do_not_square_in_floats():
+    for scale in (2.0**100, 2.0**-100, 2.0**120):
+        x = (torch.randn(4, 100, generator=torch.Generator().manual_seed(1)) * scale).cuda()
+        Y, rstd = torch.zeros_like(x), torch.zeros(4).cuda()
+        C.costa_mx_norm(2.0**-126, x, Y=Y, rstd=rstd)
+        h = wide(x)
+        s = 1 / np.sqrt((h * h).mean(1) + 2.0**-126)
+        assert (np.abs(wide(rstd) - s) <= 3 * U * s).all()
+        assert (np.abs(wide(Y) - h * s[:, None]) <= 8 * U * np.abs(h * s[:, None]) + 2.0**-149).all()
+
+
+def test_rows_of_zeros_infinities_and_nan():
+    x = torch.ones(4, 300)
+    x[0], x[1, 7], x[2, 299] = 0.0, float("inf"), float("nan")
+    for dtype in ("f32", "bf16", "f16"):
+        Y, rstd, q = torch.zeros(4, 300, dtype=TORCH[dtype]).cuda(), torch.zeros(4).cuda(), C.MxMatrix.empty(8, 4, 300)
+        C.costa_mx_norm(EPS, x.to(TORCH[dtype]).cuda(), Y=Y, Q=q, rstd=rstd)
+        y = wide(Y)
+        assert not y[0].any() and abs(float(rstd[0]) * EPS**0.5 - 1) < 1e-6
+        # 1 / sqrt(inf) = 0: zeros, and a NaN where the infinity is
+        assert np.isnan(y[1, 7]) and not np.delete(y[1], 7).any() and float(rstd[1]) == 0
+        assert np.isnan(y[2]).all()
+        one = 1 / np.sqrt(1 + float(np.float32(EPS)))  # (a row of ones)
+        assert (np.abs(y[3] - one) <= (8 * U + HALF[dtype]) * one).all()
+        scales = q.scales.cpu().numpy().reshape(4, -1)
+        assert (scales[1, :10] == [255] + [0] * 9).all() and (scales[2, :10] == 255).all() and not scales[:, 10:].any()
+
+
+def test_no_rows_and_no_columns():
+    for m, n in ((0, 5), (5, 0), (0, 0)):
+        x = torch.zeros(m, n).cuda()
+        w, rstd = torch.ones(n).cuda(), torch.full((m,), 7.0).cuda()
+        dw = torch.full((n,), 7.0).cuda()
+        C.costa_mx_norm(EPS, x, w, Y=torch.zeros_like(x), rstd=rstd)
+        C.costa_mx_norm_backward(x, x.clone(), w, rstd, torch.zeros_like(x), dW=dw)
+        assert (rstd == 7).all() and not dw.any()
+
+
+def test_more_rows_than_a_launch_has_workgroups():
+    """Rows past 2^16 workgroups are taken in the kernel's loop; a shorter and a longer row."""
+    for m, n in ((300_001, 3), (70_000, 1030)):
+        x = torch.randn(m, n, generator=torch.Generator("cuda").manual_seed(1), device="cuda").bfloat16()
+        Y, rstd, D, dw = torch.zeros_like(x), torch.zeros(m, device="cuda"), torch.zeros_like(x), torch.zeros(n, device="cuda")
+        w = torch.rand(n, device="cuda").bfloat16()
+        C.costa_mx_norm(EPS, x, w, Y=Y, rstd=rstd)
+        s = 1 / (x.double().square().mean(1) + EPS).sqrt()
+        assert ((rstd - s).abs() <= 3 * U * s).all()
+        y = x.double() * s[:, None] * w.double()
+        assert ((Y - y).abs() <= (HALF["bf16"] + 8 * U) * y.abs() + 2.0**-133).all()
+        C.costa_mx_norm_backward(x, x, None, rstd, D, dW=dw)
+        u = x.double() * rstd.double()[:, None]
+        want = (x.double() * u).sum(0)
+        # (each part has up to m / 1024 rows and 4 more in one lane's chain)
+        assert ((dw - want).abs() <= (m / 256 + 8) * U * (x.double() * u).abs().sum(0)).all()
+        dx = rstd.double()[:, None] * (x.double() - u * (x.double() * u).mean(1, keepdim=True))
+        off = 20 * U * rstd.double()[:, None] * (x.double().abs() + u.abs() * (x.double() * u).abs().mean(1, keepdim=True))
+        assert ((D - dx).abs() <= off + HALF["bf16"] * dx.abs() + 2.0**-133).all()
+
+
+def test_on_another_stream_and_in_a_graph():
+    m, n = 37, 1000
+    x = torch.randn(m, n, device="cuda").bfloat16()
+    dy, w = torch.randn(m, n, device="cuda").bfloat16(), torch.rand(n, device="cuda")
+    Y, H, D, rstd, dw = torch.zeros_like(x), torch.zeros_like(x), torch.zeros_like(x), torch.zeros(m, device="cuda"), torch.zeros(n, device="cuda")
+    ws = torch.empty(C.costa_mx_norm_workspace(m, n)[1], dtype=torch.uint8, device="cuda")
+
+    def both(stream=None):
+        C.costa_mx_norm(EPS, x, w, H=H, Y=Y, rstd=rstd, stream=stream)
+        C.costa_mx_norm_backward(dy, H, w, rstd, D, dW=dw, workspace=ws, stream=stream)
+
+    both()
+    want = [t.clone() for t in (Y, D, rstd, dw)]
+    side = torch.cuda.Stream()
+    for t in (Y, D, rstd, dw):
+        t.zero_()
+    torch.cuda.synchronize()
+    both(side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, (Y, D, rstd, dw)))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        both()
+    for k in range(3):
+        x.normal_()
+        dy.normal_()
+        for t in (Y, D, rstd, dw):
+            t.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (Y, D, rstd, dw)]
+        both()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, (Y, D, rstd, dw)))
