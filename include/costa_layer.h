@@ -1,7 +1,7 @@
 /*
  * costa_layer.h -- what stands around the products of a layer whose weights are
- * kept in few bits (costa_mx.h): the norm that makes a product's operand, with its
- * gradients.
+ * kept in few bits (costa_mx.h): the norm that makes a product's operand and low-rank
+ * adapters beside a product, each with its gradients.
  *
  * Conventions are those of costa_mx.h: calls are asynchronous on `stream`, on the
  * current device; every argument error is returned before anything is enqueued; the
@@ -55,6 +55,47 @@ costa_status costa_mx_norm_backward(const costa_matrix* dY, const costa_matrix* 
 
 /* Workspace of costa_mx_norm_backward() with dW (without: none). */
 costa_status costa_mx_norm_workspace(int64_t rows, int64_t cols, size_t* least, size_t* most);
+
+/* ---- low-rank adapters beside a product ------------------------------------
+ * `count` adapters of up to `rank` (at most 256): rows a*rank .. of A (count*rank x k)
+ * and of B (count*rank x n) are those of adapter a, both kept rank by rank: B is
+ * the transpose of the usual n x rank matrix, so that the two change places in the backward
+ * pass.  ranks (device memory, `count` entries; NULL: all of them `rank`): how many of its
+ * rows an adapter has (taken into 0 .. rank); those past it are not read.  scales (device
+ * memory, `count`; NULL: 1): s below. */
+typedef struct {
+  int32_t count, rank;
+  const costa_matrix* A;
+  const costa_matrix* B;
+  const int32_t* ranks;
+  const float* scales;
+} costa_mx_adapters;
+
+/* C <- alpha X W^^T + s V B + beta C, row i with the adapter a = index[i]: V = X A_a^T.
+ * X m x k, W n x k, C m x n; A, B of X's type; index: m entries, in any order; a row whose
+ * entry is not in 0 .. count-1 has no adapter.  V (NULL: not wanted): m x rank of F32, the
+ * rows' products, 0 past their adapter's rank; what the gradients below need.  An
+ * infinity or a NaN of one adapter reaches its own rows alone (where an infinity may come out
+ * as NaN).  beta == 0: C is not read.
+ *
+ * The gradient of X is this call with dY in X's place, mx(W^T) in W's, and A and B swapped;
+ * its V is dY B_a^T. */
+costa_status costa_mx_product_adapted(float alpha, const costa_matrix* X, const costa_mx* W,
+                                      const costa_mx_adapters* adapters, const int32_t* index, float beta,
+                                      const costa_matrix* C, const costa_matrix* V, void* workspace,
+                                      size_t workspace_bytes, hipStream_t stream);
+costa_status costa_mx_adapted_workspace(int64_t m, int64_t n, int64_t k, int32_t rank, size_t* least, size_t* most);
+
+/* G_a <- s_a sum over the rows i of adapter a of V_i^T Z_i + beta G_a: with (V, Z) = (dY B^T, X)
+ * the gradient of A, with (X A^T, dY) that of B.  V m x rank of F32, Z m x len, G (count*rank) x
+ * len of any type here.  Of `adapters` A and B are not looked at (NULL allowed).  Rows past an
+ * adapter's rank, and adapters without rows, get beta G (0 for beta == 0: G is not read then). */
+costa_status costa_mx_adapter_gradient(const costa_mx_adapters* adapters, const int32_t* index,
+                                       const costa_matrix* V, const costa_matrix* Z, float beta,
+                                       const costa_matrix* G, void* workspace, size_t workspace_bytes,
+                                       hipStream_t stream);
+costa_status costa_mx_adapter_gradient_workspace(int64_t m, int64_t len, int32_t count, int32_t rank, size_t* least,
+                                                 size_t* most);
 
 #ifdef __cplusplus
 }

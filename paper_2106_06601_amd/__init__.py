@@ -137,6 +137,12 @@ _SIGS = {
     "costa_mx_norm": [ctypes.c_float, *[_P(CostaMatrix)] * 5, _P(CostaMx), _vp, _vp],
     "costa_mx_norm_backward": [*[_P(CostaMatrix)] * 3, _vp, *[_P(CostaMatrix)] * 3, _vp, ctypes.c_size_t, _vp],
     "costa_mx_norm_workspace": [_i64, _i64, _P(ctypes.c_size_t), _P(ctypes.c_size_t)],
+    "costa_mx_product_adapted": [ctypes.c_float, _P(CostaMatrix), _P(CostaMx), _P(CostaMxAdapters), _vp, ctypes.c_float,
+                                 _P(CostaMatrix), _P(CostaMatrix), _vp, ctypes.c_size_t, _vp],
+    "costa_mx_adapted_workspace": [_i64, _i64, _i64, _i32, _P(ctypes.c_size_t), _P(ctypes.c_size_t)],
+    "costa_mx_adapter_gradient": [_P(CostaMxAdapters), _vp, _P(CostaMatrix), _P(CostaMatrix), ctypes.c_float,
+                                  _P(CostaMatrix), _vp, ctypes.c_size_t, _vp],
+    "costa_mx_adapter_gradient_workspace": [_i64, _i64, _i32, _i32, _P(ctypes.c_size_t), _P(ctypes.c_size_t)],
 }
 for _name, _args in _SIGS.items():
     _f = getattr(_lib, _name)
@@ -714,6 +720,65 @@ def costa_mx_norm_backward(dY, H, W, rstd, dX, dH=None, dW=None, workspace=None,
     _check(_lib.costa_mx_norm_backward(_matrix(dY), _matrix(H), _line(W),
                                        _vector(rstd, torch.float32, dY.shape[0], "rstd"), _opt(dH), _matrix(dX),
                                        _line(dW), at, size, _stream(stream)), "costa_mx_norm_backward")
+
+
+class MxAdapters:
+    """Adapters over device tensors (kept alive by this object): A count x rank x k, B count x
+    rank x n, contiguous; ranks count int32 or None, scales count floats or None."""
+
+    def __init__(self, A, B, ranks=None, scales=None):
+        if A.dim() != 3 or B.dim() != 3 or A.shape[:2] != B.shape[:2] or A.dtype != B.dtype:
+            raise ValueError("A and B: count x rank x k and count x rank x n of one type are needed")
+        if not A.is_contiguous() or not B.is_contiguous():
+            raise ValueError("A and B: contiguous tensors are needed")
+        count, rank = A.shape[:2]
+        self.A, self.B, self.ranks, self.scales, self.count, self.rank = A, B, ranks, scales, count, rank
+        self._a, self._b = _matrix(A.flatten(0, 1)), _matrix(B.flatten(0, 1))
+        self._c = CostaMxAdapters(count, rank, ctypes.pointer(self._a), ctypes.pointer(self._b),
+                                  _vector(ranks, torch.int32, count, "ranks"),
+                                  _vector(scales, torch.float32, count, "scales"))
+        self._ref = ctypes.pointer(self._c)
+        self._turned = None
+
+    def turned(self) -> "MxAdapters":
+        """The same with A and B in each other's place: those of the backward pass."""
+        if self._turned is None:
+            self._turned = MxAdapters(self.B, self.A, self.ranks, self.scales)
+        return self._turned
+
+
+def costa_mx_adapted_workspace(m: int, n: int, k: int, rank: int):
+    """(least, most) bytes of costa_mx_product_adapted()."""
+    return _two_sizes("costa_mx_adapted_workspace", m, n, k, rank)
+
+
+def costa_mx_product_adapted(alpha: float, X, W: MxMatrix, adapters: MxAdapters, index, beta: float, C, V=None,
+                             workspace=None, stream=None) -> None:
+    """C <- alpha X W^^T + s V B + beta C with V = X A^T, row i with the adapter index[i] (int32; none where it is
+    out of range); V (m x rank floats) is kept if it is given."""
+    m, k = X.shape
+    need = 0 if workspace is not None else costa_mx_adapted_workspace(m, W.rows, k, adapters.rank)[1]
+    at, size, _keep = _workspace(need, workspace, X.device, stream)
+    _check(_lib.costa_mx_product_adapted(alpha, _matrix(X), _mx(W), adapters._ref,
+                                         _vector(index, torch.int32, m, "index"), beta, _matrix(C), _opt(V), at, size,
+                                         _stream(stream)), "costa_mx_product_adapted")
+
+
+def costa_mx_adapter_gradient_workspace(m: int, length: int, count: int, rank: int):
+    """(least, most) bytes of costa_mx_adapter_gradient()."""
+    return _two_sizes("costa_mx_adapter_gradient_workspace", m, length, count, rank)
+
+
+def costa_mx_adapter_gradient(adapters: MxAdapters, index, V, Z, beta: float, G, workspace=None, stream=None) -> None:
+    """G_a <- s_a (sum over the rows of a of V_i^T Z_i) + beta G_a; G count x rank x len, contiguous."""
+    (m, length), (count, rank) = Z.shape, (adapters.count, adapters.rank)
+    if tuple(G.shape) != (count, rank, length) or not G.is_contiguous():
+        raise ValueError(f"G: a contiguous tensor of {count} x {rank} x {length} is needed")
+    need = 0 if workspace is not None else costa_mx_adapter_gradient_workspace(m, length, count, rank)[1]
+    at, size, _keep = _workspace(need, workspace, Z.device, stream)
+    _check(_lib.costa_mx_adapter_gradient(adapters._ref, _vector(index, torch.int32, m, "index"), _matrix(V),
+                                          _matrix(Z), beta, _matrix(G.flatten(0, 1)), at, size, _stream(stream)),
+           "costa_mx_adapter_gradient")
 
 
 def costa_set_workspace_limit(nbytes: int) -> None:

@@ -177,3 +177,171 @@ extern "C" costa_status costa_mx_norm_workspace(int64_t rows, int64_t cols, size
     return COSTA_SUCCESS;
   });
 }
+
+namespace costa {
+namespace {
+
+constexpr size_t kSliceBytes = (size_t)128 << 20;  // of a slice's sums: the last-level cache holds them
+
+size_t up16(size_t v) { return (v + 15) / 16 * 16; }
+
+// Rows of C whose sums are in the workspace at a time: all, or so many.
+int64_t slice_rows(int64_t m, int64_t n) {
+  const int64_t most = (int64_t)(kSliceBytes / 4) / std::max<int64_t>(n, 1) / 256 * 256;
+  return std::min(m, std::max<int64_t>(most, 256));
+}
+
+// Bytes of the sums of `rows` rows, and of those with what a split sum can use.
+size_t sums_bytes(int64_t rows, int64_t n) { return (size_t)rows * n * 4; }
+size_t split_bytes(int64_t rows, int64_t n, int64_t k) {
+  return std::max(mx_product_workspace(rows, n, k), sums_bytes(rows, n));
+}
+
+// The adapters' index and, where they are given, A and B.
+costa_status check_adapters(const costa_mx_adapters* p, const int32_t* index, int64_t m, AdapterIndex& at) {
+  if (!p) return fail(COSTA_ERROR_INVALID_VALUE, "adapters: null");
+  if (p->count < 0 || p->rank < 0) return fail(COSTA_ERROR_INVALID_VALUE, "adapters: negative count or rank");
+  if (p->rank > kRankMax) return fail(COSTA_ERROR_NOT_SUPPORTED, "adapters: a rank above 256");
+  if ((int64_t)p->count * p->rank > INT32_MAX) return fail(COSTA_ERROR_NOT_SUPPORTED, "adapters: more than 2^31-1 rows");
+  CHECKED(check_vector("ranks", p->ranks, 0, 4));
+  CHECKED(check_vector("scales", p->scales, 0, 4));
+  CHECKED(check_vector("index", index, m, 4));
+  at = AdapterIndex{p->count, p->rank, p->ranks, p->scales, index};
+  return COSTA_SUCCESS;
+}
+
+}  // namespace
+}  // namespace costa
+
+extern "C" costa_status costa_mx_product_adapted(float alpha, const costa_matrix* X, const costa_mx* W,
+                                                 const costa_mx_adapters* adapters, const int32_t* index, float beta,
+                                                 const costa_matrix* C, const costa_matrix* V, void* workspace,
+                                                 size_t workspace_bytes, hipStream_t stream) {
+  return guarded([&]() -> costa_status {
+    CHECKED(check_rows("X", X));
+    const int64_t m = X->rows, k = X->cols;
+    MxView w;
+    CHECKED(check_mx("W", W, w));
+    if (W->cols != k) return fail(COSTA_ERROR_SHAPE_MISMATCH, "X and W have different lengths to sum over");
+    const int64_t n = W->rows;
+    AdapterIndex at;
+    CHECKED(check_adapters(adapters, index, m, at));
+    const int64_t all = (int64_t)at.count * at.rank;
+    CHECKED(check_like("A", adapters->A, all, k, X->type));
+    CHECKED(check_like("B", adapters->B, all, n, X->type));
+    CHECKED(check_rows("C", C));
+    if (C->rows != m || C->cols != n) return fail(COSTA_ERROR_SHAPE_MISMATCH, "C is not the shape of X W^T");
+    if (V) CHECKED(check_like("V", V, m, at.rank, COSTA_REAL_F32));
+    size_t least = 0;
+    CHECKED(costa_mx_adapted_workspace(m, n, k, at.rank, &least, nullptr));
+    CHECKED(check_workspace(workspace, workspace_bytes, least));
+    Uses u;
+    u.add("X", X, false), u.add("W", w, false), u.add("A", adapters->A, false), u.add("B", adapters->B, false);
+    u.add("ranks", at.ranks, (int64_t)at.count * 4, false), u.add("scales", at.scales, (int64_t)at.count * 4, false);
+    u.add("index", index, m * 4, false);
+    u.add("C", C, true), u.add("V", V, true), u.workspace(workspace, workspace_bytes);
+    CHECKED(u.check());
+    if (m == 0) return COSTA_SUCCESS;
+    char* room = static_cast<char*>(workspace);
+    size_t left = workspace ? workspace_bytes : 0;
+    AdapterDotsArgs d{at, m, k, X->type, rows_of(X), rows_of(adapters->A), nullptr, at.rank};
+    if (V) {
+      d.v = static_cast<float*>(V->data), d.v_ld = V->ld;
+    } else {
+      d.v = reinterpret_cast<float*>(room);
+      const size_t taken = up16((size_t)m * at.rank * 4);
+      room += taken, left -= taken;
+    }
+    if (at.rank > 0) HIP_OR_FAIL(launch_mx_adapter_dots(d, stream));
+    if (n == 0) return COSTA_SUCCESS;
+    // slices of rows whose sums the workspace holds
+    const int64_t per = k == 0 ? m : std::min<int64_t>(slice_rows(m, n), (int64_t)(left / sums_bytes(1, n)));
+    for (int64_t i = 0; i < m; i += per) {
+      const int64_t rows = std::min(per, m - i);
+      const int64_t es = real_size(X->type);
+      AdapterAddArgs c{};
+      c.at = at, c.at.index += i;
+      c.m = rows, c.n = n;
+      c.type = X->type, c.c_type = C->type;
+      c.low = rows_of(adapters->B);
+      c.c = RowsView{static_cast<char*>(C->data) + i * C->ld * real_size(C->type), C->ld};
+      c.v = d.v + i * d.v_ld, c.v_ld = d.v_ld;
+      c.parts = reinterpret_cast<float*>(room);
+      c.alpha = alpha, c.beta = beta;
+      if (k > 0) {
+        ProductArgs p{};
+        p.m = rows, p.n = n, p.k = k;
+        p.real = static_cast<const char*>(X->data) + i * X->ld * es;
+        p.a_rs = X->ld, p.a_cs = 1, p.a_type = X->type;
+        p.b = w;
+        p.workspace = reinterpret_cast<float*>(room), p.workspace_bytes = left;
+        HIP_OR_FAIL(launch_mx_product_parts(p, c.splits, stream));
+      }
+      HIP_OR_FAIL(launch_mx_adapter_add(c, stream));
+    }
+    return COSTA_SUCCESS;
+  });
+}
+
+extern "C" costa_status costa_mx_adapted_workspace(int64_t m, int64_t n, int64_t k, int32_t rank, size_t* least,
+                                                   size_t* most) {
+  return guarded([&]() -> costa_status {
+    CHECKED(check_dims("C", m, n));
+    CHECKED(check_dims("X", m, k));
+    if (rank < 0) return fail(COSTA_ERROR_INVALID_VALUE, "negative rank");
+    if (rank > kRankMax) return fail(COSTA_ERROR_NOT_SUPPORTED, "a rank above 256");
+    const size_t v = up16((size_t)m * rank * 4);
+    const bool sums = m > 0 && n > 0 && k > 0;
+    give(least, v + (sums ? sums_bytes(std::min<int64_t>(m, 256), n) : 0));
+    give(most, v + (sums ? split_bytes(slice_rows(m, n), n, k) : 0));
+    return COSTA_SUCCESS;
+  });
+}
+
+extern "C" costa_status costa_mx_adapter_gradient(const costa_mx_adapters* adapters, const int32_t* index,
+                                                  const costa_matrix* V, const costa_matrix* Z, float beta,
+                                                  const costa_matrix* G, void* workspace, size_t workspace_bytes,
+                                                  hipStream_t stream) {
+  return guarded([&]() -> costa_status {
+    CHECKED(check_rows("Z", Z));
+    const int64_t m = Z->rows, len = Z->cols;
+    AdapterGradArgs a{};
+    CHECKED(check_adapters(adapters, index, m, a.at));
+    CHECKED(check_like("V", V, m, a.at.rank, COSTA_REAL_F32));
+    const int64_t all = (int64_t)a.at.count * a.at.rank;
+    CHECKED(check_rows("G", G));
+    if (G->rows != all || G->cols != len) return fail(COSTA_ERROR_SHAPE_MISMATCH, "G is not the shape of the adapters' rows");
+    size_t least = 0;
+    CHECKED(costa_mx_adapter_gradient_workspace(m, len, a.at.count, a.at.rank, &least, nullptr));
+    CHECKED(check_workspace(workspace, workspace_bytes, least));
+    Uses u;
+    u.add("V", V, false), u.add("Z", Z, false), u.add("index", index, m * 4, false);
+    u.add("ranks", a.at.ranks, (int64_t)a.at.count * 4, false), u.add("scales", a.at.scales, (int64_t)a.at.count * 4, false);
+    u.add("G", G, true), u.workspace(workspace, workspace_bytes);
+    CHECKED(u.check());
+    if (all == 0 || len == 0) return COSTA_SUCCESS;
+    a.m = m, a.len = len;
+    a.type = Z->type, a.g_type = G->type;
+    a.z = rows_of(Z), a.g = rows_of(G);
+    a.v = static_cast<const float*>(V->data), a.v_ld = V->ld;
+    a.beta = beta;
+    a.parts = static_cast<float*>(workspace);
+    a.most = (int64_t)std::min<size_t>(workspace_bytes / ((size_t)all * len * 4), 65535);
+    HIP_OR_FAIL(launch_mx_adapter_grad(a, stream));
+    return COSTA_SUCCESS;
+  });
+}
+
+extern "C" costa_status costa_mx_adapter_gradient_workspace(int64_t m, int64_t len, int32_t count, int32_t rank,
+                                                            size_t* least, size_t* most) {
+  return guarded([&]() -> costa_status {
+    CHECKED(check_dims("Z", m, len));
+    if (count < 0 || rank < 0) return fail(COSTA_ERROR_INVALID_VALUE, "negative count or rank");
+    if (rank > kRankMax) return fail(COSTA_ERROR_NOT_SUPPORTED, "a rank above 256");
+    if ((int64_t)count * rank > INT32_MAX) return fail(COSTA_ERROR_NOT_SUPPORTED, "more than 2^31-1 rows");
+    const size_t part = (size_t)count * rank * len * 4;
+    give(least, part);
+    give(most, part * mx_adapter_grad_parts(m, len, count, rank));
+    return COSTA_SUCCESS;
+  });
+}

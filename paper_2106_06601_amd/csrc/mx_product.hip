@@ -334,6 +334,41 @@ size_t mx_product_workspace(int64_t m, int64_t n, int64_t k) {
   return most;
 }
 
+namespace {
+
+// Plans a product and launches its sums: split, or where `parts` says so, unscaled to their
+// places in the workspace (as many as it holds), else with e to C.
+hipError_t launch_sums(const ProductArgs& a, const Epilogue& e, bool parts, ProductPlan& plan, hipStream_t stream) {
+  const int src = a.amx.bits == 4                 ? SRC_MX4
+                  : a.amx.bits == 8               ? SRC_MX8
+                  : a.a_type == COSTA_REAL_BF16   ? SRC_BF16
+                  : a.a_type == COSTA_REAL_F16    ? SRC_F16
+                                                  : SRC_F32;
+  const bool k_next = a.amx.bits != 0 || a.a_cs == 1;
+  plan = plan_product(src, k_next, a.b.bits, a.m, a.n, a.k);
+  Args p{a.m, a.n, a.k, a.amx, a.b, a.real, a.a_rs, a.a_cs, e, 0};
+  const size_t part = (size_t)a.m * a.n * sizeof(float);
+  plan.splits = (int)std::min<size_t>(plan.splits, a.workspace_bytes / part);
+  if (plan.splits > 1 || parts) {
+    p.e = Epilogue{a.workspace, a.n, 1, COSTA_REAL_F32, a.n % 4 == 0, 1.0f, 0.0f};
+    p.part = a.m * a.n;
+  }
+  plan.splits = std::max(plan.splits, 1);
+  return plan.variant == THIN         ? launch_thin(src, p, stream)
+         : plan.variant == FEW_ROWS   ? launch_few(src, p, plan, stream)
+         : plan.variant == TILES_BF16 ? launch_tiles_bf16(src, p, plan, stream)
+                                      : launch_tiles_scaled(p, plan, stream);
+}
+
+}  // namespace
+
+hipError_t launch_mx_product_parts(const ProductArgs& a, int& splits, hipStream_t stream) {
+  ProductPlan plan{};
+  const hipError_t err = launch_sums(a, Epilogue{}, true, plan, stream);
+  splits = plan.splits;
+  return err;
+}
+
 hipError_t launch_mx_product(const ProductArgs& a, hipStream_t stream) {
   const int64_t es = a.c_type == COSTA_REAL_F32 ? 4 : 2;
   const bool vec = a.c_cs == 1 && a.c_rs % 4 == 0 && (uintptr_t)a.c % (4 * es) == 0;
@@ -343,26 +378,8 @@ hipError_t launch_mx_product(const ProductArgs& a, hipStream_t stream) {
     scale_only<<<dim3((unsigned)std::min<int64_t>(groups, 1 << 20)), 256, 0, stream>>>(e, a.m, a.n);
     return hipGetLastError();
   }
-  const int src = a.amx.bits == 4                 ? SRC_MX4
-                  : a.amx.bits == 8               ? SRC_MX8
-                  : a.a_type == COSTA_REAL_BF16   ? SRC_BF16
-                  : a.a_type == COSTA_REAL_F16    ? SRC_F16
-                                                  : SRC_F32;
-  const bool k_next = a.amx.bits != 0 || a.a_cs == 1;
-  ProductPlan plan = plan_product(src, k_next, a.b.bits, a.m, a.n, a.k);
-  Args p{a.m, a.n, a.k, a.amx, a.b, a.real, a.a_rs, a.a_cs, e, 0};
-  const size_t part = (size_t)a.m * a.n * sizeof(float);
-  plan.splits = (int)std::min<size_t>(plan.splits, a.workspace_bytes / part);
-  if (plan.splits > 1) {
-    p.e = Epilogue{a.workspace, a.n, 1, COSTA_REAL_F32, a.n % 4 == 0, 1.0f, 0.0f};
-    p.part = a.m * a.n;
-  } else {
-    plan.splits = 1;
-  }
-  hipError_t err = plan.variant == THIN         ? launch_thin(src, p, stream)
-                   : plan.variant == FEW_ROWS   ? launch_few(src, p, plan, stream)
-                   : plan.variant == TILES_BF16 ? launch_tiles_bf16(src, p, plan, stream)
-                                                : launch_tiles_scaled(p, plan, stream);
+  ProductPlan plan{};
+  hipError_t err = launch_sums(a, e, false, plan, stream);
   if (err != hipSuccess || plan.splits == 1) return err;
   // (with 16 lanes, 256 parts of a 100 x 64 sum are joined in 5 us; with one, in 66)
   const int lanes = plan.splits >= 16 ? 16 : 1;

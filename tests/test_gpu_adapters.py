@@ -1,0 +1,303 @@
+"""Adapted products and the adapters' gradients on the GPU against the formulas in 64 bits.
+
+Bounds.  A sum of n products in 32 bits, in whatever order: (n / 32 + 12) roundings of 2^-24 of the
+sum of magnitudes (instructions add 32 products and round once or a few times; on the
+vector units a lane's chain is n / 256, and 10 of joining), and as many for products of parts left out or
+rounded.  So v is off by E_v = that of |x| |A|; c by that of |x| |W| (its sum), of s |v| |B| and
+s E_v |B|, 8 * 2^-24 of the terms (scalars, additions), and half a step of its type.  Gradients: that of
+|v| |z| over the adapter's rows.
+"""
+import numpy as np
+import pytest
+import torch
+
+import mx_formula as F
+
+C = pytest.importorskip("paper_2106_06601_amd")
+pytestmark = pytest.mark.gpu
+
+TORCH = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+HALF = {"f32": 2.0**-24, "bf16": 2.0**-8, "f16": 2.0**-11}  # half of torch.finfo(t).eps
+TINY = {"f32": 2.0**-149, "bf16": 2.0**-133, "f16": 2.0**-25}
+U = 2.0**-24
+
+
+def wide(t):
+    return t.detach().to(torch.float64).cpu().numpy()
+
+
+def keep(x, bits):
+    data, scales = F.encode(x, bits)
+    return C.MxMatrix(bits, *x.shape, torch.from_numpy(data).cuda().reshape(-1), torch.from_numpy(scales).cuda().reshape(-1))
+
+
+def strided(x, dtype, ld):
+    rows, cols = x.shape
+    t = torch.full((rows, max(ld, 1)), 77.0, dtype=TORCH[dtype]).cuda()[:, :cols]
+    t.copy_(torch.as_tensor(x))
+    return t
+
+
+def indices(rng, m, count, how):
+    """Rows' adapters: runs of one, all mixed, all the same, none; out of range on both sides."""
+    if how == "runs":
+        a = np.sort(rng.integers(-1, count, m))
+    elif how == "mixed":
+        a = rng.integers(-1, count + 1, m)
+        a[rng.random(m) < 0.05] = 2**31 - 1
+        a[rng.random(m) < 0.05] = -2**31
+    elif how == "same":
+        a = np.full(m, count - 1)
+    else:
+        a = np.full(m, -1)
+    return torch.from_numpy(a.astype(np.int32))
+
+
+class Case:
+    def __init__(self, m, n, k, count, rank, dtype, bits, how, seed=0, ranks=True, scales=True):
+        rng = np.random.default_rng(seed + m * 7 + n * 11 + k * 13 + rank)
+        to = lambda x: torch.from_numpy(x).to(TORCH[dtype])  # noqa: E731
+        self.m, self.n, self.k, self.count, self.rank, self.dtype = m, n, k, count, rank, dtype
+        self.x, self.dy = to(rng.standard_normal((m, k))), to(rng.standard_normal((m, n)))
+        self.A, self.B = to(rng.standard_normal((count, rank, k)) / k**0.5), to(rng.standard_normal((count, rank, n)))
+        w = (rng.standard_normal((n, k)) / k**0.5).astype(np.float32)
+        self.w, self.wq = F.decode(*F.encode(w, bits), bits, k), keep(w, bits)
+        self.index = indices(rng, m, count, how)
+        self.ranks = torch.from_numpy(rng.integers(0, rank + 2, count).astype(np.int32)) if ranks else None
+        self.scales = torch.from_numpy((0.5 + rng.random(count)).astype(np.float32)) if scales else None
+        self.c0 = to(rng.standard_normal((m, n)))
+        on = lambda t: None if t is None else t.cuda()  # noqa: E731
+        self.adapters = C.MxAdapters(on(self.A), on(self.B), on(self.ranks), on(self.scales))
+
+    def rank_of(self, a):
+        return self.rank if self.ranks is None else min(max(int(self.ranks[a]), 0), self.rank)
+
+    def scale_of(self, a):
+        return 1.0 if self.scales is None else float(self.scales[a])
+
+    def rows(self, a):
+        return np.flatnonzero(self.index.numpy() == a)
+
+    def dots(self, x, low):
+        """v and its bound."""
+        v, e = np.zeros((self.m, self.rank)), np.zeros((self.m, self.rank))
+        for a in range(self.count):
+            r, i = self.rank_of(a), self.rows(a)
+            v[i, :r] = x[i] @ low[a, :r].T
+            e[i, :r] = 2 * (x.shape[1] / 32 + 12) * U * (np.abs(x[i]) @ np.abs(low[a, :r]).T)
+        return v, e
+
+    def forward(self, alpha, beta, out):
+        x, A, B = wide(self.x), wide(self.A), wide(self.B)
+        v, ev = self.dots(x, A)
+        c0 = wide(self.c0.to(TORCH[out]))
+        c = alpha * (x @ self.w.T) + (beta * c0 if beta else 0)
+        e = abs(alpha) * (2 * (self.k / 32 + 12) + 8) * U * (np.abs(x) @ np.abs(self.w).T) + 8 * U * np.abs(beta * c0)
+        for a in range(self.count):
+            i, s = self.rows(a), self.scale_of(a)
+            c[i] += s * (v[i] @ B[a])
+            e[i] += s * ((2 * (self.rank / 32 + 12) + 8) * U * (np.abs(v[i]) @ np.abs(B[a])) + ev[i] @ np.abs(B[a]))
+        return v, ev, c, e + HALF[out] * np.abs(c) + TINY[out]
+
+    def gradient(self, v, z):
+        g, e = np.zeros((self.count, self.rank, z.shape[1])), np.zeros((self.count, self.rank, z.shape[1]))
+        for a in range(self.count):
+            r, i, s = self.rank_of(a), self.rows(a), self.scale_of(a)
+            g[a, :r] = s * (v[i, :r].T @ z[i])
+            e[a, :r] = s * (2 * (len(i) / 32 + 12) + 8) * U * (np.abs(v[i, :r]).T @ np.abs(z[i]))
+        return g, e
+
+
+SHAPES = [(1, 1, 1, 1, 1), (1, 40, 300, 3, 4), (3, 7, 5, 2, 3), (5, 2049, 8, 4, 16), (17, 130, 2500, 6, 24), (64, 515, 127, 9, 33),
+          (65, 1, 9, 2, 5), (66, 5, 3, 2, 17), (70, 129, 1030, 3, 16), (200, 520, 257, 40, 8), (333, 199, 1250, 5, 100),
+          (130, 1000, 64, 2, 256), (513, 260, 2048, 7, 64)]
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("how", ["runs", "mixed", "same", "none"])
+def test_adapted_product(shape, dtype, how):
+    m, n, k, count, rank = shape
+    for bits, out, alpha, beta, plain in ((4, dtype, 1.0, 0.0, False), (8, "f32", -0.5, 0.25, True)):
+        c = Case(m, n, k, count, rank, dtype, bits, how, ranks=not plain, scales=not plain)
+        v, ev, want, off = c.forward(alpha, beta, out)
+        X, index = strided(c.x, dtype, k + 3 * plain), c.index.cuda()
+        least, most = C.costa_mx_adapted_workspace(m, n, k, rank)
+        assert least <= most
+        got = []
+        for size in (None, least):
+            y = strided(c.c0 if beta else c.c0 * np.nan, out, n + plain)
+            V = strided(np.full((m, rank), np.nan), "f32", rank + plain)
+            ws = None if size is None else torch.full((size,), 0xFF, dtype=torch.uint8).cuda()
+            C.costa_mx_product_adapted(alpha, X, c.wq, c.adapters, index, beta, y, V=V, workspace=ws)
+            assert (np.abs(wide(V) - v) <= ev).all()
+            assert (np.abs(wide(y) - want) <= off).all()
+            got.append(y)
+        y = strided(c.c0, out, n)
+        C.costa_mx_product_adapted(alpha, X, c.wq, c.adapters, index, beta, y)
+        assert torch.equal(y, got[0])  # V kept or not, and a second time: the same bits
+
+
+@pytest.mark.parametrize("shape", SHAPES + [(3000, 70, 600, 2, 16), (2049, 1030, 30, 1, 20)], ids=str)
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("how", ["runs", "mixed", "same", "none"])
+def test_adapter_gradients(shape, dtype, how):
+    m, n, k, count, rank = shape
+    c = Case(m, n, k, count, rank, dtype, 4, how)
+    rng = np.random.default_rng(5)
+    v = torch.from_numpy(rng.standard_normal((m, rank)).astype(np.float32))
+    for z, gtype, beta in ((c.x, "f32", 0.0), (c.dy, dtype, 0.5)):
+        g, e = c.gradient(wide(v), wide(z))
+        g0 = torch.from_numpy(rng.standard_normal(g.shape)).to(TORCH[gtype])
+        want = g + beta * wide(g0)
+        off = e + 8 * U * np.abs(beta * wide(g0)) + HALF[gtype] * np.abs(want) + TINY[gtype]
+        least, most = C.costa_mx_adapter_gradient_workspace(m, z.shape[1], count, rank)
+        for size in (None, least, most):
+            G = g0.cuda() if beta else torch.full(g.shape, float("nan"), dtype=TORCH[gtype]).cuda()
+            ws = None if size is None else torch.full((size,), 0xFF, dtype=torch.uint8).cuda()
+            C.costa_mx_adapter_gradient(c.adapters, c.index.cuda(), strided(v, "f32", rank + 1),
+                                        strided(z, dtype, z.shape[1] + 2), beta, G, workspace=ws)
+            assert (np.abs(wide(G) - want) <= off).all()
+
+
+@pytest.mark.parametrize("m", [9, 100])
+def test_gradients_are_the_forward_s_differences(m):
+    """In float: f = sum(dy c) is linear in A, in B and in x, so that a difference of f is off by
+    its roundings alone: (k + rank) * 2^-24 of some hundred terms of size 1 over steps of 1."""
+    n, k, count, rank = 20, 40, 3, 6
+    c = Case(m, n, k, count, rank, "f32", 8, "mixed")
+    index, dy = c.index.cuda(), c.dy.cuda()
+    wt = C.MxMatrix.empty(8, k, n)
+    back = torch.zeros(n, k).cuda()
+    C.costa_mx_dequantize(1.0, c.wq, 0.0, back)
+
+    def f(x, A, B):
+        y = torch.zeros(m, n).cuda()
+        C.costa_mx_product_adapted(1.0, x, c.wq, C.MxAdapters(A, B, c.adapters.ranks, c.adapters.scales), index, 0.0, y)
+        return float((y.double() * dy.double()).sum())
+
+    x, A, B = c.x.cuda(), c.adapters.A, c.adapters.B
+    y, V, dV = torch.zeros(m, n).cuda(), torch.zeros(m, rank).cuda(), torch.zeros(m, rank).cuda()
+    C.costa_mx_product_adapted(1.0, x, c.wq, c.adapters, index, 0.0, y, V=V)
+    dx, dA, dB = torch.zeros_like(x), torch.zeros_like(A), torch.zeros_like(B)
+    C.costa_mx_quantize(1.0, back, None, wt)  # (rounded along n: the product's own part of dx is compared without it)
+    C.costa_mx_product_adapted(0.0, dy, wt, c.adapters.turned(), index, 0.0, dx, V=dV)
+    dx += dy @ back
+    C.costa_mx_adapter_gradient(c.adapters, index, dV, x, 0.0, dA)
+    C.costa_mx_adapter_gradient(c.adapters, index, V, dy, 0.0, dB)
+    base = f(x, A, B)
+    for t, grad in ((x, dx), (A, dA), (B, dB)):
+        for at in range(0, t.numel(), 29):
+            step = torch.zeros_like(t).view(-1)
+            step[at] = 1.0
+            step = step.view(t.shape)
+            moved = f(*(u + step if u is t else u for u in (x, A, B)))
+            assert abs(moved - base - float(grad.reshape(-1)[at])) < 2e-3
+
+
+@pytest.mark.parametrize("m", [20, 90])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_what_is_not_finite_stays_with_its_own_rows(m, dtype):
+    """One adapter full of NaN, one of infinities, rows past their ranks too: other adapters' rows do
+    not see them, nor do rows without an adapter."""
+    n, k, count, rank = 150, 200, 4, 20
+    c = Case(m, n, k, count, rank, dtype, 4, "mixed", ranks=False)
+    c.ranks = torch.tensor([5, 20, 0, 17], dtype=torch.int32)
+    A, B = c.adapters.A, c.adapters.B
+    A[0, 5:], B[0, 5:] = float("nan"), float("inf")
+    A[1], B[3] = float("nan"), float("inf")
+    A[2], B[2] = float("inf"), float("nan")  # (rank 0)
+    A[3, 17:] = float("nan")
+    ad = C.MxAdapters(A, B, c.ranks.cuda(), c.adapters.scales)
+    y, V = torch.zeros(m, n, dtype=TORCH[dtype]).cuda(), torch.zeros(m, rank).cuda()
+    C.costa_mx_product_adapted(1.0, c.x.cuda(), c.wq, ad, c.index.cuda(), 0.0, y, V=V)
+    c.A, c.B = A.cpu(), B.cpu()
+    for a in (1, 3):
+        c.A[a] = c.B[a] = 0
+    c.A[0, 5:] = c.B[0, 5:] = 0
+    c.A[2] = c.B[2] = 0
+    v, ev, want, off = c.forward(1.0, 0.0, dtype)
+    fine = ~np.isin(c.index.numpy(), (1, 3))
+    assert (np.abs(wide(y)[fine] - want[fine]) <= off[fine]).all()
+    assert (np.abs(wide(V)[fine] - v[fine]) <= ev[fine]).all()
+    assert np.isnan(wide(V)[c.rows(1)]).all() and np.isnan(wide(y)[c.rows(1)]).all()
+    assert not np.isfinite(wide(y)[c.rows(3)]).any()
+    # gradients: rows of NaN in Z and V of one adapter
+    z, v = c.x.cuda().clone(), torch.randn(m, rank).cuda()
+    z[torch.from_numpy(c.rows(1))] = float("nan")
+    v[torch.from_numpy(np.flatnonzero(~np.isin(c.index.numpy(), range(count))))] = float("nan")
+    G = torch.zeros(count, rank, k).cuda()
+    C.costa_mx_adapter_gradient(ad, c.index.cuda(), v, z, 0.0, G)
+    g, e = c.gradient(np.nan_to_num(wide(v)), np.nan_to_num(wide(z)))
+    for a in (0, 2, 3):
+        assert (np.abs(wide(G)[a] - g[a]) <= e[a] + TINY["f32"]).all()
+    assert not len(c.rows(1)) or np.isnan(wide(G)[1]).all()
+
+
+def test_nothing_to_do():
+    for m, n, k, count, rank in ((0, 5, 6, 2, 3), (5, 0, 6, 2, 3), (5, 4, 0, 2, 3), (5, 4, 6, 0, 3), (5, 4, 6, 2, 0),
+                                 (100, 4, 0, 2, 3), (100, 4, 6, 0, 3)):
+        x, A, B = torch.ones(m, k).cuda(), torch.ones(count, rank, k).cuda(), torch.ones(count, rank, n).cuda()
+        w = keep(np.ones((n, k), np.float32), 8)
+        index = torch.zeros(m, dtype=torch.int32).cuda()
+        y, V = torch.full((m, n), 3.0).cuda(), torch.full((m, rank), 7.0).cuda()
+        ad = C.MxAdapters(A, B)
+        C.costa_mx_product_adapted(1.0, x, w, ad, index, 2.0, y, V=V)
+        v = float(k if count else 0)
+        assert (V == v).all()
+        assert (y == 6 + k + v * rank).all()
+        G = torch.full((count, rank, k), 5.0).cuda()
+        C.costa_mx_adapter_gradient(ad, index, V, x, 1.0, G)
+        if count:
+            assert (G[0] == 5 + m * v).all() and (G[1:] == 5).all()
+
+
+def test_slices_of_rows():
+    """A sum that does not fit the workspace goes by slices of rows: the same bits as whole."""
+    m, n, k, count, rank = 1100, 300, 256, 3, 16
+    c = Case(m, n, k, count, rank, "bf16", 4, "runs")
+    least, most = C.costa_mx_adapted_workspace(m, n, k, rank)
+    _, _, want, off = c.forward(1.0, 0.0, "bf16")
+    for size in (least, (least + most) // 2, most):
+        y = torch.zeros(m, n, dtype=torch.bfloat16).cuda()
+        ws = torch.empty(size, dtype=torch.uint8).cuda()
+        C.costa_mx_product_adapted(1.0, c.x.cuda(), c.wq, c.adapters, c.index.cuda(), 0.0, y, workspace=ws)
+        assert (np.abs(wide(y) - want) <= off).all()
+
+
+@pytest.mark.parametrize("m", [30, 300])
+def test_on_another_stream_and_in_a_graph(m):
+    n, k, count, rank = 260, 520, 5, 16
+    c = Case(m, n, k, count, rank, "bf16", 4, "mixed")
+    x, dy, index = c.x.cuda(), c.dy.cuda(), c.index.cuda()
+    y, V, G = torch.zeros(m, n).cuda(), torch.zeros(m, rank).cuda(), torch.zeros(count, rank, n).cuda()
+    ws = torch.empty(C.costa_mx_adapted_workspace(m, n, k, rank)[1], dtype=torch.uint8, device="cuda")
+    ws2 = torch.empty(C.costa_mx_adapter_gradient_workspace(m, n, count, rank)[1], dtype=torch.uint8, device="cuda")
+
+    def both(stream=None):
+        C.costa_mx_product_adapted(1.0, x, c.wq, c.adapters, index, 0.0, y, V=V, workspace=ws, stream=stream)
+        C.costa_mx_adapter_gradient(c.adapters, index, V, dy, 0.0, G, workspace=ws2, stream=stream)
+
+    both()
+    want = [t.clone() for t in (y, V, G)]
+    side = torch.cuda.Stream()
+    for t in (y, V, G):
+        t.zero_()
+    torch.cuda.synchronize()
+    both(side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, (y, V, G)))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        both()
+    for k in range(3):
+        x.normal_()
+        index.random_(-1, count)
+        for t in (y, V, G):
+            t.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (y, V, G)]
+        both()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, (y, V, G)))
