@@ -1,7 +1,8 @@
 /*
  * costa_layer.h -- what stands around the products of a layer whose weights are
- * kept in few bits (costa_mx.h): the norm that makes a product's operand and low-rank
- * adapters beside a product, each with its gradients.
+ * kept in few bits (costa_mx.h): the norm that makes a product's operand, low-rank
+ * adapters beside a product, and the loss behind the last one; each with its
+ * gradients.
  *
  * Conventions are those of costa_mx.h: calls are asynchronous on `stream`, on the
  * current device; every argument error is returned before anything is enqueued; the
@@ -96,6 +97,33 @@ costa_status costa_mx_adapter_gradient(const costa_mx_adapters* adapters, const 
                                        hipStream_t stream);
 costa_status costa_mx_adapter_gradient_workspace(int64_t m, int64_t len, int32_t count, int32_t rank, size_t* least,
                                                  size_t* most);
+
+/* ---- softmax cross entropy over a vocabulary -------------------------------
+ *
+ *     L = alpha X W^^T,  lse_i = log sum_j exp(L_ij),  loss_i = lse_i - L_i,target(i)
+ *
+ * X m x k, W n x k (n: the vocabulary), target, loss, lse: m entries.  A row whose target
+ * is not in 0 .. n-1 does not count: its loss is 0.  L is not kept. */
+costa_status costa_mx_loss(float alpha, const costa_matrix* X, const costa_mx* W, const int64_t* target, float* loss,
+                           float* lse, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* The gradients, by pieces of the vocabulary:
+ *
+ *     G_ij = dloss_i (exp(L_ij - lse_i) - [j = target(i)]),  0 in rows that do not count
+ *     dX <- alpha G W'^          W' = WT^T, WT = mx(W^T), k x n
+ *     dW <- alpha G^T X'^ + beta dW    X' = XT^T, XT = mx(X^T), k x m
+ *
+ * dloss (NULL: ones): m floats, the gradient that reaches each row's loss.  dX with WT and dW
+ * with XT may be NULL, not both.  lse: what costa_mx_loss() gave.  G is held in
+ * bfloat16 where dX and dW (those wanted) are BF16, in 32 bits else; probabilities below
+ * 2^-126 are 0. */
+costa_status costa_mx_loss_backward(float alpha, const costa_matrix* X, const costa_mx* W, const int64_t* target,
+                                    const float* lse, const float* dloss, const costa_mx* WT, const costa_matrix* dX,
+                                    const costa_mx* XT, float beta, const costa_matrix* dW, void* workspace,
+                                    size_t workspace_bytes, hipStream_t stream);
+
+/* Workspace of costa_mx_loss() (backward == 0) and costa_mx_loss_backward(). */
+costa_status costa_mx_loss_workspace(int64_t m, int64_t n, int64_t k, int backward, size_t* least, size_t* most);
 
 #ifdef __cplusplus
 }

@@ -142,6 +142,11 @@ _SIGS = {
     "costa_mx_adapted_workspace": [_i64, _i64, _i64, _i32, _P(ctypes.c_size_t), _P(ctypes.c_size_t)],
     "costa_mx_adapter_gradient": [_P(CostaMxAdapters), _vp, _P(CostaMatrix), _P(CostaMatrix), ctypes.c_float,
                                   _P(CostaMatrix), _vp, ctypes.c_size_t, _vp],
+    "costa_mx_loss": [ctypes.c_float, _P(CostaMatrix), _P(CostaMx), _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp],
+    "costa_mx_loss_backward": [ctypes.c_float, _P(CostaMatrix), _P(CostaMx), _vp, _vp, _vp, _P(CostaMx),
+                               _P(CostaMatrix), _P(CostaMx), ctypes.c_float, _P(CostaMatrix), _vp, ctypes.c_size_t,
+                               _vp],
+    "costa_mx_loss_workspace": [_i64, _i64, _i64, ctypes.c_int, _P(ctypes.c_size_t), _P(ctypes.c_size_t)],
     "costa_mx_adapter_gradient_workspace": [_i64, _i64, _i32, _i32, _P(ctypes.c_size_t), _P(ctypes.c_size_t)],
 }
 for _name, _args in _SIGS.items():
@@ -779,6 +784,35 @@ def costa_mx_adapter_gradient(adapters: MxAdapters, index, V, Z, beta: float, G,
     _check(_lib.costa_mx_adapter_gradient(adapters._ref, _vector(index, torch.int32, m, "index"), _matrix(V),
                                           _matrix(Z), beta, _matrix(G.flatten(0, 1)), at, size, _stream(stream)),
            "costa_mx_adapter_gradient")
+
+
+def costa_mx_loss_workspace(m: int, n: int, k: int, backward: bool):
+    """(least, most) bytes of costa_mx_loss() or costa_mx_loss_backward()."""
+    return _two_sizes("costa_mx_loss_workspace", m, n, k, 1 if backward else 0)
+
+
+def costa_mx_loss(alpha: float, X, W: MxMatrix, target, loss, lse, workspace=None, stream=None) -> None:
+    """L = alpha X W^^T, lse <- log sum exp L, loss <- lse - L_target of each row (0 where the target, an int64,
+    is none of W's rows)."""
+    m, k = X.shape
+    need = 0 if workspace is not None else costa_mx_loss_workspace(m, W.rows, k, False)[1]
+    at, size, _keep = _workspace(need, workspace, X.device, stream)
+    _check(_lib.costa_mx_loss(alpha, _matrix(X), _mx(W), _vector(target, torch.int64, m, "target"),
+                              _vector(loss, torch.float32, m, "loss"), _vector(lse, torch.float32, m, "lse"), at, size,
+                              _stream(stream)), "costa_mx_loss")
+
+
+def costa_mx_loss_backward(alpha: float, X, W: MxMatrix, target, lse, dloss=None, WT: Optional[MxMatrix] = None, dX=None,
+                           XT: Optional[MxMatrix] = None, dW=None, beta: float = 0.0, workspace=None,
+                           stream=None) -> None:
+    """With G = dloss (exp(L - lse) - [target]): dX <- alpha G WT^^T, dW <- alpha G^T XT^^T + beta dW, one or both."""
+    m, k = X.shape
+    need = 0 if workspace is not None else costa_mx_loss_workspace(m, W.rows, k, True)[1]
+    at, size, _keep = _workspace(need, workspace, X.device, stream)
+    _check(_lib.costa_mx_loss_backward(alpha, _matrix(X), _mx(W), _vector(target, torch.int64, m, "target"),
+                                       _vector(lse, torch.float32, m, "lse"),
+                                       _vector(dloss, torch.float32, m, "dloss"), _mx(WT), _opt(dX), _mx(XT), beta,
+                                       _opt(dW), at, size, _stream(stream)), "costa_mx_loss_backward")
 
 
 def costa_set_workspace_limit(nbytes: int) -> None:

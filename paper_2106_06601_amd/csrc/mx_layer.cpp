@@ -345,3 +345,212 @@ extern "C" costa_status costa_mx_adapter_gradient_workspace(int64_t m, int64_t l
     return COSTA_SUCCESS;
   });
 }
+
+namespace costa {
+namespace {
+
+constexpr int64_t kPieceColumns = 256;  // pieces of the vocabulary are multiples: blocks and rows of few-bit matrices stay whole
+constexpr size_t kPieceBytes = (size_t)256 << 20;  // of what a piece keeps of every row and column
+
+int64_t chunks_of(int64_t n) { return (n + kLossChunk - 1) / kLossChunk; }
+
+// Columns of a piece, with `bytes` of memory for `elem` bytes of each of its m x columns
+// elements: whole chunks if there is room.  At least kPieceColumns (the caller has asked for as much).
+int64_t piece_columns(int64_t m, int64_t n, size_t bytes, size_t elem) {
+  const size_t most = bytes / ((size_t)std::max<int64_t>(m, 1) * elem);
+  if (most >= (size_t)n) return n;
+  const int64_t to = most >= (size_t)kLossChunk ? kLossChunk : kPieceColumns;
+  return std::max<int64_t>((int64_t)most / to * to, kPieceColumns);
+}
+size_t piece_bytes(int64_t m, int64_t n, size_t elem) {
+  return (size_t)m * (size_t)std::min<int64_t>(n, std::max<int64_t>(piece_columns(m, n, kPieceBytes, elem), kPieceColumns)) * elem;
+}
+size_t least_piece(int64_t m, int64_t n, size_t elem) { return (size_t)m * std::min(n, kPieceColumns) * elem; }
+
+MxView columns_of(const MxView& q, int64_t first, int64_t n) {  // first: a multiple of 256
+  MxView v = q;
+  v.data += first * q.bits / 8;
+  v.scales += first / kMxBlock;
+  v.cols = n;
+  return v;
+}
+MxView rows_of(const MxView& q, int64_t first, int64_t n) {
+  MxView v = q;
+  v.data += first * q.row_bytes;
+  v.scales += first * q.row_scales;
+  v.rows = n;
+  return v;
+}
+
+// Chunks of columns whose statistics a call keeps: a piece of fewer columns than a chunk makes
+// a chunk of its own.
+int64_t chunks_kept(int64_t n, int64_t per) { return (n + per - 1) / per * chunks_of(std::min(n, per)); }
+
+// What both calls check; `w` and the row's vectors.
+costa_status check_loss(const costa_matrix* X, const costa_mx* W, const int64_t* target, MxView& w) {
+  CHECKED(check_rows("X", X));
+  CHECKED(check_mx("W", W, w));
+  if (W->cols != X->cols) return fail(COSTA_ERROR_SHAPE_MISMATCH, "X and W have different lengths to sum over");
+  return check_vector("target", target, X->rows, 8);
+}
+
+ProductArgs logits_of(const costa_matrix* X, const MxView& w, int64_t first, int64_t n) {
+  ProductArgs p{};
+  p.m = X->rows, p.n = n, p.k = X->cols;
+  p.real = X->data;
+  p.a_rs = X->ld, p.a_cs = 1, p.a_type = X->type;
+  p.b = rows_of(w, first, n);
+  return p;
+}
+
+}  // namespace
+}  // namespace costa
+
+extern "C" costa_status costa_mx_loss_workspace(int64_t m, int64_t n, int64_t k, int backward, size_t* least,
+                                                size_t* most) {
+  return guarded([&]() -> costa_status {
+    CHECKED(check_dims("logits", m, n));
+    CHECKED(check_dims("X", m, k));
+    if (m == 0) {
+      give(least, 0), give(most, 0);
+    } else if (!backward) {
+      const size_t at = up16((size_t)m * 4);
+      give(least, at + up16((size_t)m * chunks_kept(n, kPieceColumns) * sizeof(LossStat)) + least_piece(m, n, 4));
+      const size_t sums = piece_bytes(m, n, 4);
+      give(most, at + up16((size_t)m * chunks_kept(n, kPieceColumns) * sizeof(LossStat)) +
+                     std::max(sums, mx_product_workspace(m, std::min(n, piece_columns(m, n, sums, 4)), k)));
+    } else {
+      const size_t dx = up16((size_t)m * k * 4);  // what dX is summed in
+      give(least, dx + up16(least_piece(m, n, 4)) + up16(least_piece(m, n, 4)));
+      const size_t g = piece_bytes(m, n, 4);
+      const int64_t per = piece_columns(m, n, g, 4);
+      give(most, dx + up16(g) + std::max({up16(g), mx_product_workspace(m, per, k), mx_product_workspace(m, k, per),
+                                          mx_product_workspace(per, k, m)}));
+    }
+    return COSTA_SUCCESS;
+  });
+}
+
+extern "C" costa_status costa_mx_loss(float alpha, const costa_matrix* X, const costa_mx* W, const int64_t* target,
+                                      float* loss, float* lse, void* workspace, size_t workspace_bytes,
+                                      hipStream_t stream) {
+  return guarded([&]() -> costa_status {
+    MxView w;
+    CHECKED(check_loss(X, W, target, w));
+    const int64_t m = X->rows, n = W->rows, k = X->cols;
+    CHECKED(check_vector("loss", loss, m, 4));
+    CHECKED(check_vector("lse", lse, m, 4));
+    size_t least = 0;
+    CHECKED(costa_mx_loss_workspace(m, n, k, 0, &least, nullptr));
+    CHECKED(check_workspace(workspace, workspace_bytes, least));
+    Uses u;
+    u.add("X", X, false), u.add("W", w, false), u.add("target", target, m * 8, false);
+    u.add("loss", loss, m * 4, true), u.add("lse", lse, m * 4, true), u.workspace(workspace, workspace_bytes);
+    CHECKED(u.check());
+    if (m == 0) return COSTA_SUCCESS;
+    char* room = static_cast<char*>(workspace);
+    float* const at = reinterpret_cast<float*>(room);
+    room += up16((size_t)m * 4);
+    LossStat* const stats = reinterpret_cast<LossStat*>(room);
+    room += up16((size_t)m * chunks_kept(n, kPieceColumns) * sizeof(LossStat));
+    const size_t left = workspace_bytes - (size_t)(room - static_cast<char*>(workspace));
+    const int64_t per = n == 0 ? 1 : piece_columns(m, n, std::min(left, piece_bytes(m, n, 4)), 4);
+    int64_t chunks = 0;
+    for (int64_t j = 0; j < n; j += per) {
+      const int64_t cols = std::min(per, n - j);
+      LogitsPart l{m, cols, j, reinterpret_cast<float*>(room), 0, alpha, target};
+      if (k > 0) {
+        ProductArgs p = logits_of(X, w, j, cols);
+        p.workspace = reinterpret_cast<float*>(room), p.workspace_bytes = left;
+        HIP_OR_FAIL(launch_mx_product_parts(p, l.splits, stream));
+      }
+      HIP_OR_FAIL(launch_mx_loss_stats(l, stats + chunks * m, at, stream));
+      chunks += chunks_of(cols);
+    }
+    HIP_OR_FAIL(launch_mx_loss_join(m, n, chunks, stats, at, target, loss, lse, stream));
+    return COSTA_SUCCESS;
+  });
+}
+
+extern "C" costa_status costa_mx_loss_backward(float alpha, const costa_matrix* X, const costa_mx* W,
+                                               const int64_t* target, const float* lse, const float* dloss,
+                                               const costa_mx* WT, const costa_matrix* dX, const costa_mx* XT,
+                                               float beta, const costa_matrix* dW, void* workspace,
+                                               size_t workspace_bytes, hipStream_t stream) {
+  return guarded([&]() -> costa_status {
+    MxView w, wt{}, xt{};
+    CHECKED(check_loss(X, W, target, w));
+    const int64_t m = X->rows, n = W->rows, k = X->cols;
+    CHECKED(check_vector("lse", lse, m, 4));
+    if (dloss) CHECKED(check_vector("dloss", dloss, m, 4));
+    if (!dX && !dW) return fail(COSTA_ERROR_INVALID_VALUE, "neither dX nor dW");
+    if (dX) {
+      CHECKED(check_rows("dX", dX));
+      CHECKED(check_mx("WT", WT, wt));
+      if (dX->rows != m || dX->cols != k) return fail(COSTA_ERROR_SHAPE_MISMATCH, "dX is not the shape of X");
+      if (WT->rows != k || WT->cols != n) return fail(COSTA_ERROR_SHAPE_MISMATCH, "WT is not the shape of the transposed W");
+    }
+    if (dW) {
+      CHECKED(check_rows("dW", dW));
+      CHECKED(check_mx("XT", XT, xt));
+      if (dW->rows != n || dW->cols != k) return fail(COSTA_ERROR_SHAPE_MISMATCH, "dW is not the shape of W");
+      if (XT->rows != k || XT->cols != m) return fail(COSTA_ERROR_SHAPE_MISMATCH, "XT is not the shape of the transposed X");
+    }
+    size_t least = 0;
+    CHECKED(costa_mx_loss_workspace(m, n, k, 1, &least, nullptr));
+    CHECKED(check_workspace(workspace, workspace_bytes, least));
+    Uses u;
+    u.add("X", X, false), u.add("W", w, false), u.add("WT", wt, false), u.add("XT", xt, false);
+    u.add("target", target, m * 8, false), u.add("lse", lse, m * 4, false), u.add("dloss", dloss, m * 4, false);
+    u.add("dX", dX, true), u.add("dW", dW, true), u.workspace(workspace, workspace_bytes);
+    CHECKED(u.check());
+    if (k == 0) return COSTA_SUCCESS;  // no gradient has elements
+    auto product = [&](bool turned, const void* g, bool bf16, int64_t gm, int64_t gn, const MxView& b, float al, float be,
+                       void* c, int64_t ld, costa_real type, char* room, size_t bytes) {
+      ProductArgs p{};  // of G (gm x gn), turned or not
+      p.m = turned ? gn : gm, p.k = turned ? gm : gn, p.n = b.rows;
+      p.real = g;
+      p.a_rs = turned ? 1 : gn, p.a_cs = turned ? gn : 1;
+      p.a_type = bf16 ? COSTA_REAL_BF16 : COSTA_REAL_F32;
+      p.b = b;
+      p.c = c, p.c_rs = ld, p.c_cs = 1, p.c_type = type;
+      p.alpha = al, p.beta = be;
+      p.workspace = reinterpret_cast<float*>(room), p.workspace_bytes = bytes;
+      return p.m == 0 || p.n == 0 ? hipSuccess : launch_mx_product(p, stream);
+    };
+    if (m == 0 || n == 0) {  // sums over nothing
+      if (dX) HIP_OR_FAIL(product(false, nullptr, true, m, 0, columns_of(wt, 0, 0), alpha, 0.0f, dX->data, dX->ld, dX->type, nullptr, 0));
+      if (dW) HIP_OR_FAIL(product(true, nullptr, true, 0, n, columns_of(xt, 0, 0), alpha, beta, dW->data, dW->ld, dW->type, nullptr, 0));
+      return COSTA_SUCCESS;
+    }
+    const bool bf16 = (!dX || dX->type == COSTA_REAL_BF16) && (!dW || dW->type == COSTA_REAL_BF16);
+    char* room = static_cast<char*>(workspace);
+    float* const sum = reinterpret_cast<float*>(room);  // of dX
+    room += up16((size_t)m * k * 4);
+    size_t left = workspace_bytes - up16((size_t)m * k * 4);
+    // half for G, half for the logits and for what products split
+    const int64_t per = piece_columns(m, n, std::min(left / 32 * 16, piece_bytes(m, n, 4)), 4);
+    void* const g = room;
+    const size_t taken = up16((size_t)m * per * 4);
+    room += taken, left -= taken;
+    const bool whole = per >= n;
+    for (int64_t j = 0; j < n; j += per) {
+      const int64_t cols = std::min(per, n - j);
+      ProductArgs p = logits_of(X, w, j, cols);
+      p.workspace = reinterpret_cast<float*>(room), p.workspace_bytes = left;
+      LogitsPart l{m, cols, j, p.workspace, 0, alpha, target};
+      HIP_OR_FAIL(launch_mx_product_parts(p, l.splits, stream));
+      HIP_OR_FAIL(launch_mx_loss_grad(l, n, lse, dloss, g, bf16, stream));
+      if (dX) {
+        const bool direct = whole || dX->type == COSTA_REAL_F32;
+        HIP_OR_FAIL(product(false, g, bf16, m, cols, columns_of(wt, j, cols), alpha, j > 0 ? 1.0f : 0.0f,
+                            direct ? dX->data : sum, direct ? dX->ld : k, direct ? dX->type : COSTA_REAL_F32, room, left));
+      }
+      if (dW)
+        HIP_OR_FAIL(product(true, g, bf16, m, cols, xt, alpha, beta,
+                            static_cast<char*>(dW->data) + j * dW->ld * real_size(dW->type), dW->ld, dW->type, room, left));
+    }
+    if (dX && !whole && dX->type != COSTA_REAL_F32) HIP_OR_FAIL(launch_mx_round(m, k, sum, rows_of(dX), dX->type, stream));
+    return COSTA_SUCCESS;
+  });
+}

@@ -93,4 +93,31 @@ struct AdapterGradArgs {
 int64_t mx_adapter_grad_parts(int64_t m, int64_t len, int32_t count, int32_t rank);
 hipError_t launch_mx_adapter_grad(const AdapterGradArgs& a, hipStream_t stream);
 
+// ---- loss (mx_loss.hip) -----------------------------------------------------------
+// Largest logit and the sum of exponentials from it, of a row's columns of one chunk:
+// stats[chunk * m + row].
+struct LossStat {
+  float top, sum;
+};
+constexpr int64_t kLossChunk = 2048;  // columns of a chunk where logits are in memory
+
+// The logits of columns col0 .. col0 + n - 1: alpha * the sum of `splits` parts of m x n floats.
+struct LogitsPart {
+  int64_t m, n, col0;
+  const float* sums;
+  int32_t splits;
+  float alpha;
+  const int64_t* target;
+};
+// stats: of col0's chunk; at: the target's logits, of rows whose target is among the columns.
+hipError_t launch_mx_loss_stats(const LogitsPart& p, LossStat* stats, float* at, hipStream_t stream);
+// From the stats of all chunks.  n: the vocabulary.
+hipError_t launch_mx_loss_join(int64_t m, int64_t n, int64_t chunks, const LossStat* stats, const float* at,
+                               const int64_t* target, float* loss, float* lse, hipStream_t stream);
+// g (m x p.n by rows; bfloat16 or float) <- dloss (exp(logit - lse) - [target]); g may be the first part of sums
+hipError_t launch_mx_loss_grad(const LogitsPart& p, int64_t vocabulary, const float* lse, const float* dloss, void* g,
+                               bool bf16, hipStream_t stream);
+// y <- x: floats, to a row-major matrix
+hipError_t launch_mx_round(int64_t m, int64_t n, const float* x, const RowsView& y, costa_real type, hipStream_t stream);
+
 }  // namespace costa
