@@ -1,0 +1,240 @@
+"""The operators around products without a GPU: exported symbols, workspaces, and what each
+call refuses before any device work."""
+import ctypes
+import os
+import re
+
+import pytest
+
+C = pytest.importorskip("paper_2106_06601_amd")
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+F64, F32, BF16, F16 = range(4)
+COL, ROW = 0, 1
+BAD, SHAPE, NOT = C.INVALID_VALUE, C.SHAPE_MISMATCH, C.NOT_SUPPORTED
+EPS = 1e-5
+ref = lambda a: None if a is None else ctypes.byref(a)  # noqa: E731
+at = lambda k: k << 32  # noqa: E731  (addresses that no refused call reads, 4 GiB apart)
+
+
+def M(rows, cols, where, type=F32, order=ROW, ld=None, data=True):
+    return C.CostaMatrix(type, order, rows, cols, cols if ld is None else ld, at(where) if data is True else data)
+
+
+def Q(rows, cols, where, fmt=1, **how):
+    return C.CostaMx(fmt, rows, cols, how.get("data", at(where)), how.get("scales", at(where) + (1 << 31)))
+
+
+def test_every_declared_symbol_is_exported():
+    header = open(os.path.join(ROOT, "include", "costa_layer.h")).read()
+    names = set(re.findall(r"^\s*costa_status\s+(costa_\w+)\s*\(", header, re.M))
+    assert names == {"costa_mx_norm", "costa_mx_norm_backward", "costa_mx_norm_workspace", "costa_mx_product_adapted",
+                     "costa_mx_adapted_workspace", "costa_mx_adapter_gradient", "costa_mx_adapter_gradient_workspace",
+                     "costa_mx_loss", "costa_mx_loss_backward", "costa_mx_loss_workspace"}
+    assert not [n for n in sorted(names) if not hasattr(C._lib, n)]
+    assert names <= set(C._SIGS)
+
+
+# ---- each call with good arguments; a test changes some of them ----------------
+def norm(eps=EPS, X=None, W=None, R=None, H=None, Y=None, Qm=None, rstd=None, m=4, n=40, type=F32):
+    X = X or M(m, n, 1, type)
+    return C._lib.costa_mx_norm(eps, ref(X), ref(W), ref(R), ref(H), ref(Y), ref(Qm), rstd, None)
+
+
+def back(dY=None, H=None, W=None, rstd=at(4), dH=None, dX=None, dW=None, ws=at(9), size=1 << 20, m=4, n=40, type=F32):
+    dY, H, dX = dY or M(m, n, 1, type), H or M(m, n, 2, type), dX or M(m, n, 6, type)
+    return C._lib.costa_mx_norm_backward(ref(dY), ref(H), ref(W), rstd, ref(dH), ref(dX), ref(dW), ws, size, None)
+
+
+def ads(count=3, rank=5, k=30, n=40, type=F32, A=None, B=None, ranks=None, scales=None):
+    A, B = A or M(count * rank, k, 3, type), B or M(count * rank, n, 4, type)
+    return C.CostaMxAdapters(count, rank, ctypes.pointer(A), ctypes.pointer(B), ranks, scales)
+
+
+def adapted(X=None, W=None, a=None, index=at(5), Cm=None, V=None, ws=at(9), size=1 << 24, m=4, n=40, k=30, type=F32):
+    X, W, Cm = X or M(m, k, 1, type), W or Q(n, k, 2), Cm or M(m, n, 6, type)
+    return C._lib.costa_mx_product_adapted(1.0, ref(X), ref(W), ref(a or ads(type=type)), index, 0.0, ref(Cm), ref(V), ws, size,
+                                           None)
+
+
+def grad(a=None, index=at(5), V=None, Z=None, G=None, ws=at(9), size=1 << 24, m=4, n=30):
+    V, Z, G = V or M(m, 5, 1), Z or M(m, n, 2), G or M(15, n, 6)
+    return C._lib.costa_mx_adapter_gradient(ref(a or ads()), index, ref(V), ref(Z), 0.0, ref(G), ws, size, None)
+
+
+def loss(X=None, W=None, target=at(3), out=at(4), lse=at(5), ws=at(9), size=1 << 24, m=4, n=40, k=30):
+    X, W = X or M(m, k, 1), W or Q(n, k, 2)
+    return C._lib.costa_mx_loss(1.0, ref(X), ref(W), target, out, lse, ws, size, None)
+
+
+def lossback(X=None, W=None, target=at(3), lse=at(5), d=None, WT=None, dX=None, XT=None, dW=None, ws=at(9), size=1 << 24, m=4,
+             n=40, k=30):
+    X, W = X or M(m, k, 1), W or Q(n, k, 2)
+    return C._lib.costa_mx_loss_backward(1.0, ref(X), ref(W), target, lse, d, ref(WT), ref(dX), ref(XT), 0.0, ref(dW), ws, size,
+                                         None)
+
+
+Y = lambda **h: M(4, 40, 8, **h)  # noqa: E731
+
+
+@pytest.mark.parametrize("eps", [0.0, -1e-5, float("inf"), float("nan"), 1e-39])
+def test_norms_need_a_positive_eps(eps):
+    assert norm(eps, Y=Y()) == BAD
+
+
+@pytest.mark.parametrize("how,status", [
+    (dict(), BAD),  # no result
+    (dict(X=M(4, 40, 1, F64), Y=Y()), NOT), (dict(X=M(4, 40, 1, order=COL), Y=Y()), NOT),
+    (dict(X=M(4, 40, 1, ld=39), Y=Y()), BAD), (dict(X=M(4, 40, 1, data=None), Y=Y()), BAD), (dict(X=M(-4, 40, 1), Y=Y()), BAD),
+    (dict(Y=M(5, 40, 8)), SHAPE), (dict(Y=M(4, 39, 8)), SHAPE), (dict(Y=Y(type=BF16)), BAD), (dict(Y=Y(data=at(8) + 2)), BAD),
+    (dict(H=M(4, 41, 8)), SHAPE), (dict(H=Y(type=F16)), BAD), (dict(R=M(3, 40, 2), Y=Y()), SHAPE),
+    (dict(R=M(4, 40, 2, BF16), Y=Y()), BAD), (dict(W=M(1, 39, 2), Y=Y()), SHAPE), (dict(W=M(40, 1, 2), Y=Y()), SHAPE),
+    (dict(W=M(1, 40, 2, BF16), Y=Y()), BAD), (dict(Qm=Q(4, 41, 8)), SHAPE), (dict(Qm=Q(4, 40, 8, fmt=5)), BAD),
+    (dict(Qm=Q(4, 40, 8, data=at(8) + 8)), BAD), (dict(rstd=at(8) + 2), BAD),
+    # overlaps
+    (dict(Y=M(4, 40, 1)), BAD), (dict(H=Y(), Y=Y()), BAD), (dict(H=M(4, 40, 1, ld=41)), BAD), (dict(H=M(4, 40, 1, data=at(1) + 4)), BAD),
+    (dict(R=M(4, 40, 2), Y=M(4, 40, 2)), BAD), (dict(W=M(1, 40, 2), Y=M(4, 40, 2)), BAD), (dict(Y=Y(), rstd=at(8)), BAD),
+    (dict(rstd=at(1) + 8), BAD), (dict(Qm=Q(4, 40, 1)), BAD), (dict(Y=Y(), Qm=Q(4, 40, 8)), BAD),
+    (dict(Qm=Q(4, 40, 7, scales=at(7))), BAD)])
+def test_norms_that_are_refused(how, status):
+    assert norm(**how) == status
+    assert C.costa_last_error()
+
+
+@pytest.mark.parametrize("how,status", [
+    (dict(dY=M(4, 40, 1, F64)), NOT), (dict(dY=M(4, 40, 1, order=COL)), NOT), (dict(H=M(4, 41, 2)), SHAPE),
+    (dict(H=M(4, 40, 2, BF16)), BAD), (dict(W=M(1, 41, 3)), SHAPE), (dict(W=M(1, 40, 3, F16)), BAD), (dict(rstd=None), BAD),
+    (dict(rstd=at(4) + 1), BAD), (dict(dH=M(4, 41, 5)), SHAPE), (dict(dX=M(3, 40, 6)), SHAPE), (dict(dX=M(4, 40, 6, BF16)), BAD),
+    (dict(dW=M(1, 39, 7)), SHAPE), (dict(dW=M(1, 40, 7, BF16)), BAD), (dict(dW=M(1, 40, 7), ws=None, size=0), BAD),
+    (dict(dW=M(1, 40, 7), size=639), BAD), (dict(dW=M(1, 40, 7), ws=at(9) + 4), BAD),
+    (dict(dX=M(4, 40, 2)), BAD), (dict(dX=M(4, 40, 1, ld=41)), BAD), (dict(dX=M(4, 40, 4)), BAD), (dict(dW=M(1, 40, 6)), BAD),
+    (dict(dW=M(1, 40, 1)), BAD), (dict(dW=M(1, 40, 7), ws=at(7)), BAD), (dict(dW=M(1, 40, 7), ws=at(2)), BAD)])
+def test_norm_gradients_that_are_refused(how, status):
+    assert back(**how) == status
+    assert C.costa_last_error()
+
+
+@pytest.mark.parametrize("how,status", [
+    (dict(X=M(4, 30, 1, F64)), NOT), (dict(X=M(4, 30, 1, order=COL)), NOT), (dict(W=Q(40, 31, 2)), SHAPE), (dict(W=Q(40, 30, 2, fmt=3)), BAD),
+    (dict(index=None), BAD), (dict(index=at(5) + 2), BAD), (dict(Cm=M(4, 41, 6)), SHAPE), (dict(Cm=M(4, 40, 6, F64)), NOT),
+    (dict(Cm=M(4, 40, 6, order=COL)), NOT), (dict(V=M(4, 6, 7)), SHAPE), (dict(V=M(4, 5, 7, BF16)), BAD), (dict(ws=None), BAD),
+    (dict(size=100), BAD), (dict(ws=at(9) + 8), BAD), (dict(a=ads(count=-1)), BAD), (dict(a=ads(rank=-1)), BAD),
+    (dict(a=ads(rank=257)), NOT), (dict(a=ads(count=1 << 24, rank=256)), NOT), (dict(a=ads(k=31)), SHAPE), (dict(a=ads(n=41)), SHAPE),
+    (dict(a=ads(A=M(14, 30, 3))), SHAPE), (dict(a=ads(A=M(15, 30, 3, BF16))), BAD), (dict(a=ads(B=M(15, 40, 4, F16))), BAD),
+    (dict(a=ads(ranks=at(7) + 1)), BAD), (dict(a=ads(scales=at(7) + 2)), BAD),
+    (dict(Cm=M(4, 40, 1)), BAD), (dict(Cm=M(4, 40, 2)), BAD), (dict(Cm=M(4, 40, 3)), BAD), (dict(Cm=M(4, 40, 4)), BAD),
+    (dict(Cm=M(4, 40, 5)), BAD), (dict(V=M(4, 5, 6)), BAD), (dict(V=M(4, 5, 5)), BAD), (dict(ws=at(1)), BAD), (dict(ws=at(3)), BAD),
+    (dict(a=ads(ranks=at(6))), BAD), (dict(a=ads(scales=at(9) + 16)), BAD), (dict(ws=at(6)), BAD)])
+def test_adapted_products_that_are_refused(how, status):
+    assert adapted(**how) == status
+    assert C.costa_last_error()
+
+
+def test_adapters_that_are_missing():
+    A = M(15, 30, 3)
+    for a in (C.CostaMxAdapters(3, 5, None, ctypes.pointer(A), None, None), C.CostaMxAdapters(3, 5, ctypes.pointer(A), None, None, None)):
+        assert adapted(a=a) == BAD
+    assert C._lib.costa_mx_product_adapted(1.0, ref(M(4, 30, 1)), ref(Q(40, 30, 2)), None, at(5), 0.0, ref(M(4, 40, 6)), None, at(9),
+                                           1 << 24, None) == BAD
+    assert C._lib.costa_mx_adapter_gradient(None, at(5), ref(M(4, 5, 1)), ref(M(4, 30, 2)), 0.0, ref(M(15, 30, 6)), at(9), 1 << 24,
+                                            None) == BAD
+
+
+@pytest.mark.parametrize("how,status", [
+    (dict(Z=M(4, 30, 2, F64)), NOT), (dict(Z=M(4, 30, 2, order=COL)), NOT), (dict(V=M(4, 6, 1)), SHAPE), (dict(V=M(3, 5, 1)), SHAPE),
+    (dict(V=M(4, 5, 1, BF16)), BAD), (dict(G=M(14, 30, 6)), SHAPE), (dict(G=M(15, 31, 6)), SHAPE), (dict(G=M(15, 30, 6, F64)), NOT),
+    (dict(index=None), BAD), (dict(ws=None), BAD), (dict(size=15 * 30 * 4 - 1), BAD), (dict(ws=at(9) + 4), BAD), (dict(G=M(15, 30, 1)), BAD),
+    (dict(G=M(15, 30, 2)), BAD), (dict(G=M(15, 30, 5)), BAD), (dict(ws=at(6)), BAD), (dict(ws=at(2)), BAD),
+    (dict(a=ads(scales=at(6))), BAD)])
+def test_adapter_gradients_that_are_refused(how, status):
+    assert grad(**how) == status
+    assert C.costa_last_error()
+
+
+@pytest.mark.parametrize("how,status", [
+    (dict(X=M(4, 30, 1, F64)), NOT), (dict(X=M(4, 30, 1, order=COL)), NOT), (dict(W=Q(40, 29, 2)), SHAPE), (dict(target=None), BAD),
+    (dict(target=at(3) + 4), BAD), (dict(out=None), BAD), (dict(out=at(4) + 2), BAD), (dict(lse=None), BAD), (dict(ws=None), BAD),
+    (dict(size=64), BAD), (dict(ws=at(9) + 8), BAD), (dict(out=at(5)), BAD), (dict(out=at(3)), BAD), (dict(lse=at(1) + 4), BAD),
+    (dict(lse=at(2)), BAD), (dict(ws=at(3)), BAD), (dict(ws=at(1)), BAD), (dict(ws=at(4)), BAD)])
+def test_losses_that_are_refused(how, status):
+    assert loss(**how) == status
+    assert C.costa_last_error()
+
+
+GX, GW = dict(WT=Q(30, 40, 6), dX=M(4, 30, 7)), dict(XT=Q(30, 4, 8), dW=M(40, 30, 10))
+
+
+@pytest.mark.parametrize("how,status", [
+    (dict(), BAD), (dict(GX, WT=None), BAD), (dict(GW, XT=None), BAD), (dict(GX, WT=Q(30, 41, 6)), SHAPE), (dict(GX, WT=Q(40, 30, 6)), SHAPE),
+    (dict(GX, dX=M(4, 31, 7)), SHAPE), (dict(GX, dX=M(4, 30, 7, F64)), NOT), (dict(GX, dX=M(4, 30, 7, order=COL)), NOT),
+    (dict(GW, XT=Q(30, 5, 8)), SHAPE), (dict(GW, dW=M(30, 40, 10)), SHAPE), (dict(GW, dW=M(40, 30, 10, order=COL, ld=40)), NOT),
+    (dict(GX, lse=None), BAD), (dict(GX, lse=at(5) + 1), BAD), (dict(GX, d=at(11) + 2), BAD), (dict(GX, target=None), BAD),
+    (dict(GX, ws=None), BAD), (dict(GX, size=1000), BAD), (dict(GX, ws=at(9) + 2), BAD),
+    (dict(GX, dX=M(4, 30, 1)), BAD), (dict(GX, dX=M(4, 30, 2)), BAD), (dict(GX, dX=M(4, 30, 6)), BAD), (dict(GX, dX=M(4, 30, 5)), BAD),
+    (dict(GX, d=at(7)), BAD), (dict(GX, **dict(GW, dW=M(40, 30, 7))), BAD), (dict(GW, dW=M(40, 30, 8)), BAD), (dict(GX, ws=at(7)), BAD),
+    (dict(GX, ws=at(6)), BAD), (dict(GX, X=M(4, 30, 1, F64)), NOT)])
+def test_loss_gradients_that_are_refused(how, status):
+    assert lossback(**how) == status
+    assert C.costa_last_error()
+
+
+@pytest.mark.parametrize("name,sizes", [("costa_mx_norm_workspace", 2), ("costa_mx_adapted_workspace", 4),
+                                        ("costa_mx_adapter_gradient_workspace", 4), ("costa_mx_loss_workspace", 4)])
+def test_workspaces_of_all_sizes(name, sizes):
+    """least <= most, whole numbers of floats; negative and too large sizes are refused; either answer may be left out."""
+    import itertools
+    for s in itertools.product(*[[0, 1, 63, 64, 65, 5000, 100000]] * (sizes if sizes == 2 else 3)):
+        s = (*s, 7)[:sizes] if name != "costa_mx_adapter_gradient_workspace" else (*s[:2], s[2] % 700, 100)
+        for last in ((0, 1) if "loss" in name else (None,)):
+            t = s if last is None else (*s[:3], last)
+            least, most = C._two_sizes(name, *t)
+            assert 0 <= least <= most and least % 4 == 0
+    f = getattr(C._lib, name)
+    one = ctypes.c_size_t()
+    good = [8] * sizes
+    assert f(*good, None, ctypes.byref(one)) == 0 and f(*good, ctypes.byref(one), None) == 0 and f(*good, None, None) == 0
+    for i in range(2):
+        assert f(*good[:i], -1, *good[i + 1:], None, None) == BAD
+        assert f(*good[:i], 1 << 31, *good[i + 1:], None, None) == NOT
+
+
+def test_ranks_above_256_have_no_workspace():
+    for f in (C._lib.costa_mx_adapted_workspace, C._lib.costa_mx_adapter_gradient_workspace):
+        assert f(8, 8, 8, 257, None, None) == NOT and f(8, 8, 8, -1, None, None) == BAD
+
+
+def test_workspaces_stay_small():
+    """Pieces and slices, not whole logits and sums, of large calls; row statistics and the gradient's sum aside."""
+    m, n, k = 16384, 262144, 8192
+    assert C.costa_mx_loss_workspace(m, n, k, False)[1] < (512 << 20) + m * n // 256 * 8 + m * 4
+    assert C.costa_mx_loss_workspace(m, n, k, True)[1] < (768 << 20) + m * k * 4
+    assert C.costa_mx_adapted_workspace(1 << 20, 16384, k, 64)[1] < (512 << 20) + (1 << 20) * 64 * 4
+
+
+def test_python_views_are_checked():
+    import torch
+    t, v = torch.zeros(4, 4), torch.zeros(4)
+    with pytest.raises(ValueError):  # host memory never reaches a kernel
+        C.costa_mx_norm(EPS, t, Y=t)
+    with pytest.raises(ValueError):
+        C.costa_mx_norm_backward(t, t, None, v, t)
+    with pytest.raises(ValueError):
+        C.MxAdapters(torch.zeros(2, 3, 4), torch.zeros(2, 3, 5))
+    with pytest.raises(ValueError):
+        C.MxAdapters(torch.zeros(2, 3, 4), torch.zeros(2, 4, 5))
+    with pytest.raises(ValueError):
+        C.MxAdapters(torch.zeros(2, 3, 4), torch.zeros(2, 3, 5).bfloat16())
+    with pytest.raises(ValueError):
+        C.costa_mx_loss(1.0, t, type("W", (), dict(rows=4, _ref=None)), v.long(), v, v, workspace=torch.zeros(8, dtype=torch.uint8))
+    with pytest.raises(ValueError, match="index"):
+        C._vector(torch.zeros(4, dtype=torch.int64), torch.int32, 4, "index")
+
+
+@pytest.mark.spawns
+def test_header_is_plain_c(tmp_path):
+    import subprocess
+    src = tmp_path / "t.c"
+    src.write_text('#include "costa_layer.h"\nint main(void) { costa_mx_adapters a = {1, 0, 0, 0, 0, 0}; return (int)a.count - 1; }\n')
+    rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Wextra", "-Werror", "-D__HIP_PLATFORM_AMD__", "-fsyntax-only", "-I",
+                    os.path.join(ROOT, "include"), "-I", os.path.join(rocm, "include"), str(src)], check=True)
