@@ -20,21 +20,11 @@
 // zero would be a NaN in another's rows.)
 #include <algorithm>
 
-#include "mx_layer.hpp"
-#include "mx_rows.hpp"
+#include "mx_adapters.hpp"
+#include "mx_tiles.hpp"
 
 namespace costa {
 namespace {
-
-__device__ inline int32_t adapter_of(const AdapterIndex& at, int64_t row) {
-  const int32_t a = at.index[row];
-  return a >= 0 && a < at.count ? a : -1;
-}
-__device__ inline int rank_of(const AdapterIndex& at, int32_t a) {
-  if (a < 0) return 0;
-  return at.ranks ? min(max(at.ranks[a], 0), at.rank) : at.rank;
-}
-__device__ inline float scale_of(const AdapterIndex& at, int32_t a) { return at.scales ? at.scales[a] : 1.0f; }
 
 // ---- few rows: a row at a time, on the vector units ----------------------------
 // A workgroup makes RANKS of a row's products; its lanes go along the row.  The time is that
@@ -145,111 +135,128 @@ __global__ __launch_bounds__(256) void adapter_add_row(AdapterAddArgs p, int64_t
   if (c < p.n) put_sums_typed(p, row, c, add);
 }
 
-// ---- many rows: sixteen at a time, on the matrix units --------------------------
-// The distinct adapters of the lanes l < 16 whose rows are there: by turns, each with the lanes
-// that have it.  `left` holds the lanes to come; -1 (no adapter) is one of them.
-struct Turn {
-  int32_t a;
-  bool mine;  // this lane's row (l % 16) has it
-};
-__device__ inline bool next_turn(uint64_t& left, int32_t idx, Turn& t) {
-  if (left == 0) return false;
-  t.a = __builtin_amdgcn_readlane(idx, (int)__builtin_ctzll(left));
-  const uint64_t same = __ballot(idx == t.a);
-  t.mine = idx == t.a;
-  left &= ~same;
-  return true;
-}
-
-// Sums of products of parts, those of 2^-24 and less left out.
-template <int PA, int PB>
-__device__ inline v4f mfma_parts(const v4u* a, const v4u* b, v4f c) {
-#pragma unroll
-  for (int i = 0; i < PA; ++i)
-#pragma unroll
-    for (int j = 0; j < PB; ++j)
-      if (i + j < 3) c = mfma_bf16(a[i], b[j], c);
-  return c;
-}
-
-// A workgroup has sixteen rows and 16 RT ranks; its eight waves take 128 elements of the rows
-// in turn, straight to registers in the instruction's order (lane l: row l % 16, eight
-// elements from 8 (l / 16) of each 32), and their sums are joined through shared memory.
-constexpr int kDotWaves = 8, kDotSpan = 128;
-template <int SRC, int RT, bool WIDE>
-__global__ __launch_bounds__(64 * kDotWaves) void adapter_dots_tile(AdapterDotsArgs p, int64_t row0) {
-  constexpr int P = parts_of(SRC), STEPS = kDotSpan / 32;
-  __shared__ v4f red[kDotWaves][RT][64];
+// ---- many rows, on the matrix units ---------------------------------------------
+// A workgroup has BM rows and RN ranks of a part of the sum, which goes by 64: both operands' steps
+// go through shared memory (read straight to registers in the instruction's order, sixteen
+// neighbouring lanes touch sixteen lines: 4096 rows by 64 ranks over 8192 took 73 us so), two of them
+// on their way while one is worked on.  Eight waves of sixteen rows by 16 NT ranks.
+template <int SRC, int BM, int RN>
+__global__ __launch_bounds__(kLanes) void adapter_dots_tile(AdapterDotsArgs p, int64_t row0, int64_t per) {
+  constexpr int P = parts_of(SRC), STRIPS = BM / 16, NT = RN / 16 / (kWaves / STRIPS), HALVES = BM / 64;
+  __shared__ v4u xs[2][P * BM * 8];
+  __shared__ v4u as[2][P * RN * 8];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l = lane % 16,
             g = lane / 16;
-  const int64_t i0 = row0 + (int64_t)blockIdx.x * 16, row = min(i0 + l, p.m - 1);
-  const int r0 = blockIdx.y * 16 * RT;
-  const int32_t idx = i0 + l < p.m ? adapter_of(p.at, row) : -1;
-  const void* const xl = line_of<SRC>(p.x, row);
-  v4f all[RT];
+  const int64_t i0 = row0 + (int64_t)blockIdx.x * BM;
+  const int r0 = blockIdx.y * RN, strip = wave % STRIPS * 16, rn = wave / STRIPS * 16 * NT;
+  const int64_t first = blockIdx.z * per, last = min(first + per, (p.k + kStepBf16 - 1) / kStepBf16);  // steps
+  const int32_t mine = i0 + strip + l < p.m ? adapter_of(p.at, i0 + strip + l) : -1;
+  int32_t idx[HALVES];  // of the tile's rows, the same in every wave
+  uint64_t left[HALVES], any = 0;
 #pragma unroll
-  for (int t = 0; t < RT; ++t) all[t] = v4f{0, 0, 0, 0};
-  uint64_t left = __ballot(idx >= 0);
-  Turn turn;
-  while (next_turn(left, idx, turn)) {
-    const int rank = rank_of(p.at, turn.a);
-    if (r0 >= rank) continue;
-    const void* al[RT];
-    v4f acc[RT];
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {  // (past the last row: that again, and its product is not taken)
-      al[t] = line_of<SRC>(p.low, (int64_t)turn.a * p.at.rank + min(r0 + 16 * t + l, rank - 1));
-      acc[t] = v4f{0, 0, 0, 0};
-    }
-    for (int64_t k0 = wave * kDotSpan; k0 < p.k; k0 += kDotWaves * kDotSpan) {
-      Raw8<SRC> x[STEPS], a[STEPS][RT];
-#pragma unroll
-      for (int s = 0; s < STEPS; ++s) {
-        const int64_t k = k0 + 32 * s + 8 * g;
-        get8<SRC, WIDE>(x[s], xl, k, p.k);
-#pragma unroll
-        for (int t = 0; t < RT; ++t) get8<SRC, WIDE>(a[s][t], al[t], k, p.k);
-      }
-      if (k0 + kDotSpan > p.k)
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-          const int64_t k = k0 + 32 * s + 8 * g;
-          placed8<SRC, WIDE>(x[s], k, p.k);
-#pragma unroll
-          for (int t = 0; t < RT; ++t) placed8<SRC, WIDE>(a[s][t], k, p.k);
-        }
-#pragma unroll
-      for (int s = 0; s < STEPS; ++s) {
-        v4u xp[P], ap[P];
-        raw_parts<SRC>(x[s], xp);
-#pragma unroll
-        for (int t = 0; t < RT; ++t) {
-          raw_parts<SRC>(a[s][t], ap);
-          acc[t] = mfma_parts<P, P>(ap, xp, acc[t]);
-        }
-      }
-    }
-    // lane: row l, ranks r0 + 16 t + 4 g .. + 3
-#pragma unroll
-    for (int t = 0; t < RT; ++t)
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (turn.mine && r0 + 16 * t + 4 * g + q < rank) all[t][q] = acc[t][q];
+  for (int h = 0; h < HALVES; ++h) {
+    idx[h] = i0 + 64 * h + lane < p.m ? adapter_of(p.at, i0 + 64 * h + lane) : -1;
+    left[h] = __ballot(idx[h] >= 0);
+    any |= left[h];
   }
+  const Args x{p.m, 0, p.k, MxView{}, MxView{}, p.x.data, p.x.ld, 1, Epilogue{}, 0};
+  v4f all[NT];
 #pragma unroll
-  for (int t = 0; t < RT; ++t) red[wave][t][lane] = all[t];
-  __syncthreads();
-  for (int u = threadIdx.x; u < RT * 64; u += 64 * kDotWaves) {
-    const int t = u / 64, at = u % 64;
-    v4f sum = red[0][t][at];
+  for (int t = 0; t < NT; ++t) all[t] = v4f{0, 0, 0, 0};
+  while (any) {
+    int32_t a = -1;
 #pragma unroll
-    for (int w = 1; w < kDotWaves; ++w) sum += red[w][t][at];
-    const int64_t i = i0 + at % 16;
-    const int r = r0 + 16 * t + at / 16 * 4;
-    if (i < p.m)
+    for (int h = HALVES - 1; h >= 0; --h)
+      if (left[h]) a = __builtin_amdgcn_readlane(idx[h], (int)__builtin_ctzll(left[h]));
+    any = 0;
+#pragma unroll
+    for (int h = 0; h < HALVES; ++h) {
+      left[h] &= ~__ballot(idx[h] == a);
+      any |= left[h];
+    }
+    const int rank = rank_of(p.at, a);
+    if (r0 >= rank || first >= last) continue;
+    // (past the last rank: that again, and its products are not taken)
+    const char* const low = static_cast<const char*>(line_of<SRC>(p.low, (int64_t)a * p.at.rank + min(r0 + (int)threadIdx.x / 8, rank - 1)));
+    v4f acc[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[t] = v4f{0, 0, 0, 0};
+    LeftStage<SRC, false, BM, false> xl[2];
+    Raw8<SRC> al[2];
+    const int c = threadIdx.x % 8, ar = threadIdx.x / 8;
+    auto load = [&](int set, int64_t t) {
+      if (t >= last) return;
+      xl[set].load(x, i0, t * kStepBf16);
+      if (ar < RN) load8<SRC>(al[set], low, t * kStepBf16 + 8 * c, p.k);
+    };
+    auto store = [&](int set, int64_t t, int s) {
+      xl[set].store(x, i0, xs[s]);
+      if (ar < RN) {
+        if ((t + 1) * kStepBf16 > p.k) place8<SRC>(al[set], t * kStepBf16 + 8 * c, p.k);
+        v4u out[P];
+        raw_parts<SRC>(al[set], out);
+#pragma unroll
+        for (int q = 0; q < P; ++q) as[s][q * RN * 8 + chunk_at(ar, c)] = out[q];
+      }
+    };
+    load(0, first);
+    load(1, first + 1);
+    __syncthreads();  // (the adapter's before: its last step is read)
+    store(0, first, 0);
+    load(0, first + 2);
+    __syncthreads();
+    for (int64_t t0 = first; t0 < last; t0 += 2) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const int64_t t = t0 + s;
+        if (t >= last) break;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          v4u xp[P];
+#pragma unroll
+          for (int q = 0; q < P; ++q) xp[q] = xs[s][q * BM * 8 + chunk_at(strip + l, 2 * g + h)];
+#pragma unroll
+          for (int u = 0; u < NT; ++u) {
+            v4u ap[P];
+#pragma unroll
+            for (int q = 0; q < P; ++q) ap[q] = as[s][q * RN * 8 + chunk_at(rn + 16 * u + l, 2 * g + h)];
+            acc[u] = mfma_parts<P, P>(ap, xp, acc[u]);
+          }
+        }
+        if (t + 1 < last) {
+          store(1 - s, t + 1, 1 - s);
+          load(1 - s, t + 3);
+        }
+        __syncthreads();
+      }
+    }
+    // lane: row l of the strip, ranks r0 + rn + 16 u + 4 g .. + 3
+#pragma unroll
+    for (int u = 0; u < NT; ++u)
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        if (r + q < p.at.rank) p.v[i * p.v_ld + r + q] = sum[q];
+        if (mine == a && r0 + rn + 16 * u + 4 * g + q < rank) all[u][q] = acc[u][q];
+  }
+  const int64_t row = i0 + strip + l;
+  if (row >= p.m) return;
+  float* const v = p.parts ? p.parts + ((int64_t)blockIdx.z * p.m + row) * p.at.rank : p.v + row * p.v_ld;
+#pragma unroll
+  for (int u = 0; u < NT; ++u)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int r = r0 + rn + 16 * u + 4 * g + q;
+      if (r < p.at.rank) v[r] = all[u][q];
+    }
+}
+
+// The parts of v, in a fixed order.
+__global__ __launch_bounds__(256) void adapter_dots_join(AdapterDotsArgs p, int64_t splits) {
+  const int64_t all = p.m * p.at.rank;
+  for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < all; u += (int64_t)gridDim.x * 256) {
+    float sum = 0.0f;
+#pragma unroll 4
+    for (int64_t s = 0; s < splits; ++s) sum += p.parts[s * all + u];
+    p.v[u / p.at.rank * p.v_ld + u % p.at.rank] = sum;
   }
 }
 
@@ -273,94 +280,6 @@ __device__ inline void column_parts(const Raw8<SRC> z[8], int e, v4u out[parts_o
       r.w[q / 2] = __builtin_amdgcn_perm(z[q + 1].w[e / 2], z[q].w[e / 2], e % 2 ? 0x07060302u : 0x05040100u);
   }
   raw_parts<SRC>(r, out);
-}
-
-// A wave has 16 S rows and 128 columns; four waves of a workgroup have the same columns of
-// rows that follow one another.  The results lie so that a lane has four runs of eight columns
-// of a row.
-template <int SRC, int S, bool WIDE>
-__global__ __launch_bounds__(256) void adapter_add_tile(AdapterAddArgs p, int64_t row0, int64_t col0) {
-  constexpr int P = parts_of(SRC);
-  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l = lane % 16,
-            g = lane / 16;
-  const int64_t i0 = row0 + ((int64_t)blockIdx.x * 4 + wave) * 16 * S,
-                j0 = col0 + (int64_t)blockIdx.y * 128;
-  if (i0 >= p.m) return;
-  int32_t idx[S];
-  uint64_t left[S], any = 0;
-#pragma unroll
-  for (int s = 0; s < S; ++s) {
-    const int64_t row = i0 + 16 * s + l;
-    idx[s] = row < p.m ? adapter_of(p.at, row) : -2;
-    left[s] = __ballot(idx[s] != -2);
-    any |= left[s];
-  }
-  while (any) {
-    // the first strip's next adapter, and the strips that have it
-    int32_t a = -2;
-#pragma unroll
-    for (int s = S - 1; s >= 0; --s)
-      if (left[s]) a = __builtin_amdgcn_readlane(idx[s], (int)__builtin_ctzll(left[s]));
-    uint64_t has[S];
-    any = 0;
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-      has[s] = __ballot(idx[s] == a);
-      left[s] &= ~has[s];
-      any |= left[s];
-    }
-    const int rank = rank_of(p.at, a);
-    const float scale = a < 0 ? 0.0f : scale_of(p.at, a);
-    v4f acc[S][8];
-#pragma unroll
-    for (int s = 0; s < S; ++s)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc[s][e] = v4f{0, 0, 0, 0};
-    for (int r0 = 0; r0 < rank; r0 += 32) {
-      Raw8<SRC> b[8];
-#pragma unroll
-      for (int q = 0; q < 8; ++q)
-        get8<SRC, WIDE>(b[q], line_of<SRC>(p.low, (int64_t)a * p.at.rank + min(r0 + 8 * g + q, rank - 1)), j0 + 8 * l, p.n);
-      if (j0 + 128 > p.n)
-#pragma unroll
-        for (int q = 0; q < 8; ++q) placed8<SRC, WIDE>(b[q], j0 + 8 * l, p.n);
-      if (r0 + 32 > rank)
-#pragma unroll
-        for (int q = 0; q < 8; ++q) keep8<SRC>(b[q], r0 + 8 * g + q < rank);
-      v4u v[S][3];
-#pragma unroll
-      for (int s = 0; s < S; ++s) {
-        if (!has[s]) continue;
-        const float* at = p.v + min(i0 + 16 * s + l, p.m - 1) * p.v_ld + r0 + 8 * g;
-        Raw8<SRC_F32> raw;
-#pragma unroll
-        for (int q = 0; q < 8; ++q)
-          raw.w[q] = r0 + 8 * g + q < rank ? __builtin_bit_cast(uint32_t, scale * at[q]) : 0u;
-        raw_parts<SRC_F32>(raw, v[s]);
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        v4u bp[P];
-        column_parts<SRC>(b, e, bp);
-#pragma unroll
-        for (int s = 0; s < S; ++s)
-          if (has[s]) acc[s][e] = mfma_parts<P, 3>(bp, v[s], acc[s][e]);
-      }
-    }
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-      if (idx[s] != a) continue;
-      const int64_t row = i0 + 16 * s + l;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float add[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) add[e] = acc[s][e][q];
-        const int64_t c = j0 + 8 * (4 * g + q);
-        if (c < p.n) put_sums_typed(p, row, c, add);
-      }
-    }
-  }
 }
 
 // ---- gradients --------------------------------------------------------------------
@@ -493,7 +412,7 @@ __global__ __launch_bounds__(256) void adapter_grad_join(AdapterGradArgs p, int6
 // ---- launches ----------------------------------------------------------------------
 // Workgroups of a launch, along x and along y: together, and with the parts of a gradient, below
 // 2^32 lanes.
-constexpr int64_t kRowGrid = 1 << 9, kColGrid = 1 << 12;
+constexpr int64_t kRowGrid = 1 << 12, kColGrid = 1 << 9;
 
 // Calls f<SRC, WIDE>
 template <typename F>
@@ -508,7 +427,17 @@ hipError_t by_type(costa_real type, bool wide, F f) {
   return hipGetLastError();
 }
 
-constexpr int64_t kFewRows = 64;
+// Whether products are made row by row, each reading its adapter's rows out of the cache, where the
+// tiles' kernel reads them once for its rows that share them.
+constexpr int64_t kByRowsBytes = (int64_t)1 << 30;
+bool dots_by_rows(int64_t m, int rank, int64_t k, costa_real type) {
+  return m <= 64 || k < 8 || m * rank * k * (type == COSTA_REAL_F32 ? 4 : 2) <= kByRowsBytes;
+}
+// Rows and ranks of a workgroup of the tiles' kernel.
+void dots_tile(int rank, int& bm, int& rn) {
+  rn = rank <= 16 ? 16 : rank <= 32 ? 32 : 64;
+  bm = rn == 16 ? 128 : 64;
+}
 
 // Ranks of a workgroup of the gradients' kernel, in sixteens, and workgroups along the columns.
 struct GradPlan {
@@ -522,38 +451,55 @@ GradPlan plan_grad(int64_t len, int32_t count, int32_t rank) {
 
 }  // namespace
 
+// (so that the workgroups are three for each CU, with 512 elements of the sum at least)
+int64_t mx_adapter_dots_parts(int64_t m, int64_t k, int rank) {
+  int bm, rn;
+  dots_tile(rank, bm, rn);
+  const int64_t tiles = up_div(m, bm) * up_div(std::max(rank, 1), rn);
+  return std::max<int64_t>(std::min(3 * kCUs / std::max<int64_t>(tiles, 1), k / 512), 1);
+}
+
 hipError_t launch_mx_adapter_dots(const AdapterDotsArgs& a, hipStream_t stream) {
-  const bool few = a.m <= kFewRows;
-  const int64_t groups = few ? a.m : up_div(a.m, 16);
-  const int rt = a.at.rank <= 16 ? 1 : a.at.rank <= 32 ? 2 : 4;
-  constexpr int64_t kDotGrid = 1 << 16;
-  for (int64_t at = 0; at < groups; at += kDotGrid) {
-    const unsigned x = (unsigned)std::min(kDotGrid, groups - at);
-    const hipError_t e = by_type(a.type, a.k >= 8, [&](auto src, auto wide) {
+  constexpr int64_t kGrid = 1 << 16;
+  if (dots_by_rows(a.m, a.at.rank, a.k, a.type)) {
+    for (int64_t at = 0; at < a.m; at += kGrid) {
+      const dim3 grid((unsigned)std::min(kGrid, a.m - at), (unsigned)up_div(a.at.rank, kDotRanks));
+      const hipError_t e = by_type(a.type, a.k >= 8, [&](auto src, auto wide) {
+        adapter_dots_row<decltype(src)::value, decltype(wide)::value><<<grid, 256, 0, stream>>>(a, at);
+      });
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+  }
+  AdapterDotsArgs b = a;
+  const int64_t splits = std::min(mx_adapter_dots_parts(a.m, a.k, a.at.rank), std::max<int64_t>(a.most, 1));
+  if (splits == 1) b.parts = nullptr;
+  int bm, rn;
+  dots_tile(a.at.rank, bm, rn);
+  const int64_t steps = up_div(a.k, kStepBf16), per = up_div(steps, splits), tiles = up_div(a.m, bm);
+  for (int64_t at = 0; at < tiles; at += kGrid) {
+    const dim3 grid((unsigned)std::min(kGrid, tiles - at), (unsigned)up_div(a.at.rank, rn), (unsigned)splits);
+    const hipError_t e = by_type(a.type, true, [&](auto src, auto wide) {
       constexpr int SRC = decltype(src)::value;
-      constexpr bool WIDE = decltype(wide)::value;
-      const dim3 tiles(x, (unsigned)up_div(a.at.rank, 16 * rt));
-      if (few) adapter_dots_row<SRC, WIDE><<<dim3(x, (unsigned)up_div(a.at.rank, kDotRanks)), 256, 0, stream>>>(a, at);
-      else if (rt == 1) adapter_dots_tile<SRC, 1, WIDE><<<tiles, 64 * kDotWaves, 0, stream>>>(a, at * 16);
-      else if (rt == 2) adapter_dots_tile<SRC, 2, WIDE><<<tiles, 64 * kDotWaves, 0, stream>>>(a, at * 16);
-      else adapter_dots_tile<SRC, 4, WIDE><<<tiles, 64 * kDotWaves, 0, stream>>>(a, at * 16);
+      if (!decltype(wide)::value) return;
+      if (rn == 16) adapter_dots_tile<SRC, 128, 16><<<grid, kLanes, 0, stream>>>(b, at * bm, per);
+      else if (rn == 32) adapter_dots_tile<SRC, 64, 32><<<grid, kLanes, 0, stream>>>(b, at * bm, per);
+      else adapter_dots_tile<SRC, 64, 64><<<grid, kLanes, 0, stream>>>(b, at * bm, per);
     });
     if (e != hipSuccess) return e;
   }
-  return hipSuccess;
+  if (splits == 1) return hipSuccess;
+  adapter_dots_join<<<dim3((unsigned)std::min<int64_t>(up_div(a.m * a.at.rank, 256), 1 << 20)), 256, 0, stream>>>(b, splits);
+  return hipGetLastError();
 }
 
 hipError_t launch_mx_adapter_add(const AdapterAddArgs& a, hipStream_t stream) {
-  const bool few = a.m <= kFewRows;
-  const int64_t rows = few ? 1 : 128, cols = few ? 2048 : 128, down = up_div(a.m, rows), across = up_div(a.n, cols);
+  const int64_t across = up_div(a.n, 2048);
   for (int64_t j = 0; j < across; j += kColGrid)
-    for (int64_t i = 0; i < down; i += kRowGrid) {
-      const dim3 grid((unsigned)std::min(kRowGrid, down - i), (unsigned)std::min(kColGrid, across - j));
+    for (int64_t i = 0; i < a.m; i += kRowGrid) {
+      const dim3 grid((unsigned)std::min(kRowGrid, a.m - i), (unsigned)std::min(kColGrid, across - j));
       const hipError_t e = by_type(a.type, a.n >= 8, [&](auto src, auto wide) {
-        constexpr int SRC = decltype(src)::value;
-        constexpr bool WIDE = decltype(wide)::value;
-        if (few) adapter_add_row<SRC, WIDE><<<grid, 256, 0, stream>>>(a, i * rows, j * cols);
-        else adapter_add_tile<SRC, 2, WIDE><<<grid, 256, 0, stream>>>(a, i * rows, j * cols);
+        adapter_add_row<decltype(src)::value, decltype(wide)::value><<<grid, 256, 0, stream>>>(a, i, j * 2048);
       });
       if (e != hipSuccess) return e;
     }
@@ -570,9 +516,9 @@ hipError_t launch_mx_adapter_grad(const AdapterGradArgs& a, hipStream_t stream) 
   const GradPlan g = plan_grad(a.len, a.at.count, a.at.rank);
   const int64_t splits = std::min(mx_adapter_grad_parts(a.m, a.len, a.at.count, a.at.rank), a.most);
   const int64_t per = up_div(a.m, splits);
-  for (int64_t j = 0; j < g.across; j += kRowGrid)
-    for (int64_t i = 0; i < g.pairs; i += kColGrid) {
-      const dim3 grid((unsigned)std::min(kRowGrid, g.across - j), (unsigned)std::min(kColGrid, g.pairs - i),
+  for (int64_t j = 0; j < g.across; j += kColGrid)
+    for (int64_t i = 0; i < g.pairs; i += kRowGrid) {
+      const dim3 grid((unsigned)std::min(kColGrid, g.across - j), (unsigned)std::min(kRowGrid, g.pairs - i),
                       (unsigned)splits);
       const hipError_t e = by_type(a.type, a.len >= 8, [&](auto src, auto wide) {
         constexpr int SRC = decltype(src)::value;

@@ -244,7 +244,7 @@ extern "C" costa_status costa_mx_product_adapted(float alpha, const costa_matrix
     if (m == 0) return COSTA_SUCCESS;
     char* room = static_cast<char*>(workspace);
     size_t left = workspace ? workspace_bytes : 0;
-    AdapterDotsArgs d{at, m, k, X->type, rows_of(X), rows_of(adapters->A), nullptr, at.rank};
+    AdapterDotsArgs d{at, m, k, X->type, rows_of(X), rows_of(adapters->A), nullptr, at.rank, nullptr, 0};
     if (V) {
       d.v = static_cast<float*>(V->data), d.v_ld = V->ld;
     } else {
@@ -252,8 +252,17 @@ extern "C" costa_status costa_mx_product_adapted(float alpha, const costa_matrix
       const size_t taken = up16((size_t)m * at.rank * 4);
       room += taken, left -= taken;
     }
-    if (at.rank > 0) HIP_OR_FAIL(launch_mx_adapter_dots(d, stream));
+    if (at.rank > 0) {  // (the parts of v lie where the product's sums will)
+      d.parts = reinterpret_cast<float*>(room);
+      d.most = (int64_t)(left / ((size_t)m * at.rank * 4));
+      HIP_OR_FAIL(launch_mx_adapter_dots(d, stream));
+    }
     if (n == 0) return COSTA_SUCCESS;
+    if (mx_adapted_fused(X->type, w.bits, m, n, k)) {
+      const AdapterAddArgs c{at, m, n, X->type, C->type, rows_of(adapters->B), rows_of(C), d.v, d.v_ld, nullptr, 0, alpha, beta};
+      HIP_OR_FAIL(launch_mx_adapted_product(c, rows_of(X), k, w, stream));
+      return COSTA_SUCCESS;
+    }
     // slices of rows whose sums the workspace holds
     const int64_t per = k == 0 ? m : std::min<int64_t>(slice_rows(m, n), (int64_t)(left / sums_bytes(1, n)));
     for (int64_t i = 0; i < m; i += per) {
@@ -293,7 +302,8 @@ extern "C" costa_status costa_mx_adapted_workspace(int64_t m, int64_t n, int64_t
     const size_t v = up16((size_t)m * rank * 4);
     const bool sums = m > 0 && n > 0 && k > 0;
     give(least, v + (sums ? sums_bytes(std::min<int64_t>(m, 256), n) : 0));
-    give(most, v + (sums ? split_bytes(slice_rows(m, n), n, k) : 0));
+    give(most, v + std::max(sums ? split_bytes(slice_rows(m, n), n, k) : 0,
+                            (size_t)m * rank * 4 * mx_adapter_dots_parts(m, k, rank)));
     return COSTA_SUCCESS;
   });
 }

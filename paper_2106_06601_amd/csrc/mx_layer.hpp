@@ -61,7 +61,11 @@ struct AdapterDotsArgs {
   RowsView x, low;
   float* v;
   int64_t v_ld;
+  float* parts;  // m x rank floats each
+  int64_t most;  // parts that there is room for
 };
+// Parts of v that a call can use.
+int64_t mx_adapter_dots_parts(int64_t m, int64_t k, int rank);
 hipError_t launch_mx_adapter_dots(const AdapterDotsArgs& a, hipStream_t stream);
 
 // c <- alpha * (the sum of `splits` parts, m x n floats each) + s v low + beta c
@@ -77,6 +81,10 @@ struct AdapterAddArgs {
   float alpha, beta;
 };
 hipError_t launch_mx_adapter_add(const AdapterAddArgs& a, hipStream_t stream);
+// The same in the product's own kernel, from x (m x k) and w, where that takes one (mx_tiles_adapted.hip).
+bool mx_adapted_fused(costa_real type, int bits, int64_t m, int64_t n, int64_t k);
+hipError_t launch_mx_adapted_product(const AdapterAddArgs& a, const RowsView& x, int64_t k, const MxView& w,
+                                     hipStream_t stream);
 
 // g ((count rank) x len) <- s * sum over the rows of v^T z + beta g
 struct AdapterGradArgs {

@@ -138,6 +138,55 @@ def test_adapted_product(shape, dtype, how):
         assert torch.equal(y, got[0])  # V kept or not, and a second time: the same bits
 
 
+# rows enough for the products' own tiles to add the adapters' part: tiles of 256 columns and of 128, last
+# ones cut in both directions, ranks that are no multiple of 32, columns no multiple of 4
+TILED = [(2047, 8190, 100, 3, 20), (2048, 8191, 130, 40, 70), (1024, 4096, 64, 2, 32), (1030, 2051, 300, 9, 5), (1300, 1999, 40, 1, 100)]
+
+
+@pytest.mark.parametrize("shape", TILED, ids=str)
+@pytest.mark.parametrize("dtype,bits", [("f32", 4), ("f32", 8), ("bf16", 4), ("bf16", 8), ("f16", 4), ("f16", 8)])
+@pytest.mark.parametrize("how", ["runs", "mixed"])
+def test_adapted_product_of_many_rows(shape, dtype, bits, how):
+    m, n, k, count, rank = shape
+    out, alpha, beta = (dtype, 1.0, 0.0) if how == "runs" else ("f32", -0.5, 0.25)
+    c = Case(m, n, k, count, rank, dtype, bits, how)
+    c.adapters.A[0, 1:], c.adapters.B[0, 1:] = float("nan"), float("inf")  # (no row sees these)
+    c.A[0, 1:] = c.B[0, 1:] = 0
+    c.ranks[0] = 1
+    ad = C.MxAdapters(c.adapters.A, c.adapters.B, c.ranks.cuda(), c.adapters.scales)
+    v, ev, want, off = c.forward(alpha, beta, out)
+    y, V = strided(c.c0 if beta else c.c0 * np.nan, out, n + (how == "mixed")), strided(np.full((m, rank), np.nan), "f32", rank)
+    C.costa_mx_product_adapted(alpha, strided(c.x, dtype, k + 1), c.wq, ad, c.index.cuda(), beta, y, V=V)
+    assert (np.abs(wide(V) - v) <= ev).all()
+    assert (np.abs(wide(y) - want) <= off).all()
+
+
+# so many elements that a tile's rows share what is read of their adapter: of 16, 32 and 64 ranks at a time, the last
+# ones cut, sums of whole steps and not, split and (least workspace) not
+SHARED = [(8300, 9, 4100, 7, 16), (6001, 16, 4096, 3, 30), (2101, 10, 4161, 5, 70), (1100, 8, 8200, 2, 256)]
+
+
+@pytest.mark.parametrize("shape", SHARED, ids=str)
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("how", ["runs", "mixed"])
+def test_rows_that_share_their_adapter(shape, dtype, how):
+    m, n, k, count, rank = shape
+    assert m * rank * k * (4 if dtype == "f32" else 2) > 2**30
+    c = Case(m, n, k, count, rank, dtype, 8, how)
+    c.adapters.A[0, 1:] = float("nan")  # (no row sees these)
+    c.A[0, 1:] = 0
+    c.ranks[0] = 1
+    ad = C.MxAdapters(c.adapters.A, c.adapters.B, c.ranks.cuda(), c.adapters.scales)
+    v, ev, want, off = c.forward(1.0, 0.0, dtype)
+    X, index = strided(c.x, dtype, k + 1), c.index.cuda()
+    for size in (None, C.costa_mx_adapted_workspace(m, n, k, rank)[0]):
+        y, V = strided(c.c0 * np.nan, dtype, n), strided(np.full((m, rank), np.nan), "f32", rank + 3)
+        ws = None if size is None else torch.full((size,), 0xFF, dtype=torch.uint8).cuda()
+        C.costa_mx_product_adapted(1.0, X, c.wq, ad, index, 0.0, y, V=V, workspace=ws)
+        assert (np.abs(wide(V) - v) <= ev).all()
+        assert (np.abs(wide(y) - want) <= off).all()
+
+
 @pytest.mark.parametrize("shape", SHAPES + [(3000, 70, 600, 2, 16), (2049, 1030, 30, 1, 20)], ids=str)
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("how", ["runs", "mixed", "same", "none"])
