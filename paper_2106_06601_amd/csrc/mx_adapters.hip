@@ -260,6 +260,37 @@ __global__ __launch_bounds__(256) void adapter_dots_join(AdapterDotsArgs p, int6
   }
 }
 
+// v from its parts (or as it is) to v and, spread, to the operands that the products' tiles add.
+__global__ __launch_bounds__(256) void adapter_spread(AdapterDotsArgs p, int64_t splits, v4u* spread) {
+  const int64_t steps = (p.at.rank + 31) / 32, units = (p.m + 15) / 16 * steps * 64, all = p.m * p.at.rank;
+  for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (int64_t)gridDim.x * 256) {
+    const int lane = (int)(u % 64);
+    const int64_t unit = u / 64, tile = unit / steps, row = tile * 16 + lane % 16;
+    const int r0 = (int)(unit - tile * steps) * 32 + lane / 16 * 8;
+    Raw8<SRC_F32> raw;
+    const int32_t a = row < p.m ? adapter_of(p.at, row) : -1;
+    const float scale = a < 0 ? 0.0f : scale_of(p.at, a);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      float x = 0.0f;
+      if (row < p.m && r0 + q < p.at.rank) {
+        if (splits > 0) {
+#pragma unroll 4
+          for (int64_t s = 0; s < splits; ++s) x += p.parts[s * all + row * p.at.rank + r0 + q];
+          p.v[row * p.v_ld + r0 + q] = x;
+        } else {
+          x = p.v[row * p.v_ld + r0 + q];
+        }
+      }
+      raw.w[q] = a < 0 ? 0u : __builtin_bit_cast(uint32_t, scale * x);
+    }
+    v4u out[3];
+    raw_parts<SRC_F32>(raw, out);
+#pragma unroll
+    for (int x = 0; x < 3; ++x) spread[(unit * 3 + x) * 64 + lane] = out[x];
+  }
+}
+
 // Zeros in place of what is not there.
 template <int SRC>
 __device__ inline void keep8(Raw8<SRC>& r, bool there) {
@@ -283,22 +314,29 @@ __device__ inline void column_parts(const Raw8<SRC> z[8], int e, v4u out[parts_o
 }
 
 // ---- gradients --------------------------------------------------------------------
-// A workgroup's four waves have 128 columns each of 16 RT ranks of an adapter, and a part of the
-// rows, of which those of the adapter are listed in shared memory, 2048 rows at a time, and
-// taken by 32.
+// A workgroup has 128 columns of 16 RT ranks of an adapter, and a part of the rows, of which those
+// of the adapter are listed in shared memory, 2048 rows at a time.  Its four waves take 32 of them by
+// turns, straight to registers (the next ones are on their way while some are worked on), and
+// their sums are joined through shared memory.
 constexpr int kListed = 2048;
 template <int SRC, int RT, bool WIDE>
 __global__ __launch_bounds__(256) void adapter_grad_tile(AdapterGradArgs p, int64_t col0, int64_t pair0,
                                                          int64_t per) {
   constexpr int P = parts_of(SRC);
-  __shared__ int32_t list[kListed + 32];
-  __shared__ int32_t counts[4];
+  __shared__ union {
+    struct {
+      int32_t list[kListed + 128];
+      int32_t counts[4];
+    } rows;
+    v4f sums[2][RT * 8][64];
+  } shared;
+  int32_t* const list = shared.rows.list;
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l = lane % 16,
             g = lane / 16;
   const int chunks = (p.at.rank + 16 * RT - 1) / (16 * RT);
   const int32_t pair = (int32_t)(pair0 + blockIdx.y), a = pair / chunks;
   const int r0 = pair % chunks * 16 * RT, rank = rank_of(p.at, a);
-  const int64_t j0 = col0 + ((int64_t)blockIdx.x * 4 + wave) * 128, j = j0 + 8 * l;
+  const int64_t j0 = col0 + (int64_t)blockIdx.x * 128, j = j0 + 8 * l;
   const int64_t first = (int64_t)blockIdx.z * per, last = min(first + per, p.m);
   v4f acc[RT][8];
 #pragma unroll
@@ -311,57 +349,74 @@ __global__ __launch_bounds__(256) void adapter_grad_tile(AdapterGradArgs p, int6
       const int64_t row = at + threadIdx.x;
       const bool mine = row < last && p.at.index[row] == a;
       const uint64_t who = __ballot(mine);
-      if (lane == 0) counts[wave] = __popcll(who);
+      if (lane == 0) shared.rows.counts[wave] = __popcll(who);
       __syncthreads();
       int before = n + __popcll(who & (((uint64_t)1 << lane) - 1));
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        if (w < wave) before += counts[w];
-        n += counts[w];
+        if (w < wave) before += shared.rows.counts[w];
+        n += shared.rows.counts[w];
       }
       if (mine) list[before] = (int32_t)(row - first);
       __syncthreads();
     }
     if (n == 0) continue;
-    if (threadIdx.x < 32) list[n + threadIdx.x] = list[n - 1];
+    if (threadIdx.x < 128) list[n + threadIdx.x] = list[n - 1];
     __syncthreads();
-    if (j0 < p.len)
-      for (int at = 0; at < n; at += 32) {
-        Raw8<SRC> z[8];
-        uint32_t v[RT][8];
+    Raw8<SRC> z[8];
+    uint32_t v[RT][8];
+    auto load = [&](int at) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          const int64_t row = first + list[at + 8 * g + q];
-          get8<SRC, WIDE>(z[q], line_of<SRC>(p.z, row), j, p.len);
+      for (int q = 0; q < 8; ++q) {
+        const int64_t row = first + list[min(at, n) + 8 * g + q];
+        get8<SRC, WIDE>(z[q], line_of<SRC>(p.z, row), j, p.len);
 #pragma unroll
-          for (int t = 0; t < RT; ++t)
-            v[t][q] = __builtin_bit_cast(uint32_t, p.v[row * p.v_ld + min(r0 + 16 * t + l, rank - 1)]);
-        }
-        if (at + 32 > n)  // (past the list's end is its last row again)
-#pragma unroll
-          for (int q = 0; q < 8; ++q) keep8<SRC>(z[q], at + 8 * g + q < n);
-        if (j0 + 128 > p.len)
-#pragma unroll
-          for (int q = 0; q < 8; ++q) placed8<SRC, WIDE>(z[q], j, p.len);
-        v4u vp[RT][3];
-#pragma unroll
-        for (int t = 0; t < RT; ++t) {
-          Raw8<SRC_F32> raw;
-#pragma unroll
-          for (int q = 0; q < 8; ++q) raw.w[q] = at + 8 * g + q < n ? v[t][q] : 0u;
-          raw_parts<SRC_F32>(raw, vp[t]);
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          v4u zp[P];
-          column_parts<SRC>(z, e, zp);
-#pragma unroll
-          for (int t = 0; t < RT; ++t) acc[t][e] = mfma_parts<P, 3>(zp, vp[t], acc[t][e]);
-        }
+        for (int t = 0; t < RT; ++t)
+          v[t][q] = __builtin_bit_cast(uint32_t, p.v[row * p.v_ld + min(r0 + 16 * t + l, rank - 1)]);
       }
+    };
+    load(wave * 32);
+    for (int at = wave * 32; at < n; at += 128) {
+      Raw8<SRC> zs[8];
+      v4u vp[RT][3];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) zs[q] = z[q];
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        Raw8<SRC_F32> raw;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) raw.w[q] = at + 8 * g + q < n ? v[t][q] : 0u;
+        raw_parts<SRC_F32>(raw, vp[t]);
+      }
+      load(at + 128);
+      if (at + 32 > n)  // (past the list's end is its last row again)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) keep8<SRC>(zs[q], at + 8 * g + q < n);
+      if (j0 + 128 > p.len)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) placed8<SRC, WIDE>(zs[q], j, p.len);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        v4u zp[P];
+        column_parts<SRC>(zs, e, zp);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) acc[t][e] = mfma_parts<P, 3>(zp, vp[t], acc[t][e]);
+      }
+    }
     __syncthreads();  // (the list is read)
   }
-  if (j0 >= p.len) return;
+#pragma unroll
+  for (int half = 2; half > 0; half /= 2) {
+    if (wave >= half && wave < 2 * half)
+#pragma unroll
+      for (int t = 0; t < RT * 8; ++t) shared.sums[wave - half][t][lane] = acc[t / 8][t % 8];
+    __syncthreads();
+    if (wave < half)
+#pragma unroll
+      for (int t = 0; t < RT * 8; ++t) acc[t / 8][t % 8] += shared.sums[wave][t][lane];
+    __syncthreads();
+  }
+  if (wave != 0) return;
   const float scale = scale_of(p.at, a);
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
@@ -446,7 +501,7 @@ struct GradPlan {
 };
 GradPlan plan_grad(int64_t len, int32_t count, int32_t rank) {
   const int rt = rank <= 16 ? 1 : rank <= 32 ? 2 : 4;
-  return {rt, up_div(len, 512), (int64_t)count * up_div(rank, 16 * rt)};
+  return {rt, up_div(len, 128), (int64_t)count * up_div(rank, 16 * rt)};
 }
 
 }  // namespace
@@ -459,7 +514,8 @@ int64_t mx_adapter_dots_parts(int64_t m, int64_t k, int rank) {
   return std::max<int64_t>(std::min(3 * kCUs / std::max<int64_t>(tiles, 1), k / 512), 1);
 }
 
-hipError_t launch_mx_adapter_dots(const AdapterDotsArgs& a, hipStream_t stream) {
+hipError_t launch_mx_adapter_dots(const AdapterDotsArgs& a, int64_t& left, hipStream_t stream) {
+  left = 0;
   constexpr int64_t kGrid = 1 << 16;
   if (dots_by_rows(a.m, a.at.rank, a.k, a.type)) {
     for (int64_t at = 0; at < a.m; at += kGrid) {
@@ -488,8 +544,19 @@ hipError_t launch_mx_adapter_dots(const AdapterDotsArgs& a, hipStream_t stream) 
     });
     if (e != hipSuccess) return e;
   }
-  if (splits == 1) return hipSuccess;
-  adapter_dots_join<<<dim3((unsigned)std::min<int64_t>(up_div(a.m * a.at.rank, 256), 1 << 20)), 256, 0, stream>>>(b, splits);
+  left = splits > 1 ? splits : 0;
+  return hipSuccess;
+}
+
+hipError_t launch_mx_adapter_dots_join(const AdapterDotsArgs& a, int64_t splits, hipStream_t stream) {
+  adapter_dots_join<<<dim3((unsigned)std::min<int64_t>(up_div(a.m * a.at.rank, 256), 1 << 20)), 256, 0, stream>>>(a, splits);
+  return hipGetLastError();
+}
+
+hipError_t launch_mx_adapter_spread(const AdapterDotsArgs& a, int64_t splits, void* spread, hipStream_t stream) {
+  const int64_t units = up_div(a.m, 16) * up_div(a.at.rank, 32) * 64;
+  adapter_spread<<<dim3((unsigned)std::min<int64_t>(up_div(units, 256), 1 << 20)), 256, 0, stream>>>(
+      a, splits, static_cast<v4u*>(spread));
   return hipGetLastError();
 }
 
@@ -506,10 +573,10 @@ hipError_t launch_mx_adapter_add(const AdapterAddArgs& a, hipStream_t stream) {
   return hipSuccess;
 }
 
-// (so that the workgroups are two for each CU, with 128 rows of each at least)
+// (so that the workgroups are two for each CU, with 512 rows of each at least)
 int64_t mx_adapter_grad_parts(int64_t m, int64_t len, int32_t count, int32_t rank) {
   const GradPlan g = plan_grad(len, count, rank);
-  return std::max<int64_t>(std::min(2 * kCUs / std::max<int64_t>(g.across * g.pairs, 1), m / 128), 1);
+  return std::max<int64_t>(std::min(2 * kCUs / std::max<int64_t>(g.across * g.pairs, 1), m / 512), 1);
 }
 
 hipError_t launch_mx_adapter_grad(const AdapterGradArgs& a, hipStream_t stream) {
@@ -523,9 +590,9 @@ hipError_t launch_mx_adapter_grad(const AdapterGradArgs& a, hipStream_t stream) 
       const hipError_t e = by_type(a.type, a.len >= 8, [&](auto src, auto wide) {
         constexpr int SRC = decltype(src)::value;
         constexpr bool WIDE = decltype(wide)::value;
-        if (g.rt == 1) adapter_grad_tile<SRC, 1, WIDE><<<grid, 256, 0, stream>>>(a, j * 512, i, per);
-        else if (g.rt == 2) adapter_grad_tile<SRC, 2, WIDE><<<grid, 256, 0, stream>>>(a, j * 512, i, per);
-        else adapter_grad_tile<SRC, 4, WIDE><<<grid, 256, 0, stream>>>(a, j * 512, i, per);
+        if (g.rt == 1) adapter_grad_tile<SRC, 1, WIDE><<<grid, 256, 0, stream>>>(a, j * 128, i, per);
+        else if (g.rt == 2) adapter_grad_tile<SRC, 2, WIDE><<<grid, 256, 0, stream>>>(a, j * 128, i, per);
+        else adapter_grad_tile<SRC, 4, WIDE><<<grid, 256, 0, stream>>>(a, j * 128, i, per);
       });
       if (e != hipSuccess) return e;
     }

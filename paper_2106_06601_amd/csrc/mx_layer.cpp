@@ -252,14 +252,26 @@ extern "C" costa_status costa_mx_product_adapted(float alpha, const costa_matrix
       const size_t taken = up16((size_t)m * at.rank * 4);
       room += taken, left -= taken;
     }
+    const bool fused = mx_adapted_fused(X->type, w.bits, m, n, k);
+    void* const spread = room;
+    if (fused) room += mx_spread_bytes(m, at.rank), left -= mx_spread_bytes(m, at.rank);
     if (at.rank > 0) {  // (the parts of v lie where the product's sums will)
+      int64_t splits = 0;
       d.parts = reinterpret_cast<float*>(room);
       d.most = (int64_t)(left / ((size_t)m * at.rank * 4));
-      HIP_OR_FAIL(launch_mx_adapter_dots(d, stream));
+      HIP_OR_FAIL(launch_mx_adapter_dots(d, splits, stream));
+      if (fused) HIP_OR_FAIL(launch_mx_adapter_spread(d, splits, spread, stream));
+      else if (splits > 0) HIP_OR_FAIL(launch_mx_adapter_dots_join(d, splits, stream));
     }
     if (n == 0) return COSTA_SUCCESS;
-    if (mx_adapted_fused(X->type, w.bits, m, n, k)) {
-      const AdapterAddArgs c{at, m, n, X->type, C->type, rows_of(adapters->B), rows_of(C), d.v, d.v_ld, nullptr, 0, alpha, beta};
+    if (fused) {
+      AdapterAddArgs c{};
+      c.at = at;
+      c.m = m, c.n = n;
+      c.type = X->type, c.c_type = C->type;
+      c.low = rows_of(adapters->B), c.c = rows_of(C);
+      c.alpha = alpha, c.beta = beta;
+      c.spread = static_cast<const v4u*>(spread);
       HIP_OR_FAIL(launch_mx_adapted_product(c, rows_of(X), k, w, stream));
       return COSTA_SUCCESS;
     }
@@ -299,7 +311,7 @@ extern "C" costa_status costa_mx_adapted_workspace(int64_t m, int64_t n, int64_t
     CHECKED(check_dims("X", m, k));
     if (rank < 0) return fail(COSTA_ERROR_INVALID_VALUE, "negative rank");
     if (rank > kRankMax) return fail(COSTA_ERROR_NOT_SUPPORTED, "a rank above 256");
-    const size_t v = up16((size_t)m * rank * 4);
+    const size_t v = up16((size_t)m * rank * 4) + mx_spread_bytes(m, rank);
     const bool sums = m > 0 && n > 0 && k > 0;
     give(least, v + (sums ? sums_bytes(std::min<int64_t>(m, 256), n) : 0));
     give(most, v + std::max(sums ? split_bytes(slice_rows(m, n), n, k) : 0,

@@ -6,6 +6,8 @@
 
 namespace costa {
 
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+
 // ---- norm (mx_norm.hip) ------------------------------------------------------
 // A plain row-major matrix as the kernels see it; data null: not there.
 struct RowsView {
@@ -64,9 +66,15 @@ struct AdapterDotsArgs {
   float* parts;  // m x rank floats each
   int64_t most;  // parts that there is room for
 };
+// s v as operands of the matrix instructions, three bfloat16 parts: of sixteen rows and 32 ranks, 64 lanes' 16
+// bytes of each part (lane l: row l % 16, eight ranks from 8 (l / 16) on).
+inline size_t mx_spread_bytes(int64_t m, int rank) { return (size_t)((m + 15) / 16) * ((rank + 31) / 32) * 3 * 1024; }
+hipError_t launch_mx_adapter_spread(const AdapterDotsArgs& a, int64_t splits, void* spread, hipStream_t stream);
 // Parts of v that a call can use.
 int64_t mx_adapter_dots_parts(int64_t m, int64_t k, int rank);
-hipError_t launch_mx_adapter_dots(const AdapterDotsArgs& a, hipStream_t stream);
+// splits: parts of v that are left to be added (0: v is there).
+hipError_t launch_mx_adapter_dots(const AdapterDotsArgs& a, int64_t& splits, hipStream_t stream);
+hipError_t launch_mx_adapter_dots_join(const AdapterDotsArgs& a, int64_t splits, hipStream_t stream);
 
 // c <- alpha * (the sum of `splits` parts, m x n floats each) + s v low + beta c
 struct AdapterAddArgs {
@@ -79,6 +87,7 @@ struct AdapterAddArgs {
   const float* parts;
   int32_t splits;
   float alpha, beta;
+  const v4u* spread;
 };
 hipError_t launch_mx_adapter_add(const AdapterAddArgs& a, hipStream_t stream);
 // The same in the product's own kernel, from x (m x k) and w, where that takes one (mx_tiles_adapted.hip).

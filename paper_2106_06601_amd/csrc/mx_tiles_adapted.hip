@@ -18,6 +18,7 @@ __device__ inline void add_adapters(const AdapterAddArgs& a, TileSums<MT, NT>& t
   const int lane = threadIdx.x % 64, l = lane % 16, g = lane / 16;
   const int64_t col = t.col + NT * l;
   const bool edge = t.col + 16 * NT > a.n;
+  const int64_t steps = (a.at.rank + 31) / 32, last = (a.m - 1) / 16 - t.row / 16;  // (the last piece with rows)
   int32_t idx[MT];
   uint32_t left[MT], any = 0;
 #pragma unroll
@@ -37,17 +38,17 @@ __device__ inline void add_adapters(const AdapterAddArgs& a, TileSums<MT, NT>& t
 #pragma unroll
     for (int i = MT - 1; i >= 0; --i)
       if (left[i]) id = __builtin_amdgcn_readlane(idx[i], __builtin_ctz(left[i]));
-    uint32_t has = 0;
+    uint32_t has = 0, full = 0;
     any = 0;
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       const uint32_t mine = (uint32_t)__ballot(idx[i] == id) & 0xffff;
       has |= mine ? 1u << i : 0u;
+      full |= mine == 0xffff ? 1u << i : 0u;
       left[i] &= ~mine;
       any |= left[i];
     }
     const int rank = rank_of(a.at, id);
-    const float scale = scale_of(a.at, id);
     for (int r0 = 0; r0 < rank; r0 += 32) {
       uint32_t b[8][WORDS];
 #pragma unroll
@@ -67,16 +68,12 @@ __device__ inline void add_adapters(const AdapterAddArgs& a, TileSums<MT, NT>& t
             }
         }
       }
-      // eight ranks of a row's v; where fewer than eight are left, those before them too, to be
-      // moved into place (the next piece's are on their way while one is worked on)
-      const int have = a.at.rank, k = r0 + 8 * g;
-      Raw8<SRC_F32> next;
-      auto load_v = [&](int i) {
-        const char* at = reinterpret_cast<const char*>(a.v + min(t.row + 16 * i + l, a.m - 1) * a.v_ld);
-        if (have >= 8) load8<SRC_F32>(next, at, k, have);
-        else
+      // s v of a piece's rows, as operands (the next piece's are on their way while one is worked on)
+      const v4u* const spread = a.spread + ((t.row / 16 * steps + r0 / 32) * 3) * 64 + lane;
+      v4u next[3];
+      auto load_v = [&](int i) {  // (a wave past the last row has nothing to do here)
 #pragma unroll
-          for (int q = 0; q < 8; ++q) next.w[q] = k + q < have ? reinterpret_cast<const uint32_t*>(at)[k + q] : 0u;
+        for (int x = 0; x < 3; ++x) next[x] = spread[(min((int64_t)i, last) * steps * 3 + x) * 64];
       };
       load_v(0);
       if (r0 + 32 > rank)  // (past the last rank was that again)
@@ -97,22 +94,21 @@ __device__ inline void add_adapters(const AdapterAddArgs& a, TileSums<MT, NT>& t
       }
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
-        Raw8<SRC_F32> raw = next;
+        v4u v[3];
+#pragma unroll
+        for (int x = 0; x < 3; ++x) v[x] = next[x];
         if (i + 1 < MT) load_v(i + 1);
         if (!(has >> i & 1)) continue;
-        if (r0 + 32 > have && have >= 8) place8<SRC_F32>(raw, k, have);
+        if (full >> i & 1) {  // all of the piece's rows
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {  // (0 past the adapter's rank)
-          const float x = scale * __builtin_bit_cast(float, raw.w[q]);
-          raw.w[q] = k + q < rank ? __builtin_bit_cast(uint32_t, x) : 0u;
-        }
-        v4u v[3];
-        raw_parts<SRC_F32>(raw, v);
+          for (int e = 0; e < NT; ++e) t.acc[i][e] = mfma_parts<P, 3>(bp[e], v, t.acc[i][e]);
+        } else {
 #pragma unroll
-        for (int e = 0; e < NT; ++e) {
-          const v4f d = mfma_parts<P, 3>(bp[e], v, v4f{0, 0, 0, 0});
+          for (int e = 0; e < NT; ++e) {
+            const v4f d = mfma_parts<P, 3>(bp[e], v, v4f{0, 0, 0, 0});
 #pragma unroll
-          for (int q = 0; q < 4; ++q) t.acc[i][e][q] += idx[i] == id ? d[q] : 0.0f;
+            for (int q = 0; q < 4; ++q) t.acc[i][e][q] += idx[i] == id ? d[q] : 0.0f;
+          }
         }
       }
     }
