@@ -270,20 +270,31 @@ __global__ __launch_bounds__(256) void adapter_spread(AdapterDotsArgs p, int64_t
     Raw8<SRC_F32> raw;
     const int32_t a = row < p.m ? adapter_of(p.at, row) : -1;
     const float scale = a < 0 ? 0.0f : scale_of(p.at, a);
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      float x = 0.0f;
-      if (row < p.m && r0 + q < p.at.rank) {
-        if (splits > 0) {
+    float x[8] = {};
+    if (row < p.m && r0 + 8 <= p.at.rank) {
+      const float* at = splits > 0 ? p.parts + row * p.at.rank + r0 : p.v + row * p.v_ld + r0;
 #pragma unroll 4
-          for (int64_t s = 0; s < splits; ++s) x += p.parts[s * all + row * p.at.rank + r0 + q];
-          p.v[row * p.v_ld + r0 + q] = x;
+      for (int64_t s = 0; s < max(splits, (int64_t)1); ++s) {
+        float w[8];
+        __builtin_memcpy(w, at + s * all, sizeof w);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) x[q] += w[q];
+      }
+      if (splits > 0) __builtin_memcpy(p.v + row * p.v_ld + r0, x, sizeof x);
+    } else if (row < p.m) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        if (r0 + q >= p.at.rank) continue;
+        if (splits > 0) {
+          for (int64_t s = 0; s < splits; ++s) x[q] += p.parts[s * all + row * p.at.rank + r0 + q];
+          p.v[row * p.v_ld + r0 + q] = x[q];
         } else {
-          x = p.v[row * p.v_ld + r0 + q];
+          x[q] = p.v[row * p.v_ld + r0 + q];
         }
       }
-      raw.w[q] = a < 0 ? 0u : __builtin_bit_cast(uint32_t, scale * x);
     }
+#pragma unroll
+    for (int q = 0; q < 8; ++q) raw.w[q] = a < 0 ? 0u : __builtin_bit_cast(uint32_t, scale * x[q]);
     v4u out[3];
     raw_parts<SRC_F32>(raw, out);
 #pragma unroll
@@ -483,8 +494,11 @@ hipError_t by_type(costa_real type, bool wide, F f) {
 }
 
 // Whether products are made row by row, each reading its adapter's rows out of the cache, where the
-// tiles' kernel reads them once for its rows that share them.
-constexpr int64_t kByRowsBytes = (int64_t)1 << 30;
+// tiles' kernel reads them once for its rows that share them: 300 rows of 32 to 64 adapters of 16
+// ranks over 8192 cost 20 us by rows and 209 in tiles, 4096 rows in runs of 8 adapters 65 us by rows and
+// 22 in tiles.  (Whether rows share is in device memory: many rows of many adapters mixed go in tiles all the
+// same, 4096 of 64 adapters 800 us.)
+constexpr int64_t kByRowsBytes = (int64_t)256 << 20;
 bool dots_by_rows(int64_t m, int rank, int64_t k, costa_real type) {
   return m <= 64 || k < 8 || m * rank * k * (type == COSTA_REAL_F32 ? 4 : 2) <= kByRowsBytes;
 }

@@ -416,12 +416,13 @@ costa_status check_loss(const costa_matrix* X, const costa_mx* W, const int64_t*
   return check_vector("target", target, X->rows, 8);
 }
 
-ProductArgs logits_of(const costa_matrix* X, const MxView& w, int64_t first, int64_t n) {
+ProductArgs logits_of(const costa_matrix* X, const MxView& w, int64_t first, int64_t n, float alpha) {
   ProductArgs p{};
   p.m = X->rows, p.n = n, p.k = X->cols;
   p.real = X->data;
   p.a_rs = X->ld, p.a_cs = 1, p.a_type = X->type;
   p.b = rows_of(w, first, n);
+  p.alpha = alpha;
   return p;
 }
 
@@ -439,8 +440,10 @@ extern "C" costa_status costa_mx_loss_workspace(int64_t m, int64_t n, int64_t k,
       const size_t at = up16((size_t)m * 4);
       give(least, at + up16((size_t)m * chunks_kept(n, kPieceColumns) * sizeof(LossStat)) + least_piece(m, n, 4));
       const size_t sums = piece_bytes(m, n, 4);
-      give(most, at + up16((size_t)m * chunks_kept(n, kPieceColumns) * sizeof(LossStat)) +
-                     std::max(sums, mx_product_workspace(m, std::min(n, piece_columns(m, n, sums, 4)), k)));
+      // (statistics of every 32 columns, where the logits stay in the tiles)
+      give(most, at + std::max(up16((size_t)m * chunks_kept(n, kPieceColumns) * sizeof(LossStat)) +
+                                   std::max(sums, mx_product_workspace(m, std::min(n, piece_columns(m, n, sums, 4)), k)),
+                               (size_t)m * ((n + 31) / 32) * sizeof(LossStat)));
     } else {
       const size_t dx = up16((size_t)m * k * 4);  // what dX is summed in
       give(least, dx + up16(least_piece(m, n, 4)) + up16(least_piece(m, n, 4)));
@@ -476,13 +479,21 @@ extern "C" costa_status costa_mx_loss(float alpha, const costa_matrix* X, const 
     LossStat* const stats = reinterpret_cast<LossStat*>(room);
     room += up16((size_t)m * chunks_kept(n, kPieceColumns) * sizeof(LossStat));
     const size_t left = workspace_bytes - (size_t)(room - static_cast<char*>(workspace));
+    if (mx_loss_fused(X->type, w.bits, m, n, k)) {
+      const int64_t chunks = mx_loss_tile_chunks(X->type, w.bits, m, n, k);
+      if (workspace_bytes >= up16((size_t)m * 4) + (size_t)m * chunks * sizeof(LossStat)) {
+        HIP_OR_FAIL(launch_mx_loss_tiles(logits_of(X, w, 0, n, alpha), target, stats, at, stream));
+        HIP_OR_FAIL(launch_mx_loss_join(m, n, chunks, stats, at, target, loss, lse, stream));
+        return COSTA_SUCCESS;
+      }
+    }
     const int64_t per = n == 0 ? 1 : piece_columns(m, n, std::min(left, piece_bytes(m, n, 4)), 4);
     int64_t chunks = 0;
     for (int64_t j = 0; j < n; j += per) {
       const int64_t cols = std::min(per, n - j);
       LogitsPart l{m, cols, j, reinterpret_cast<float*>(room), 0, alpha, target};
       if (k > 0) {
-        ProductArgs p = logits_of(X, w, j, cols);
+        ProductArgs p = logits_of(X, w, j, cols, alpha);
         p.workspace = reinterpret_cast<float*>(room), p.workspace_bytes = left;
         HIP_OR_FAIL(launch_mx_product_parts(p, l.splits, stream));
       }
@@ -550,19 +561,26 @@ extern "C" costa_status costa_mx_loss_backward(float alpha, const costa_matrix* 
     float* const sum = reinterpret_cast<float*>(room);  // of dX
     room += up16((size_t)m * k * 4);
     size_t left = workspace_bytes - up16((size_t)m * k * 4);
-    // half for G, half for the logits and for what products split
-    const int64_t per = piece_columns(m, n, std::min(left / 32 * 16, piece_bytes(m, n, 4)), 4);
+    // half for G, half for the logits, where they are kept, and for what products split
+    const size_t half = std::min(left / 32 * 16, up16(piece_bytes(m, n, 4)));
+    int64_t per = piece_columns(m, n, half, bf16 ? 2 : 4);
+    const bool fused = mx_loss_fused(X->type, w.bits, m, per, k);
+    if (!fused) per = piece_columns(m, n, half, 4);
     void* const g = room;
-    const size_t taken = up16((size_t)m * per * 4);
+    const size_t taken = up16((size_t)m * per * (fused && bf16 ? 2 : 4));
     room += taken, left -= taken;
     const bool whole = per >= n;
     for (int64_t j = 0; j < n; j += per) {
       const int64_t cols = std::min(per, n - j);
-      ProductArgs p = logits_of(X, w, j, cols);
-      p.workspace = reinterpret_cast<float*>(room), p.workspace_bytes = left;
-      LogitsPart l{m, cols, j, p.workspace, 0, alpha, target};
-      HIP_OR_FAIL(launch_mx_product_parts(p, l.splits, stream));
-      HIP_OR_FAIL(launch_mx_loss_grad(l, n, lse, dloss, g, bf16, stream));
+      ProductArgs p = logits_of(X, w, j, cols, alpha);
+      if (fused) {
+        HIP_OR_FAIL(launch_mx_loss_grad_tiles(p, n, j, target, lse, dloss, g, bf16, stream));
+      } else {
+        p.workspace = reinterpret_cast<float*>(room), p.workspace_bytes = left;
+        LogitsPart l{m, cols, j, p.workspace, 0, alpha, target};
+        HIP_OR_FAIL(launch_mx_product_parts(p, l.splits, stream));
+        HIP_OR_FAIL(launch_mx_loss_grad(l, n, lse, dloss, g, bf16, stream));
+      }
       if (dX) {
         const bool direct = whole || dX->type == COSTA_REAL_F32;
         HIP_OR_FAIL(product(false, g, bf16, m, cols, columns_of(wt, j, cols), alpha, j > 0 ? 1.0f : 0.0f,

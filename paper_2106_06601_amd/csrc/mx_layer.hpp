@@ -134,6 +134,14 @@ hipError_t launch_mx_loss_join(int64_t m, int64_t n, int64_t chunks, const LossS
 // g (m x p.n by rows; bfloat16 or float) <- dloss (exp(logit - lse) - [target]); g may be the first part of sums
 hipError_t launch_mx_loss_grad(const LogitsPart& p, int64_t vocabulary, const float* lse, const float* dloss, void* g,
                                bool bf16, hipStream_t stream);
+// Both in the product's own kernel (mx_tiles_loss.hip), where that takes one: statistics by mx_loss_tile_chunks() chunks of
+// columns; of the arguments C, beta and the workspace are not looked at.
+bool mx_loss_fused(costa_real type, int bits, int64_t m, int64_t n, int64_t k);
+int64_t mx_loss_tile_chunks(costa_real type, int bits, int64_t m, int64_t n, int64_t k);
+hipError_t launch_mx_loss_tiles(const ProductArgs& x, const int64_t* target, LossStat* stats, float* at,
+                                hipStream_t stream);
+hipError_t launch_mx_loss_grad_tiles(const ProductArgs& x, int64_t vocabulary, int64_t col0, const int64_t* target,
+                                     const float* lse, const float* dloss, void* g, bool bf16, hipStream_t stream);
 // y <- x: floats, to a row-major matrix
 hipError_t launch_mx_round(int64_t m, int64_t n, const float* x, const RowsView& y, costa_real type, hipStream_t stream);
 

@@ -75,7 +75,7 @@ __device__ inline void add_adapters(const AdapterAddArgs& a, TileSums<MT, NT>& t
 #pragma unroll
         for (int x = 0; x < 3; ++x) next[x] = spread[(min((int64_t)i, last) * steps * 3 + x) * 64];
       };
-      load_v(0);
+      if (has & 1) load_v(0);
       if (r0 + 32 > rank)  // (past the last rank was that again)
 #pragma unroll
         for (int q = 0; q < 8; ++q)
@@ -97,7 +97,7 @@ __device__ inline void add_adapters(const AdapterAddArgs& a, TileSums<MT, NT>& t
         v4u v[3];
 #pragma unroll
         for (int x = 0; x < 3; ++x) v[x] = next[x];
-        if (i + 1 < MT) load_v(i + 1);
+        if (i + 1 < MT && (has >> (i + 1) & 1)) load_v(i + 1);
         if (!(has >> i & 1)) continue;
         if (full >> i & 1) {  // all of the piece's rows
 #pragma unroll

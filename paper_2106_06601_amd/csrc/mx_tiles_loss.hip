@@ -1,0 +1,149 @@
+// Products with a vocabulary in tiles of the logits, whose sums go no further than a row's statistics or
+// the gradient of the logits: they are never written.
+//
+// A lane has, of 16 MT rows, one of each sixteen and four neighbouring columns of each of NT
+// pieces; a row's columns of a wave lie in four lanes.
+#include "mx_loss.hpp"
+#include "mx_tiles.hpp"
+
+namespace costa {
+namespace {
+
+struct LossTile {
+  float alpha;
+  int64_t n, col0;  // the vocabulary, and the first of the product's columns in it
+  const int64_t* target;
+  LossStat* stats;
+  float* at;
+  const float* lse;
+  const float* dloss;
+};
+
+// Largest logit and the sum of exponentials from it of a wave's columns, to stats[wave column * m + row]; the
+// target's logit, to at[row].
+template <int SRC, int BBITS, int BM, int BN>
+__global__ __launch_bounds__(kLanes) void tiles_loss_stats(Args p, LossTile a, uint32_t nm, uint32_t nn) {
+  constexpr int MT = BM / 2 / 16, NT = BN / (kWaves / 2) / 16;
+  TileSums<MT, NT> t;
+  tile_sums<SRC, false, BBITS, BM, BN, 2, 1, true, 0>(p, nm, nn, t);
+  const int lane = threadIdx.x % 64, l = lane % 16, g = lane / 16;
+  LossStat* const to = a.stats + t.col / (16 * NT) * p.m;
+  if (t.col >= p.n) return;
+  int64_t target[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) target[i] = a.target[min(t.row + 16 * i + l, p.m - 1)];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int64_t row = t.row + 16 * i + l, at = target[i] - t.col - 4 * g;
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float x = t.col + 16 * j + 4 * g + q < p.n ? a.alpha * t.acc[i][j][q] : -__builtin_inff();
+        t.acc[i][j][q] = x;
+        top = fmaxf(top, x);
+        if (at == 16 * j + q && target[i] < p.n && row < p.m) a.at[row] = x;
+      }
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float from = top == -__builtin_inff() ? 0.0f : top;
+    float sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) sum += exp_of(t.acc[i][j][q] - from);
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (g == 0 && row < p.m) to[row] = LossStat{top, sum};
+  }
+}
+
+// dloss (exp(logit - lse) - [target]) in the logits' place, to p.e.
+template <int SRC, int BBITS, int BM, int BN>
+__global__ __launch_bounds__(kLanes) void tiles_loss_grad(Args p, LossTile a, uint32_t nm, uint32_t nn) {
+  constexpr int MT = BM / 2 / 16, NT = BN / (kWaves / 2) / 16;
+  TileSums<MT, NT> t;
+  tile_sums<SRC, false, BBITS, BM, BN, 2, 1, true, 0>(p, nm, nn, t);
+  const int lane = threadIdx.x % 64, l = lane % 16, g = lane / 16;
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int64_t row = min(t.row + 16 * i + l, p.m - 1), target = a.target[row];
+    const bool counts = target >= 0 && target < a.n;
+    const float d = counts && a.dloss ? a.dloss[row] : 1.0f, lse = a.lse[row];
+    const int64_t at = target - a.col0 - t.col - 4 * g;
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        t.acc[i][j][q] = counts ? d * (exp_of(a.alpha * t.acc[i][j][q] - lse) - (at == 16 * j + q ? 1.0f : 0.0f)) : 0.0f;
+      }
+  }
+  put_wave<MT, NT>(p, t.acc, t.shared, t.wave, t.row, t.col);
+}
+
+int source_of(costa_real type) { return type == COSTA_REAL_BF16 ? SRC_BF16 : type == COSTA_REAL_F16 ? SRC_F16 : SRC_F32; }
+
+// The tile that a product takes; one of 128x128 where that is narrower.
+ProductPlan plan_loss(int src, int bits, int64_t m, int64_t n, int64_t k) {
+  ProductPlan r = plan_product(src, true, bits, m, n, k);
+  if (r.bn < 256) r.bm = r.bn = 128;
+  return r;
+}
+
+template <int SRC, int BBITS>
+hipError_t launch_loss(const Args& p, const LossTile& a, hipStream_t stream) {
+  constexpr int BM = parts_of(SRC) == 1 ? 256 : 128;
+  const ProductPlan plan = plan_loss(SRC, BBITS, p.m, p.n, p.k);
+  const uint32_t nm = (uint32_t)up_div(p.m, plan.bm), nn = (uint32_t)up_div(p.n, plan.bn);
+  const dim3 grid(nm * nn);
+  if (plan.bn == 256) {
+    if (a.stats) tiles_loss_stats<SRC, BBITS, BM, 256><<<grid, kLanes, 0, stream>>>(p, a, nm, nn);
+    else tiles_loss_grad<SRC, BBITS, BM, 256><<<grid, kLanes, 0, stream>>>(p, a, nm, nn);
+  } else {
+    if (a.stats) tiles_loss_stats<SRC, BBITS, 128, 128><<<grid, kLanes, 0, stream>>>(p, a, nm, nn);
+    else tiles_loss_grad<SRC, BBITS, 128, 128><<<grid, kLanes, 0, stream>>>(p, a, nm, nn);
+  }
+  return hipGetLastError();
+}
+template <int SRC>
+hipError_t launch_loss_bits(const Args& p, const LossTile& a, hipStream_t stream) {
+  return p.b.bits == 4 ? launch_loss<SRC, 4>(p, a, stream) : launch_loss<SRC, 8>(p, a, stream);
+}
+hipError_t launch_loss_type(costa_real type, const Args& p, const LossTile& a, hipStream_t stream) {
+  if (type == COSTA_REAL_BF16) return launch_loss_bits<SRC_BF16>(p, a, stream);
+  if (type == COSTA_REAL_F16) return launch_loss_bits<SRC_F16>(p, a, stream);
+  return launch_loss_bits<SRC_F32>(p, a, stream);
+}
+
+Args args_of(const ProductArgs& a, const Epilogue& e) {
+  return Args{a.m, a.n, a.k, MxView{}, a.b, a.real, a.a_rs, 1, e, 0};
+}
+
+}  // namespace
+
+bool mx_loss_fused(costa_real type, int bits, int64_t m, int64_t n, int64_t k) {
+  if (k == 0) return false;
+  const ProductPlan r = plan_product(source_of(type), true, bits, m, n, k);
+  // (tiles of 128 columns and more, whole sums: where there are fewer the logits are few, too)
+  return r.variant == TILES_BF16 && r.splits == 1 && r.bn >= 128 && up_div(m, 128) * up_div(n, 128) <= kTileSlice;
+}
+
+int64_t mx_loss_tile_chunks(costa_real type, int bits, int64_t m, int64_t n, int64_t k) {
+  return up_div(n, plan_loss(source_of(type), bits, m, n, k).bn / 4);
+}
+
+hipError_t launch_mx_loss_tiles(const ProductArgs& x, const int64_t* target, LossStat* stats, float* at,
+                                hipStream_t stream) {
+  return launch_loss_type(x.a_type, args_of(x, Epilogue{}),
+                          LossTile{x.alpha, x.n, 0, target, stats, at, nullptr, nullptr}, stream);
+}
+
+hipError_t launch_mx_loss_grad_tiles(const ProductArgs& x, int64_t vocabulary, int64_t col0, const int64_t* target,
+                                     const float* lse, const float* dloss, void* g, bool bf16, hipStream_t stream) {
+  const Epilogue e{g, x.n, 1, bf16 ? COSTA_REAL_BF16 : COSTA_REAL_F32, x.n % 4 == 0, 1.0f, 0.0f};
+  return launch_loss_type(x.a_type, args_of(x, e),
+                          LossTile{x.alpha, vocabulary, col0, target, nullptr, nullptr, lse, dloss}, stream);
+}
+
+}  // namespace costa

@@ -121,6 +121,42 @@ def test_loss_and_gradients(shape, dtype, bits):
                     assert (np.abs(wide(DW) - dw) <= ew + HALF[out] * np.abs(dw) + TINY[out]).all()
 
 
+# logits enough for the products' own tiles to keep them to themselves: tiles of 256 columns and of 128, the last
+# ones cut in both directions
+TILED = [(130, 33000, 40), (2047, 4101, 36), (1000, 9002, 24), (700, 16385, 8)]
+
+
+@pytest.mark.parametrize("shape", TILED, ids=str)
+@pytest.mark.parametrize("dtype,bits", [("f32", 4), ("f32", 8), ("bf16", 4), ("bf16", 8), ("f16", 4), ("f16", 8)])
+def test_loss_of_many_logits(shape, dtype, bits):
+    m, n, k = shape
+    out = "bf16" if dtype == "bf16" else "f32"
+    c = Case(m, n, k, dtype, bits, -0.5)
+    c.target[-1], c.target[0], c.target[1] = n - 1, 0, n // 256 * 256  # (a tile's corners)
+    t = c.target.numpy()
+    c.counts = (t >= 0) & (t < n)
+    c.at = np.where(c.counts, t, 0)
+    i = np.arange(m)
+    c.loss = np.where(c.counts, c.lse - c.L[i, c.at], 0)
+    c.loss_off = np.where(c.counts, c.E[i, c.at] + c.lse_off + 2 * U * np.abs(c.loss), 0)
+    x, target = strided(c.x, dtype, k + 1), c.target.cuda()
+    least, most = C.costa_mx_loss_workspace(m, n, k, False)
+    got = []
+    for size in (least, most):
+        loss, lse = torch.full((m,), 7.0).cuda(), torch.full((m,), 7.0).cuda()
+        C.costa_mx_loss(-0.5, x, c.wq, target, loss, lse, workspace=torch.full((size,), 0xFF, dtype=torch.uint8).cuda())
+        assert (np.abs(wide(lse) - c.lse) <= c.lse_off).all()
+        assert (np.abs(wide(loss) - c.loss) <= c.loss_off).all()
+    dx, ex, dw, ew = c.gradients(out == "bf16", np.zeros((n, k)))
+    least, most = C.costa_mx_loss_workspace(m, n, k, True)
+    for size in (least, least + (most - least) // 20, most):
+        DX, DW = strided(np.full((m, k), np.nan), out, k + 1), strided(np.full((n, k), np.nan), out, k + 2)
+        C.costa_mx_loss_backward(-0.5, x, c.wq, target, lse, c.d.cuda(), WT=c.wtq, dX=DX, XT=c.xtq, dW=DW,
+                                 workspace=torch.full((size,), 0xFF, dtype=torch.uint8).cuda())
+        assert (np.abs(wide(DX) - dx) <= ex + HALF[out] * np.abs(dx) + TINY[out]).all()
+        assert (np.abs(wide(DW) - dw) <= ew + HALF[out] * np.abs(dw) + TINY[out]).all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_pieces_of_a_larger_vocabulary(dtype):
     """Some thousand columns in pieces of every size that a workspace allows."""
