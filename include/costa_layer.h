@@ -114,9 +114,10 @@ costa_status costa_mx_loss(float alpha, const costa_matrix* X, const costa_mx* W
  *     dW <- alpha G^T X'^ + beta dW    X' = XT^T, XT = mx(X^T), k x m
  *
  * dloss (NULL: ones): m floats, the gradient that reaches each row's loss.  dX with WT and dW
- * with XT may be NULL, not both.  lse: what costa_mx_loss() gave.  G is held in
- * bfloat16 where dX and dW (those wanted) are BF16, in 32 bits else; probabilities below
- * 2^-126 are 0. */
+ * with XT may be NULL, not both.  lse: what costa_mx_loss() gave.  Probabilities below 2^-126 are 0.
+ * G is held in 32 bits, or, where dX and dW (those wanted) are BF16, in bfloat16 as G divided by
+ * the largest |dloss| (dW: where the vocabulary is large enough for whole tiles); it goes
+ * back in before dX and dW are rounded. */
 costa_status costa_mx_loss_backward(float alpha, const costa_matrix* X, const costa_mx* W, const int64_t* target,
                                     const float* lse, const float* dloss, const costa_mx* WT, const costa_matrix* dX,
                                     const costa_mx* XT, float beta, const costa_matrix* dW, void* workspace,

@@ -445,7 +445,7 @@ extern "C" costa_status costa_mx_loss_workspace(int64_t m, int64_t n, int64_t k,
                                    std::max(sums, mx_product_workspace(m, std::min(n, piece_columns(m, n, sums, 4)), k)),
                                (size_t)m * ((n + 31) / 32) * sizeof(LossStat)));
     } else {
-      const size_t dx = up16((size_t)m * k * 4);  // what dX is summed in
+      const size_t dx = up16((size_t)m * k * 4) + 16;  // what dX is summed in, and G's scale
       give(least, dx + up16(least_piece(m, n, 4)) + up16(least_piece(m, n, 4)));
       const size_t g = piece_bytes(m, n, 4);
       const int64_t per = piece_columns(m, n, g, 4);
@@ -538,34 +538,43 @@ extern "C" costa_status costa_mx_loss_backward(float alpha, const costa_matrix* 
     u.add("dX", dX, true), u.add("dW", dW, true), u.workspace(workspace, workspace_bytes);
     CHECKED(u.check());
     if (k == 0) return COSTA_SUCCESS;  // no gradient has elements
-    auto product = [&](bool turned, const void* g, bool bf16, int64_t gm, int64_t gn, const MxView& b, float al, float be,
-                       void* c, int64_t ld, costa_real type, char* room, size_t bytes) {
-      ProductArgs p{};  // of G (gm x gn), turned or not
+    // alpha G B^^T or alpha G^T B^^T + be C, of G (gm x gn); by: a factor in device memory (null: none)
+    auto product = [&](bool turned, const void* g, bool bf16, int64_t gm, int64_t gn, const MxView& b, float be, void* c,
+                       int64_t ld, costa_real type, char* room, size_t bytes, const float* by) {
+      ProductArgs p{};
       p.m = turned ? gn : gm, p.k = turned ? gm : gn, p.n = b.rows;
       p.real = g;
       p.a_rs = turned ? 1 : gn, p.a_cs = turned ? gn : 1;
       p.a_type = bf16 ? COSTA_REAL_BF16 : COSTA_REAL_F32;
       p.b = b;
       p.c = c, p.c_rs = ld, p.c_cs = 1, p.c_type = type;
-      p.alpha = al, p.beta = be;
+      p.alpha = alpha, p.beta = be;
       p.workspace = reinterpret_cast<float*>(room), p.workspace_bytes = bytes;
-      return p.m == 0 || p.n == 0 ? hipSuccess : launch_mx_product(p, stream);
+      return p.m == 0 || p.n == 0 ? hipSuccess : by ? launch_mx_loss_dw(p, by, stream) : launch_mx_product(p, stream);
     };
     if (m == 0 || n == 0) {  // sums over nothing
-      if (dX) HIP_OR_FAIL(product(false, nullptr, true, m, 0, columns_of(wt, 0, 0), alpha, 0.0f, dX->data, dX->ld, dX->type, nullptr, 0));
-      if (dW) HIP_OR_FAIL(product(true, nullptr, true, 0, n, columns_of(xt, 0, 0), alpha, beta, dW->data, dW->ld, dW->type, nullptr, 0));
+      if (dX) HIP_OR_FAIL(product(false, nullptr, true, m, 0, columns_of(wt, 0, 0), 0.0f, dX->data, dX->ld, dX->type, nullptr, 0, nullptr));
+      if (dW) HIP_OR_FAIL(product(true, nullptr, true, 0, n, columns_of(xt, 0, 0), beta, dW->data, dW->ld, dW->type, nullptr, 0, nullptr));
       return COSTA_SUCCESS;
     }
-    const bool bf16 = (!dX || dX->type == COSTA_REAL_BF16) && (!dW || dW->type == COSTA_REAL_BF16);
     char* room = static_cast<char*>(workspace);
     float* const sum = reinterpret_cast<float*>(room);  // of dX
     room += up16((size_t)m * k * 4);
-    size_t left = workspace_bytes - up16((size_t)m * k * 4);
+    float* const scale = reinterpret_cast<float*>(room);
+    room += 16;
+    size_t left = workspace_bytes - up16((size_t)m * k * 4) - 16;
     // half for G, half for the logits, where they are kept, and for what products split
     const size_t half = std::min(left / 32 * 16, up16(piece_bytes(m, n, 4)));
-    int64_t per = piece_columns(m, n, half, bf16 ? 2 : 4);
-    const bool fused = mx_loss_fused(X->type, w.bits, m, per, k);
-    if (!fused) per = piece_columns(m, n, half, 4);
+    int64_t per = piece_columns(m, n, half, 2);
+    bool fused = mx_loss_fused(X->type, w.bits, m, per, k);
+    const bool bf16 = (!dX || dX->type == COSTA_REAL_BF16) && (!dW || dW->type == COSTA_REAL_BF16) &&
+                      (!dW || (fused && mx_loss_dw_fused(xt.bits, m, per, k)));
+    if (!bf16 || !fused) {
+      per = piece_columns(m, n, half, 4);
+      fused = mx_loss_fused(X->type, w.bits, m, per, k);
+    }
+    if (bf16) HIP_OR_FAIL(launch_mx_loss_scale(m, dloss, scale, stream));
+    const float* const by = bf16 ? scale : nullptr;
     void* const g = room;
     const size_t taken = up16((size_t)m * per * (fused && bf16 ? 2 : 4));
     room += taken, left -= taken;
@@ -574,23 +583,25 @@ extern "C" costa_status costa_mx_loss_backward(float alpha, const costa_matrix* 
       const int64_t cols = std::min(per, n - j);
       ProductArgs p = logits_of(X, w, j, cols, alpha);
       if (fused) {
-        HIP_OR_FAIL(launch_mx_loss_grad_tiles(p, n, j, target, lse, dloss, g, bf16, stream));
+        HIP_OR_FAIL(launch_mx_loss_grad_tiles(p, n, j, target, lse, dloss, by, g, bf16, stream));
       } else {
         p.workspace = reinterpret_cast<float*>(room), p.workspace_bytes = left;
         LogitsPart l{m, cols, j, p.workspace, 0, alpha, target};
         HIP_OR_FAIL(launch_mx_product_parts(p, l.splits, stream));
-        HIP_OR_FAIL(launch_mx_loss_grad(l, n, lse, dloss, g, bf16, stream));
+        HIP_OR_FAIL(launch_mx_loss_grad(l, n, lse, dloss, by, g, bf16, stream));
       }
       if (dX) {
-        const bool direct = whole || dX->type == COSTA_REAL_F32;
-        HIP_OR_FAIL(product(false, g, bf16, m, cols, columns_of(wt, j, cols), alpha, j > 0 ? 1.0f : 0.0f,
-                            direct ? dX->data : sum, direct ? dX->ld : k, direct ? dX->type : COSTA_REAL_F32, room, left));
+        const bool direct = !bf16 && (whole || dX->type == COSTA_REAL_F32);
+        HIP_OR_FAIL(product(false, g, bf16, m, cols, columns_of(wt, j, cols), j > 0 ? 1.0f : 0.0f,
+                            direct ? dX->data : sum, direct ? dX->ld : k, direct ? dX->type : COSTA_REAL_F32, room, left,
+                            nullptr));
       }
       if (dW)
-        HIP_OR_FAIL(product(true, g, bf16, m, cols, xt, alpha, beta,
-                            static_cast<char*>(dW->data) + j * dW->ld * real_size(dW->type), dW->ld, dW->type, room, left));
+        HIP_OR_FAIL(product(true, g, bf16, m, cols, xt, beta,
+                            static_cast<char*>(dW->data) + j * dW->ld * real_size(dW->type), dW->ld, dW->type, room, left, by));
     }
-    if (dX && !whole && dX->type != COSTA_REAL_F32) HIP_OR_FAIL(launch_mx_round(m, k, sum, rows_of(dX), dX->type, stream));
+    if (dX && (bf16 || (!whole && dX->type != COSTA_REAL_F32)))
+      HIP_OR_FAIL(launch_mx_round(m, k, sum, by, rows_of(dX), dX->type, stream));
     return COSTA_SUCCESS;
   });
 }

@@ -132,8 +132,9 @@ hipError_t launch_mx_loss_stats(const LogitsPart& p, LossStat* stats, float* at,
 hipError_t launch_mx_loss_join(int64_t m, int64_t n, int64_t chunks, const LossStat* stats, const float* at,
                                const int64_t* target, float* loss, float* lse, hipStream_t stream);
 // g (m x p.n by rows; bfloat16 or float) <- dloss (exp(logit - lse) - [target]); g may be the first part of sums
-hipError_t launch_mx_loss_grad(const LogitsPart& p, int64_t vocabulary, const float* lse, const float* dloss, void* g,
-                               bool bf16, hipStream_t stream);
+// / *scale (null: 1)
+hipError_t launch_mx_loss_grad(const LogitsPart& p, int64_t vocabulary, const float* lse, const float* dloss,
+                               const float* scale, void* g, bool bf16, hipStream_t stream);
 // Both in the product's own kernel (mx_tiles_loss.hip), where that takes one: statistics by mx_loss_tile_chunks() chunks of
 // columns; of the arguments C, beta and the workspace are not looked at.
 bool mx_loss_fused(costa_real type, int bits, int64_t m, int64_t n, int64_t k);
@@ -141,8 +142,17 @@ int64_t mx_loss_tile_chunks(costa_real type, int bits, int64_t m, int64_t n, int
 hipError_t launch_mx_loss_tiles(const ProductArgs& x, const int64_t* target, LossStat* stats, float* at,
                                 hipStream_t stream);
 hipError_t launch_mx_loss_grad_tiles(const ProductArgs& x, int64_t vocabulary, int64_t col0, const int64_t* target,
-                                     const float* lse, const float* dloss, void* g, bool bf16, hipStream_t stream);
-// y <- x: floats, to a row-major matrix
-hipError_t launch_mx_round(int64_t m, int64_t n, const float* x, const RowsView& y, costa_real type, hipStream_t stream);
+                                     const float* lse, const float* dloss, const float* scale, void* g, bool bf16,
+                                     hipStream_t stream);
+// scale <- the largest |dloss| (1 where that is 0 or not finite, and without dloss): what a G in bfloat16
+// is divided by, and its products are multiplied by.
+hipError_t launch_mx_loss_scale(int64_t m, const float* dloss, float* scale, hipStream_t stream);
+// The gradient of the vocabulary's weights from a G in bfloat16, with the scale out of device memory:
+// C <- alpha scale G^T B^^T + beta C, where the products' tiles take it (G m x n by rows, n rows of C).
+bool mx_loss_dw_fused(int bits, int64_t m, int64_t n, int64_t k);
+hipError_t launch_mx_loss_dw(const ProductArgs& a, const float* scale, hipStream_t stream);
+// y <- scale x (scale null: x): floats, to a row-major matrix
+hipError_t launch_mx_round(int64_t m, int64_t n, const float* x, const float* scale, const RowsView& y, costa_real type,
+                           hipStream_t stream);
 
 }  // namespace costa

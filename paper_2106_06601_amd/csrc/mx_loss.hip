@@ -96,7 +96,7 @@ __global__ __launch_bounds__(1024) void loss_join(int64_t m, int64_t n, int64_t 
 
 template <int GSRC>
 __global__ __launch_bounds__(256) void loss_grad(LogitsPart p, int64_t vocabulary, const float* lse,
-                                                 const float* dloss, void* g) {
+                                                 const float* dloss, const float* scale, void* g) {
   const int64_t upr = (p.n + 7) / 8, units = p.m * upr;
   for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (int64_t)gridDim.x * 256) {
     const int64_t row = ((u | upr) >> 32) == 0 ? (int64_t)((uint32_t)u / (uint32_t)upr) : u / upr, c = (u - row * upr) * 8;
@@ -104,16 +104,33 @@ __global__ __launch_bounds__(256) void loss_grad(LogitsPart p, int64_t vocabular
     logits8(p, row, c, x);
     const int64_t t = p.target[row];
     const bool counts = t >= 0 && t < vocabulary;
-    const float d = counts && dloss ? dloss[row] : 1.0f, l = lse[row];
+    const float d = counts && dloss ? (scale ? dloss[row] / *scale : dloss[row]) : 1.0f, l = lse[row];
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = counts ? d * (exp_of(x[i] - l) - (t - p.col0 - c == i ? 1.0f : 0.0f)) : 0.0f;
     put8<GSRC>(static_cast<Elem<GSRC>*>(g) + row * p.n, c, p.n, x);
   }
 }
 
+__global__ __launch_bounds__(1024) void loss_scale(int64_t m, const float* dloss, float* scale) {
+  __shared__ uint32_t red[16];
+  uint32_t top = 0;  // (magnitudes' bits: NaN above infinity above the finite ones)
+  if (dloss)
+#pragma unroll 8
+    for (int64_t i = threadIdx.x; i < m; i += 1024) top = max(top, magnitude(dloss[i]));
+#pragma unroll
+  for (int by = 32; by > 0; by /= 2) top = max(top, (uint32_t)__shfl_xor((int)top, by));
+  if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = top;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) top = max(top, red[i]);
+  *scale = top == 0 || top >= 0x7f800000u ? 1.0f : __builtin_bit_cast(float, top);
+}
+
 template <int SRC>
-__global__ __launch_bounds__(256) void round_rows(int64_t m, int64_t n, const float* x, RowsView y) {
+__global__ __launch_bounds__(256) void round_rows(int64_t m, int64_t n, const float* x, const float* scale, RowsView y) {
   const int64_t upr = (n + 7) / 8;
+  const float by = scale ? *scale : 1.0f;
   for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < m * upr; u += (int64_t)gridDim.x * 256) {
     const int64_t row = u / upr, c = (u - row * upr) * 8;
     float v[8] = {};
@@ -121,6 +138,8 @@ __global__ __launch_bounds__(256) void round_rows(int64_t m, int64_t n, const fl
     else
       for (int i = 0; i < 8; ++i)
         if (c + i < n) v[i] = x[row * n + c + i];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= by;
     put8<SRC>(line_to<SRC>(y, row), c, n, v);
   }
 }
@@ -150,19 +169,25 @@ hipError_t launch_mx_loss_join(int64_t m, int64_t n, int64_t chunks, const LossS
   return hipGetLastError();
 }
 
-hipError_t launch_mx_loss_grad(const LogitsPart& p, int64_t vocabulary, const float* lse, const float* dloss, void* g,
-                               bool bf16, hipStream_t stream) {
-  const dim3 grid = groups_for(p.m * up_div(p.n, 8));
-  if (bf16) loss_grad<SRC_BF16><<<grid, 256, 0, stream>>>(p, vocabulary, lse, dloss, g);
-  else loss_grad<SRC_F32><<<grid, 256, 0, stream>>>(p, vocabulary, lse, dloss, g);
+hipError_t launch_mx_loss_scale(int64_t m, const float* dloss, float* scale, hipStream_t stream) {
+  loss_scale<<<1, 1024, 0, stream>>>(m, dloss, scale);
   return hipGetLastError();
 }
 
-hipError_t launch_mx_round(int64_t m, int64_t n, const float* x, const RowsView& y, costa_real type, hipStream_t stream) {
+hipError_t launch_mx_loss_grad(const LogitsPart& p, int64_t vocabulary, const float* lse, const float* dloss,
+                               const float* scale, void* g, bool bf16, hipStream_t stream) {
+  const dim3 grid = groups_for(p.m * up_div(p.n, 8));
+  if (bf16) loss_grad<SRC_BF16><<<grid, 256, 0, stream>>>(p, vocabulary, lse, dloss, scale, g);
+  else loss_grad<SRC_F32><<<grid, 256, 0, stream>>>(p, vocabulary, lse, dloss, scale, g);
+  return hipGetLastError();
+}
+
+hipError_t launch_mx_round(int64_t m, int64_t n, const float* x, const float* scale, const RowsView& y, costa_real type,
+                           hipStream_t stream) {
   const dim3 grid = groups_for(m * up_div(n, 8));
-  if (type == COSTA_REAL_F32) round_rows<SRC_F32><<<grid, 256, 0, stream>>>(m, n, x, y);
-  else if (type == COSTA_REAL_BF16) round_rows<SRC_BF16><<<grid, 256, 0, stream>>>(m, n, x, y);
-  else round_rows<SRC_F16><<<grid, 256, 0, stream>>>(m, n, x, y);
+  if (type == COSTA_REAL_F32) round_rows<SRC_F32><<<grid, 256, 0, stream>>>(m, n, x, scale, y);
+  else if (type == COSTA_REAL_BF16) round_rows<SRC_BF16><<<grid, 256, 0, stream>>>(m, n, x, scale, y);
+  else round_rows<SRC_F16><<<grid, 256, 0, stream>>>(m, n, x, scale, y);
   return hipGetLastError();
 }
 

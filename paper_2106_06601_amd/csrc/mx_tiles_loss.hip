@@ -17,6 +17,7 @@ struct LossTile {
   float* at;
   const float* lse;
   const float* dloss;
+  const float* scale;  // dloss is divided by it (null: 1)
 };
 
 // Largest logit and the sum of exponentials from it of a wave's columns, to stats[wave column * m + row]; the
@@ -70,7 +71,7 @@ __global__ __launch_bounds__(kLanes) void tiles_loss_grad(Args p, LossTile a, ui
   for (int i = 0; i < MT; ++i) {
     const int64_t row = min(t.row + 16 * i + l, p.m - 1), target = a.target[row];
     const bool counts = target >= 0 && target < a.n;
-    const float d = counts && a.dloss ? a.dloss[row] : 1.0f, lse = a.lse[row];
+    const float d = counts && a.dloss ? (a.scale ? a.dloss[row] / *a.scale : a.dloss[row]) : 1.0f, lse = a.lse[row];
     const int64_t at = target - a.col0 - t.col - 4 * g;
 #pragma unroll
     for (int j = 0; j < NT; ++j)
@@ -82,6 +83,16 @@ __global__ __launch_bounds__(kLanes) void tiles_loss_grad(Args p, LossTile a, ui
   put_wave<MT, NT>(p, t.acc, t.shared, t.wave, t.row, t.col);
 }
 
+// A product with a transposed left operand in bfloat16 whose factor is in device memory.
+template <int BBITS, int BM, int BN, bool EDGE>
+__global__ __launch_bounds__(kLanes) void tiles_loss_dw(Args p, const float* scale, uint32_t nm, uint32_t nn) {
+  constexpr int MT = BM / 2 / 16, NT = BN / (kWaves / 2) / 16;
+  TileSums<MT, NT> t;
+  tile_sums<SRC_BF16, true, BBITS, BM, BN, 2, 1, EDGE, 0>(p, nm, nn, t);
+  p.e.alpha *= *scale;
+  put_wave<MT, NT>(p, t.acc, t.shared, t.wave, t.row, t.col);
+}
+
 int source_of(costa_real type) { return type == COSTA_REAL_BF16 ? SRC_BF16 : type == COSTA_REAL_F16 ? SRC_F16 : SRC_F32; }
 
 // The tile that a product takes; one of 128x128 where that is narrower.
@@ -89,6 +100,18 @@ ProductPlan plan_loss(int src, int bits, int64_t m, int64_t n, int64_t k) {
   ProductPlan r = plan_product(src, true, bits, m, n, k);
   if (r.bn < 256) r.bm = r.bn = 128;
   return r;
+}
+
+template <int BBITS>
+hipError_t launch_dw(const Args& p, const float* scale, hipStream_t stream) {
+  ProductPlan plan = plan_product(SRC_BF16, false, BBITS, p.m, p.n, p.k);
+  if (plan.bn < 256) plan.bm = plan.bn = 128;
+  const uint32_t nm = (uint32_t)up_div(p.m, plan.bm), nn = (uint32_t)up_div(p.n, plan.bn);
+  const dim3 grid(nm * nn);
+  if (plan.bn < 256) tiles_loss_dw<BBITS, 128, 128, true><<<grid, kLanes, 0, stream>>>(p, scale, nm, nn);
+  else if (p.m % 4 == 0) tiles_loss_dw<BBITS, 256, 256, false><<<grid, kLanes, 0, stream>>>(p, scale, nm, nn);
+  else tiles_loss_dw<BBITS, 256, 256, true><<<grid, kLanes, 0, stream>>>(p, scale, nm, nn);
+  return hipGetLastError();
 }
 
 template <int SRC, int BBITS>
@@ -136,14 +159,27 @@ int64_t mx_loss_tile_chunks(costa_real type, int bits, int64_t m, int64_t n, int
 hipError_t launch_mx_loss_tiles(const ProductArgs& x, const int64_t* target, LossStat* stats, float* at,
                                 hipStream_t stream) {
   return launch_loss_type(x.a_type, args_of(x, Epilogue{}),
-                          LossTile{x.alpha, x.n, 0, target, stats, at, nullptr, nullptr}, stream);
+                          LossTile{x.alpha, x.n, 0, target, stats, at, nullptr, nullptr, nullptr}, stream);
 }
 
 hipError_t launch_mx_loss_grad_tiles(const ProductArgs& x, int64_t vocabulary, int64_t col0, const int64_t* target,
-                                     const float* lse, const float* dloss, void* g, bool bf16, hipStream_t stream) {
+                                     const float* lse, const float* dloss, const float* scale, void* g, bool bf16,
+                                     hipStream_t stream) {
   const Epilogue e{g, x.n, 1, bf16 ? COSTA_REAL_BF16 : COSTA_REAL_F32, x.n % 4 == 0, 1.0f, 0.0f};
   return launch_loss_type(x.a_type, args_of(x, e),
-                          LossTile{x.alpha, vocabulary, col0, target, nullptr, nullptr, lse, dloss}, stream);
+                          LossTile{x.alpha, vocabulary, col0, target, nullptr, nullptr, lse, dloss, scale}, stream);
+}
+
+bool mx_loss_dw_fused(int bits, int64_t m, int64_t n, int64_t k) {
+  const ProductPlan r = plan_product(SRC_BF16, false, bits, n, k, m);
+  return r.variant == TILES_BF16 && r.splits == 1 && r.bn >= 128 && up_div(n, 128) * up_div(k, 128) <= kTileSlice;
+}
+
+hipError_t launch_mx_loss_dw(const ProductArgs& a, const float* scale, hipStream_t stream) {
+  const int64_t es = a.c_type == COSTA_REAL_F32 ? 4 : 2;
+  const Epilogue e{a.c, a.c_rs, 1, a.c_type, a.c_rs % 4 == 0 && (uintptr_t)a.c % (4 * es) == 0, a.alpha, a.beta};
+  const Args p{a.m, a.n, a.k, MxView{}, a.b, a.real, a.a_rs, a.a_cs, e, 0};
+  return a.b.bits == 4 ? launch_dw<4>(p, scale, stream) : launch_dw<8>(p, scale, stream);
 }
 
 }  // namespace costa

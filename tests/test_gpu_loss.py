@@ -5,7 +5,7 @@ its row (the log sum is a mean's shift at most), by 2 (n / 256 + 40) * 2^-24 for
 n / 256, joins, the exponential's and the logarithm's last places) and by 2^-24 of |lse|; loss by E of the target's logit and as much.
 The gradient G = d (exp(L - lse) - 1_t): the exponent off by e = E + (lse's) + 4 * 2^-24 (1 + |L - lse|), so |d| p e more, and 2 * 2^-24 |G|;
 an exponential below 2^-126 is 0 (the instruction has no subnormal results), and of a float G what is below 2^-133 does not
-enter a product: 2^-126 |d| + 2^-133 (with 40 times the usual logits, probabilities of 8e-43 came out as 0); in bfloat16 half a step, 2^-8 |G| and 2^-133.  dX, dW: G's bound times |W'|, |X'|, sums in 32 bits with
+enter a product: 2^-126 |d| + 2^-133 (with 40 times the usual logits, probabilities of 8e-43 came out as 0); in bfloat16 (as a part of the largest |d|, D) half a step, 2^-8 |G| and 2^-133 D.  dX, dW: G's bound times |W'|, |X'|, sums in 32 bits with
 (2 (length / 32 + 12) + 8) * 2^-24 (a piece more or less is an addition more: the pieces' number on top), and the type's half step.
 """
 import numpy as np
@@ -78,7 +78,7 @@ class Case:
         off = p * (self.E + self.lse_off[:, None] + 4 * U * (1 + np.abs(self.L - self.lse[:, None]))) + 4 * U * (np.abs(g) + np.abs(d) * (np.abs(g) > p)) + 2.0**-126 * np.abs(d) + 2.0**-133
         off[~self.counts] = 0
         if bf16:
-            off += HALF["bf16"] * (np.abs(g) + off) + TINY["bf16"]
+            off += (HALF["bf16"] + 2 * U) * (np.abs(g) + off) + TINY["bf16"] * max(1, np.abs(d).max())
         a, pieces = abs(self.alpha), 2 + self.n / 256
         dx, dw = self.alpha * (g @ self.wt.T), self.alpha * (g.T @ self.xt.T) + beta_dw
         ex = a * (off @ np.abs(self.wt).T + (2 * (self.n / 32 + 12) + 8 + pieces) * U * (np.abs(g) @ np.abs(self.wt).T))
@@ -107,7 +107,7 @@ def test_loss_and_gradients(shape, dtype, bits):
         for wx, ww, d in ((True, True, True), (True, False, False), (False, True, True)):
             beta = 0.5 if ww and wx else 0.0
             dw0 = torch.randn(n, k).to(TORCH[out])
-            bf16 = out == "bf16"
+            bf16 = out == "bf16"  # (at most so coarse)
             dx, ex, dw, ew = c.gradients(bf16, beta * wide(dw0), None if d else np.ones(m))
             for size in (None, *C.costa_mx_loss_workspace(m, n, k, True)):
                 ws = None if size is None else torch.full((size,), 0xFF, dtype=torch.uint8).cuda()
@@ -124,10 +124,13 @@ def test_loss_and_gradients(shape, dtype, bits):
 # logits enough for the products' own tiles to keep them to themselves: tiles of 256 columns and of 128, the last
 # ones cut in both directions
 TILED = [(130, 33000, 40), (2047, 4101, 36), (1000, 9002, 24), (700, 16385, 8)]
+# and, in bfloat16, for those of the weights' gradient (rows in fours and odd, tiles of 256 and of 128)
+WEIGHTS = [(512, 8200, 1030), (300, 8201, 1024), (260, 2500, 520)]
 
 
-@pytest.mark.parametrize("shape", TILED, ids=str)
-@pytest.mark.parametrize("dtype,bits", [("f32", 4), ("f32", 8), ("bf16", 4), ("bf16", 8), ("f16", 4), ("f16", 8)])
+@pytest.mark.parametrize("shape,dtype,bits", [
+    *[(s, *t) for s in TILED for t in (("f32", 4), ("f32", 8), ("bf16", 4), ("bf16", 8), ("f16", 4), ("f16", 8))],
+    *[(s, "bf16", 4) for s in WEIGHTS]], ids=str)
 def test_loss_of_many_logits(shape, dtype, bits):
     m, n, k = shape
     out = "bf16" if dtype == "bf16" else "f32"
