@@ -72,29 +72,9 @@ __global__ __launch_bounds__(256) void adapter_dots_row(AdapterDotsArgs p, int64
     p.v[row * p.v_ld + r] = r < rank ? (red[0][j] + red[1][j]) + (red[2][j] + red[3][j]) : 0.0f;
 }
 
-// c's elements c .. c + 7 of a row: the product's parts, what the adapter adds, c.
+// v, with what c holds there, to c's elements c .. c + 7 of a row.
 template <int CSRC>
-__device__ inline void put_sums(const AdapterAddArgs& p, int64_t row, int64_t c, const float add[8]) {
-  float v[8] = {};
-  const bool all = c + 8 <= p.n;
-  const float* part = p.parts + row * p.n + c;
-  for (int s = 0; s < p.splits; ++s, part += p.m * p.n) {
-    if (all) {
-      float w[8];
-      __builtin_memcpy(w, part, sizeof w);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] += w[i];
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (c + i < p.n) v[i] += part[i];
-    }
-  }
-  if (p.splits > 0)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] *= p.alpha;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] += add[i];
+__device__ inline void put_scaled(const AdapterAddArgs& p, int64_t row, int64_t c, float v[8]) {
   if (p.beta != 0.0f) {
     const Elem<CSRC>* old = static_cast<const Elem<CSRC>*>(p.c.data) + row * p.c.ld + c;
 #pragma unroll
@@ -103,45 +83,73 @@ __device__ inline void put_sums(const AdapterAddArgs& p, int64_t row, int64_t c,
   }
   put8<CSRC>(line_to<CSRC>(p.c, row), c, p.n, v);
 }
-__device__ inline void put_sums_typed(const AdapterAddArgs& p, int64_t row, int64_t c, const float add[8]) {
-  if (p.c_type == COSTA_REAL_F32) put_sums<SRC_F32>(p, row, c, add);
-  else if (p.c_type == COSTA_REAL_BF16) put_sums<SRC_BF16>(p, row, c, add);
-  else put_sums<SRC_F16>(p, row, c, add);
-}
 
-// A workgroup has 2048 columns of a row, eight a lane.
+constexpr int kAddRanks = 8;  // rows of an adapter that are on their way at once
+// A workgroup has 2048 columns of a row, eight a lane: the product's parts, what the adapter
+// adds, c.  (Of the adapter all rows are read, those past its rank for nothing: how many there are
+// is known later than where they are.)
 template <int SRC, bool WIDE>
 __global__ __launch_bounds__(256) void adapter_add_row(AdapterAddArgs p, int64_t row0, int64_t col0) {
   const int64_t row = row0 + blockIdx.x, c = col0 + ((int64_t)blockIdx.y * 256 + threadIdx.x) * 8;
+  const bool all = c + 8 <= p.n;
   const int32_t a = adapter_of(p.at, row);
-  const int rank = rank_of(p.at, a);
-  float add[8] = {};
-  if (rank > 0) {
-    const float* const v = p.v + row * p.v_ld;
-#pragma unroll 8
-    for (int r = 0; r < rank; ++r) {
-      Raw8<SRC> raw;
-      float b[8];
-      get8<SRC, WIDE>(raw, line_of<SRC>(p.low, (int64_t)a * p.at.rank + r), c, p.n);
-      floats8<SRC, WIDE>(raw, c, p.n, b);
-      const float x = v[r];
+  float v[8] = {};
+  const float* part = p.parts + row * p.n + c;
+#pragma unroll 4
+  for (int s = 0; s < p.splits; ++s, part += p.m * p.n) {
+    float w[8] = {};
+    if (all) __builtin_memcpy(w, part, sizeof w);
+    else
 #pragma unroll
-      for (int i = 0; i < 8; ++i) add[i] = fmaf(x, b[i], add[i]);
-    }
-    const float s = scale_of(p.at, a);
+      for (int i = 0; i < 8; ++i)
+        if (c + i < p.n) w[i] = part[i];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) add[i] *= s;
+    for (int i = 0; i < 8; ++i) v[i] += w[i];
   }
-  if (c < p.n) put_sums_typed(p, row, c, add);
+  if (p.splits > 0)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= p.alpha;
+  if (a >= 0) {
+    const int rank = rank_of(p.at, a);
+    const float s = scale_of(p.at, a);
+    const float* const x = p.v + row * p.v_ld;
+    const void* const low = line_of<SRC>(p.low, (int64_t)a * p.at.rank);
+    float add[8] = {};
+    for (int r0 = 0; r0 < p.at.rank; r0 += kAddRanks) {
+      Raw8<SRC> raw[kAddRanks];
+      float xr[kAddRanks];
+#pragma unroll
+      for (int j = 0; j < kAddRanks; ++j) {
+        const int r = min(r0 + j, p.at.rank - 1);
+        get8<SRC, WIDE>(raw[j], static_cast<const char*>(low) + r * p.low.ld * bytes_of(SRC), c, p.n);
+        xr[j] = x[r];
+      }
+#pragma unroll
+      for (int j = 0; j < kAddRanks; ++j) {
+        if (r0 + j >= rank) break;
+        float b[8];
+        floats8<SRC, WIDE>(raw[j], c, p.n, b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) add[i] = fmaf(xr[j], b[i], add[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += s * add[i];
+  }
+  if (c >= p.n) return;
+  if (p.c_type == COSTA_REAL_F32) put_scaled<SRC_F32>(p, row, c, v);
+  else if (p.c_type == COSTA_REAL_BF16) put_scaled<SRC_BF16>(p, row, c, v);
+  else put_scaled<SRC_F16>(p, row, c, v);
 }
 
 // ---- many rows, on the matrix units ---------------------------------------------
 // A workgroup has BM rows and RN ranks of a part of the sum, which goes by 64: both operands' steps
 // go through shared memory (read straight to registers in the instruction's order, sixteen
-// neighbouring lanes touch sixteen lines: 4096 rows by 64 ranks over 8192 took 73 us so), two of them
+// neighbouring lanes touch sixteen lines: 4096 rows by 64 ranks over 8192 took 73 us so), four of them
 // on their way while one is worked on.  Eight waves of sixteen rows by 16 NT ranks.
+constexpr int kDotAhead = 4;
 template <int SRC, int BM, int RN>
-__global__ __launch_bounds__(kLanes) void adapter_dots_tile(AdapterDotsArgs p, int64_t row0, int64_t per) {
+__global__ __launch_bounds__(kLanes, parts_of(SRC) == 1 ? 4 : 2) void adapter_dots_tile(AdapterDotsArgs p, int64_t row0, int64_t per) {
   constexpr int P = parts_of(SRC), STRIPS = BM / 16, NT = RN / 16 / (kWaves / STRIPS), HALVES = BM / 64;
   __shared__ v4u xs[2][P * BM * 8];
   __shared__ v4u as[2][P * RN * 8];
@@ -181,8 +189,8 @@ __global__ __launch_bounds__(kLanes) void adapter_dots_tile(AdapterDotsArgs p, i
     v4f acc[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) acc[t] = v4f{0, 0, 0, 0};
-    LeftStage<SRC, false, BM, false> xl[2];
-    Raw8<SRC> al[2];
+    LeftStage<SRC, false, BM, false> xl[kDotAhead];
+    Raw8<SRC> al[kDotAhead];
     const int c = threadIdx.x % 8, ar = threadIdx.x / 8;
     auto load = [&](int set, int64_t t) {
       if (t >= last) return;
@@ -199,33 +207,33 @@ __global__ __launch_bounds__(kLanes) void adapter_dots_tile(AdapterDotsArgs p, i
         for (int q = 0; q < P; ++q) as[s][q * RN * 8 + chunk_at(ar, c)] = out[q];
       }
     };
-    load(0, first);
-    load(1, first + 1);
+#pragma unroll
+    for (int s = 0; s < kDotAhead; ++s) load(s, first + s);
     __syncthreads();  // (the adapter's before: its last step is read)
     store(0, first, 0);
-    load(0, first + 2);
+    load(0, first + kDotAhead);
     __syncthreads();
-    for (int64_t t0 = first; t0 < last; t0 += 2) {
+    for (int64_t t0 = first; t0 < last; t0 += kDotAhead) {
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
+      for (int s = 0; s < kDotAhead; ++s) {
         const int64_t t = t0 + s;
         if (t >= last) break;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           v4u xp[P];
 #pragma unroll
-          for (int q = 0; q < P; ++q) xp[q] = xs[s][q * BM * 8 + chunk_at(strip + l, 2 * g + h)];
+          for (int q = 0; q < P; ++q) xp[q] = xs[s % 2][q * BM * 8 + chunk_at(strip + l, 2 * g + h)];
 #pragma unroll
           for (int u = 0; u < NT; ++u) {
             v4u ap[P];
 #pragma unroll
-            for (int q = 0; q < P; ++q) ap[q] = as[s][q * RN * 8 + chunk_at(rn + 16 * u + l, 2 * g + h)];
+            for (int q = 0; q < P; ++q) ap[q] = as[s % 2][q * RN * 8 + chunk_at(rn + 16 * u + l, 2 * g + h)];
             acc[u] = mfma_parts<P, P>(ap, xp, acc[u]);
           }
         }
         if (t + 1 < last) {
-          store(1 - s, t + 1, 1 - s);
-          load(1 - s, t + 3);
+          store((s + 1) % kDotAhead, t + 1, (s + 1) % 2);
+          load((s + 1) % kDotAhead, t + 1 + kDotAhead);
         }
         __syncthreads();
       }
@@ -520,12 +528,12 @@ GradPlan plan_grad(int64_t len, int32_t count, int32_t rank) {
 
 }  // namespace
 
-// (so that the workgroups are three for each CU, with 512 elements of the sum at least)
+// (so that the workgroups are two for each CU, with 512 elements of the sum at least)
 int64_t mx_adapter_dots_parts(int64_t m, int64_t k, int rank) {
   int bm, rn;
   dots_tile(rank, bm, rn);
   const int64_t tiles = up_div(m, bm) * up_div(std::max(rank, 1), rn);
-  return std::max<int64_t>(std::min(3 * kCUs / std::max<int64_t>(tiles, 1), k / 512), 1);
+  return std::max<int64_t>(std::min(2 * kCUs / std::max<int64_t>(tiles, 1), k / 512), 1);
 }
 
 hipError_t launch_mx_adapter_dots(const AdapterDotsArgs& a, int64_t& left, hipStream_t stream) {

@@ -44,13 +44,13 @@ __device__ inline float rsqrt_of(double v) {
 
 // y in few bits: a block's scale from four neighbouring lanes.  Lanes past the matrix have
 // zeros, up to the end of the padded row.
-template <int BITS>
-__device__ inline void quantize8(const MxView& q, int64_t row, int64_t unit, const float y[8]) {
+template <int BITS, typename I>
+__device__ inline void quantize8(const MxView& q, int64_t row, I unit, const float y[8]) {
   uint32_t m = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) m = max(m, magnitude(y[i]));
   const uint32_t s = mx_scale<BITS>(quad_max(m));
-  if (unit >= q.row_scales * 4) return;
+  if (unit >= (I)(q.row_scales * 4)) return;
   const v2u d = mx_encode8<BITS>(y, s);
   if (BITS == 4) *reinterpret_cast<uint32_t*>(q.data + row * q.row_bytes + unit * 4) = d.x;
   else *reinterpret_cast<v2u*>(q.data + row * q.row_bytes + unit * 8) = d;
@@ -58,21 +58,21 @@ __device__ inline void quantize8(const MxView& q, int64_t row, int64_t unit, con
 }
 
 // h of a unit; x and r as loaded.
-template <int SRC, bool WIDE>
-__device__ inline void unit_h(const NormArgs& a, Raw8<SRC>& x, Raw8<SRC>& r, int64_t c, float h[8]) {
-  floats8<SRC, WIDE>(x, c, a.cols, h);
+template <int SRC, bool WIDE, typename I>
+__device__ inline void unit_h(const NormArgs& a, Raw8<SRC>& x, Raw8<SRC>& r, I c, I cols, float h[8]) {
+  floats8<SRC, WIDE>(x, c, cols, h);
   if (a.r.data) {
     float v[8];
-    floats8<SRC, WIDE>(r, c, a.cols, v);
+    floats8<SRC, WIDE>(r, c, cols, v);
 #pragma unroll
     for (int i = 0; i < 8; ++i) h[i] += v[i];
   }
 }
-template <int SRC, int WSRC, bool WIDE>
-__device__ inline void unit_y(const NormArgs& a, int64_t row, int64_t unit, const float h[8], const Raw8<WSRC>& w,
+template <int SRC, int WSRC, bool WIDE, typename I>
+__device__ inline void unit_y(const NormArgs& a, int64_t row, I unit, I cols, const float h[8], const Raw8<WSRC>& w,
                               float s) {
-  const int64_t c = unit * 8;
-  if (a.h.data && c < a.cols) put8<SRC>(line_to<SRC>(a.h, row), c, a.cols, h);
+  const I c = unit * 8;
+  if (a.h.data && c < cols) put8<SRC>(line_to<SRC>(a.h, row), c, cols, h);
   if (!a.y.data && !a.q.data) return;
   float y[8];
 #pragma unroll
@@ -83,10 +83,10 @@ __device__ inline void unit_y(const NormArgs& a, int64_t row, int64_t unit, cons
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] *= v[i];
   }
-  if (c + 8 > a.cols)  // (what pads a row is +0, whatever s)
+  if (c + 8 > cols)  // (what pads a row is +0, whatever s)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = c + i < a.cols ? y[i] : 0.0f;
-  if (a.y.data && c < a.cols) put8<SRC>(line_to<SRC>(a.y, row), c, a.cols, y);
+    for (int i = 0; i < 8; ++i) y[i] = c + i < cols ? y[i] : 0.0f;
+  if (a.y.data && c < cols) put8<SRC>(line_to<SRC>(a.y, row), c, cols, y);
   if (a.q.data) {
     if (a.q.bits == 4) quantize8<4>(a.q, row, unit, y);
     else quantize8<8>(a.q, row, unit, y);
@@ -97,16 +97,17 @@ __device__ inline void unit_y(const NormArgs& a, int64_t row, int64_t unit, cons
 template <int SRC, int WSRC, int LANES, int PER, bool WIDE>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_rows(NormArgs a) {
   constexpr int ROWS = LANES < 256 ? 256 / LANES : 1, KEPT = PER ? PER : 1;
+  typedef typename std::conditional<(PER > 0), int32_t, int64_t>::type I;  // (of columns)
   __shared__ double sums[LANES / 64];
-  const int lane = threadIdx.x % LANES;
-  const int64_t units = a.q.data ? a.q.row_scales * 4 : (a.cols + 7) / 8;
+  const I lane = threadIdx.x % LANES, cols = (I)a.cols;
+  const I units = (I)(a.q.data ? a.q.row_scales * 4 : (a.cols + 7) / 8);
   Raw8<WSRC> w[KEPT];
   if constexpr (PER > 0)
     if (a.w)
 #pragma unroll
       for (int p = 0; p < PER; ++p) {
-        get8<WSRC, WIDE>(w[p], a.w, (int64_t)(lane + p * LANES) * 8, a.cols);
-        placed8<WSRC, WIDE>(w[p], (int64_t)(lane + p * LANES) * 8, a.cols);
+        get8<WSRC, WIDE>(w[p], a.w, (lane + p * LANES) * 8, cols);
+        placed8<WSRC, WIDE>(w[p], (lane + p * LANES) * 8, cols);
       }
   for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < a.rows; row0 += (int64_t)gridDim.x * ROWS) {
     const int64_t mine = row0 + threadIdx.x / LANES, row = min(mine, a.rows - 1);
@@ -117,13 +118,13 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_rows(NormArgs 
       Raw8<SRC> x[PER], r[PER];
       float h[PER][8];
 #pragma unroll
-      for (int p = 0; p < PER; ++p) get8<SRC, WIDE>(x[p], xl, (int64_t)(lane + p * LANES) * 8, a.cols);
+      for (int p = 0; p < PER; ++p) get8<SRC, WIDE>(x[p], xl, (lane + p * LANES) * 8, cols);
       if (rl)
 #pragma unroll
-        for (int p = 0; p < PER; ++p) get8<SRC, WIDE>(r[p], rl, (int64_t)(lane + p * LANES) * 8, a.cols);
+        for (int p = 0; p < PER; ++p) get8<SRC, WIDE>(r[p], rl, (lane + p * LANES) * 8, cols);
 #pragma unroll
       for (int p = 0; p < PER; ++p) {
-        unit_h<SRC, WIDE>(a, x[p], r[p], (int64_t)(lane + p * LANES) * 8, h[p]);
+        unit_h<SRC, WIDE>(a, x[p], r[p], (lane + p * LANES) * 8, cols, h[p]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum = fma((double)h[p][i], (double)h[p][i], sum);
       }
@@ -131,53 +132,59 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_rows(NormArgs 
       if (mine < a.rows) {
         if (a.rstd && lane == 0) a.rstd[row] = s;
 #pragma unroll
-        for (int p = 0; p < PER; ++p) unit_y<SRC, WSRC, WIDE>(a, row, lane + p * LANES, h[p], w[p], s);
+        for (int p = 0; p < PER; ++p) unit_y<SRC, WSRC, WIDE>(a, row, lane + p * LANES, cols, h[p], w[p], s);
       }
     } else {
       Raw8<SRC> x, r;
       float h[8];
-      for (int64_t u = lane; u < units; u += LANES) {
-        get8<SRC, WIDE>(x, xl, u * 8, a.cols);
-        if (rl) get8<SRC, WIDE>(r, rl, u * 8, a.cols);
-        unit_h<SRC, WIDE>(a, x, r, u * 8, h);
+      for (I u = lane; u < units; u += LANES) {
+        get8<SRC, WIDE>(x, xl, u * 8, cols);
+        if (rl) get8<SRC, WIDE>(r, rl, u * 8, cols);
+        unit_h<SRC, WIDE>(a, x, r, u * 8, cols, h);
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum = fma((double)h[i], (double)h[i], sum);
       }
       const float s = rsqrt_of(row_sum<LANES>(sum, sums) * a.inverse + (double)a.eps);
       if (a.rstd && lane == 0) a.rstd[row] = s;
       // (whole rounds of lanes: a block's four lanes stay together)
-      for (int64_t u = lane; u < (units + LANES - 1) / LANES * LANES; u += LANES) {
-        get8<SRC, WIDE>(x, xl, u * 8, a.cols);
-        if (rl) get8<SRC, WIDE>(r, rl, u * 8, a.cols);
+      for (I u = lane; u < (units + LANES - 1) / LANES * LANES; u += LANES) {
+        get8<SRC, WIDE>(x, xl, u * 8, cols);
+        if (rl) get8<SRC, WIDE>(r, rl, u * 8, cols);
         if (a.w) {
-          get8<WSRC, WIDE>(w[0], a.w, u * 8, a.cols);
-          placed8<WSRC, WIDE>(w[0], u * 8, a.cols);
+          get8<WSRC, WIDE>(w[0], a.w, u * 8, cols);
+          placed8<WSRC, WIDE>(w[0], u * 8, cols);
         }
-        unit_h<SRC, WIDE>(a, x, r, u * 8, h);
-        unit_y<SRC, WSRC, WIDE>(a, row, u, h, w[0], s);
+        unit_h<SRC, WIDE>(a, x, r, u * 8, cols, h);
+        unit_y<SRC, WSRC, WIDE>(a, row, u, cols, h, w[0], s);
       }
     }
   }
 }
 
 // ---- gradients ---------------------------------------------------------------
+// The sum of eight products, in 32 bits: three roundings of each, its own among them four.
+__device__ inline float sum8(const float a[8], const float b[8]) {
+  return ((a[0] * b[0] + a[1] * b[1]) + (a[2] * b[2] + a[3] * b[3])) +
+         ((a[4] * b[4] + a[5] * b[5]) + (a[6] * b[6] + a[7] * b[7]));
+}
+
 // A workgroup's rows share its lanes' part of dw, in registers; the parts are added by
 // another kernel.
 template <int SRC, int WSRC, int LANES, int PER, bool WIDE>
-__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_grad_rows(NormBackArgs a) {
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES, SRC == SRC_F32 ? 2 : 4) void norm_grad_rows(NormBackArgs a) {
   constexpr int ROWS = LANES < 256 ? 256 / LANES : 1, KEPT = PER ? PER : 1;
+  typedef typename std::conditional<(PER > 0), int32_t, int64_t>::type I;  // (of columns)
   __shared__ double sums[LANES / 64];
-  const int lane = threadIdx.x % LANES;
-  const int64_t units = (a.cols + 7) / 8;
-  float* const part = a.parts + ((int64_t)blockIdx.x * ROWS + threadIdx.x / LANES) * a.cols;
+  const I lane = threadIdx.x % LANES, cols = (I)a.cols, units = (I)((a.cols + 7) / 8);
+  float* const part = a.parts + (int64_t)blockIdx.x * a.cols;
   Raw8<WSRC> w[KEPT];
   float dw[KEPT][8];
   if constexpr (PER > 0) {
     if (a.w)
 #pragma unroll
       for (int p = 0; p < PER; ++p) {
-        get8<WSRC, WIDE>(w[p], a.w, (int64_t)(lane + p * LANES) * 8, a.cols);
-        placed8<WSRC, WIDE>(w[p], (int64_t)(lane + p * LANES) * 8, a.cols);
+        get8<WSRC, WIDE>(w[p], a.w, (lane + p * LANES) * 8, cols);
+        placed8<WSRC, WIDE>(w[p], (lane + p * LANES) * 8, cols);
       }
 #pragma unroll
     for (int p = 0; p < PER; ++p)
@@ -186,8 +193,8 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_grad_rows(Norm
   }
   bool first = true;
   // g of a unit, its dy beside it
-  auto unit_g = [&](Raw8<SRC>& raw, const Raw8<WSRC>& wr, int64_t c, float dy[8], float g[8]) {
-    floats8<SRC, WIDE>(raw, c, a.cols, dy);
+  auto unit_g = [&](const Raw8<SRC>& raw, const Raw8<WSRC>& wr, float dy[8], float g[8]) {  // (both in place)
+    raw_floats<SRC>(raw, dy);
     if (a.w) {
       raw_floats<WSRC>(wr, g);
 #pragma unroll
@@ -197,19 +204,18 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_grad_rows(Norm
       for (int i = 0; i < 8; ++i) g[i] = dy[i];
     }
   };
-  auto unit_dx = [&](int64_t row, int64_t c, const float g[8], const float u[8], float s, float mean, const Raw8<SRC>* dh) {
-    if (c >= a.cols) return;
+  auto unit_dx = [&](int64_t row, I c, const float g[8], const float u[8], float s, float mean, Raw8<SRC> d) {
+    if (c >= cols) return;
     float dx[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) dx[i] = s * (g[i] - u[i] * mean);
-    if (dh) {
-      Raw8<SRC> d = *dh;
+    if (a.dh.data) {
       float v[8];
-      floats8<SRC, WIDE>(d, c, a.cols, v);
+      floats8<SRC, WIDE>(d, c, cols, v);
 #pragma unroll
       for (int i = 0; i < 8; ++i) dx[i] += v[i];
     }
-    put8<SRC>(line_to<SRC>(a.dx, row), c, a.cols, dx);
+    put8<SRC>(line_to<SRC>(a.dx, row), c, cols, dx);
   };
   for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < a.rows; row0 += (int64_t)gridDim.x * ROWS) {
     const int64_t mine = row0 + threadIdx.x / LANES, row = min(mine, a.rows - 1);
@@ -222,76 +228,104 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_grad_rows(Norm
       Raw8<SRC> dyr[PER], hr[PER], dhr[PER];
 #pragma unroll
       for (int p = 0; p < PER; ++p) {
-        get8<SRC, WIDE>(dyr[p], dyl, (int64_t)(lane + p * LANES) * 8, a.cols);
-        get8<SRC, WIDE>(hr[p], hl, (int64_t)(lane + p * LANES) * 8, a.cols);
+        get8<SRC, WIDE>(dyr[p], dyl, (lane + p * LANES) * 8, cols);
+        get8<SRC, WIDE>(hr[p], hl, (lane + p * LANES) * 8, cols);
       }
       if (dhl)
 #pragma unroll
-        for (int p = 0; p < PER; ++p) get8<SRC, WIDE>(dhr[p], dhl, (int64_t)(lane + p * LANES) * 8, a.cols);
-      float g[PER][8], u[PER][8];
+        for (int p = 0; p < PER; ++p) get8<SRC, WIDE>(dhr[p], dhl, (lane + p * LANES) * 8, cols);
+      // (g and u are made again after the sum: a row in 16 bits takes half the registers of theirs)
+      float dy[8], g[8], u[8];
 #pragma unroll
       for (int p = 0; p < PER; ++p) {
-        const int64_t c = (int64_t)(lane + p * LANES) * 8;
-        float dy[8];
-        unit_g(dyr[p], w[p], c, dy, g[p]);
-        floats8<SRC, WIDE>(hr[p], c, a.cols, u[p]);
+        const I c = (lane + p * LANES) * 8;
+        placed8<SRC, WIDE>(dyr[p], c, cols);
+        placed8<SRC, WIDE>(hr[p], c, cols);
+        unit_g(dyr[p], w[p], dy, g);
+        raw_floats<SRC>(hr[p], u);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          u[p][i] *= s;
-          sum = fma((double)g[p][i], (double)u[p][i], sum);
-          if (mine < a.rows) dw[p][i] += dy[i] * u[p][i];
+          u[i] *= s;
+          if (mine < a.rows) dw[p][i] += dy[i] * u[i];
         }
+        sum += (double)sum8(g, u);
       }
       const float mean = (float)(row_sum<LANES>(sum, sums) * a.inverse);
       if (mine < a.rows)
 #pragma unroll
-        for (int p = 0; p < PER; ++p)
-          unit_dx(row, (int64_t)(lane + p * LANES) * 8, g[p], u[p], s, mean, dhl ? &dhr[p] : nullptr);
+        for (int p = 0; p < PER; ++p) {
+          unit_g(dyr[p], w[p], dy, g);
+          raw_floats<SRC>(hr[p], u);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) u[i] *= s;
+          unit_dx(row, (lane + p * LANES) * 8, g, u, s, mean, dhr[p]);
+        }
     } else {
       Raw8<SRC> dyr, hr, dhr;
       float dy[8], g[8], u[8];
-      for (int64_t un = lane; un < units; un += LANES) {
-        get8<SRC, WIDE>(dyr, dyl, un * 8, a.cols);
-        get8<SRC, WIDE>(hr, hl, un * 8, a.cols);
+      for (I un = lane; un < units; un += LANES) {
+        get8<SRC, WIDE>(dyr, dyl, un * 8, cols);
+        get8<SRC, WIDE>(hr, hl, un * 8, cols);
         if (a.w) {
-          get8<WSRC, WIDE>(w[0], a.w, un * 8, a.cols);
-          placed8<WSRC, WIDE>(w[0], un * 8, a.cols);
+          get8<WSRC, WIDE>(w[0], a.w, un * 8, cols);
+          placed8<WSRC, WIDE>(w[0], un * 8, cols);
         }
-        unit_g(dyr, w[0], un * 8, dy, g);
-        floats8<SRC, WIDE>(hr, un * 8, a.cols, u);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum = fma((double)g[i], (double)(u[i] * s), sum);
-      }
-      const float mean = (float)(row_sum<LANES>(sum, sums) * a.inverse);
-      for (int64_t un = lane; un < units; un += LANES) {
-        const int64_t c = un * 8;
-        get8<SRC, WIDE>(dyr, dyl, c, a.cols);
-        get8<SRC, WIDE>(hr, hl, c, a.cols);
-        if (a.w) {
-          get8<WSRC, WIDE>(w[0], a.w, c, a.cols);
-          placed8<WSRC, WIDE>(w[0], c, a.cols);
-        }
-        if (dhl) get8<SRC, WIDE>(dhr, dhl, c, a.cols);
-        unit_g(dyr, w[0], c, dy, g);
-        floats8<SRC, WIDE>(hr, c, a.cols, u);
+        placed8<SRC, WIDE>(dyr, un * 8, cols);
+        unit_g(dyr, w[0], dy, g);
+        floats8<SRC, WIDE>(hr, un * 8, cols, u);
 #pragma unroll
         for (int i = 0; i < 8; ++i) u[i] *= s;
-        unit_dx(row, c, g, u, s, mean, dhl ? &dhr : nullptr);
+        sum += (double)sum8(g, u);
+      }
+      const float mean = (float)(row_sum<LANES>(sum, sums) * a.inverse);
+      for (I un = lane; un < units; un += LANES) {
+        const I c = un * 8;
+        get8<SRC, WIDE>(dyr, dyl, c, cols);
+        get8<SRC, WIDE>(hr, hl, c, cols);
+        if (a.w) {
+          get8<WSRC, WIDE>(w[0], a.w, c, cols);
+          placed8<WSRC, WIDE>(w[0], c, cols);
+        }
+        if (dhl) get8<SRC, WIDE>(dhr, dhl, c, cols);
+        placed8<SRC, WIDE>(dyr, c, cols);
+        unit_g(dyr, w[0], dy, g);
+        floats8<SRC, WIDE>(hr, c, cols, u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] *= s;
+        unit_dx(row, c, g, u, s, mean, dhr);
         if (a.dw)
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            if (c + i < a.cols) part[c + i] = (first ? 0.0f : part[c + i]) + dy[i] * u[i];
+            if (c + i < cols) part[c + i] = (first ? 0.0f : part[c + i]) + dy[i] * u[i];
       }
       first = false;
     }
   }
-  if constexpr (PER > 0)
-    if (a.dw)
+  if constexpr (PER > 0) {
+    if (!a.dw) return;
+    if constexpr (ROWS > 1) {  // the waves' parts, in a fixed order
+      __shared__ float red[ROWS - 1][PER][8][64];
+      const int wave = threadIdx.x / 64;
+      if (wave > 0)
 #pragma unroll
-      for (int p = 0; p < PER; ++p) {
-        const int64_t c = (int64_t)(lane + p * LANES) * 8;
-        if (c < a.cols) put8<SRC_F32>(part, c, a.cols, dw[p]);
-      }
+        for (int p = 0; p < PER; ++p)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) red[wave - 1][p][i][lane] = dw[p][i];
+      __syncthreads();
+      if (wave > 0) return;
+#pragma unroll
+      for (int w = 0; w < ROWS - 1; ++w)
+#pragma unroll
+        for (int p = 0; p < PER; ++p)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) dw[p][i] += red[w][p][i][lane];
+    }
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      const I c = (lane + p * LANES) * 8;
+      if (c < cols) put8<SRC_F32>(part, c, cols, dw[p]);
+    }
+  }
 }
 
 // dw from its parts, in a fixed order and in 64 bits: a workgroup has 32 columns, 32 lanes
@@ -323,25 +357,32 @@ struct RowPlan {
 RowPlan plan_row(int64_t units) {
   for (int per : {1, 2, 4})
     if (units <= 64 * per) return {64, per};
-  for (int per : {2, 4, 8})
+  for (int per : {2, 4})
     if (units <= 256 * per) return {256, per};
-  if (units <= 1024 * 4) return {1024, 4};
+  if (units <= 512 * 4) return {512, 4};
   return {1024, 0};
+}
+// Of the gradients, which hold more of a row: two units a lane at most, so that four waves of
+// a SIMD fit (16-bit types).
+RowPlan plan_grad_row(int64_t units, costa_real type) {
+  for (int lanes : {64, 256, 512})
+    for (int per : {1, 2})
+      if (units <= lanes * per) return {lanes, per};
+  return {1024, type != COSTA_REAL_F32 && units <= 2048 ? 2 : 0};
 }
 
 constexpr int64_t kNormGroups = 1 << 16;  // workgroups of a launch; they loop over more rows
 
 template <template <int, int, int, int, bool> class Launch, int SRC, int WSRC, typename A>
 hipError_t launch_rows(const A& a, RowPlan r, int64_t groups, hipStream_t stream) {
+  const int at = r.lanes * 8 + r.per;
   if (a.cols < 8) Launch<SRC, WSRC, 64, 1, false>::go(a, groups, stream);
-  else if (r.lanes == 64 && r.per == 1) Launch<SRC, WSRC, 64, 1, true>::go(a, groups, stream);
-  else if (r.lanes == 64 && r.per == 2) Launch<SRC, WSRC, 64, 2, true>::go(a, groups, stream);
-  else if (r.lanes == 64) Launch<SRC, WSRC, 64, 4, true>::go(a, groups, stream);
-  else if (r.lanes == 256 && r.per == 2) Launch<SRC, WSRC, 256, 2, true>::go(a, groups, stream);
-  else if (r.lanes == 256 && r.per == 4) Launch<SRC, WSRC, 256, 4, true>::go(a, groups, stream);
-  else if (r.lanes == 256) Launch<SRC, WSRC, 256, 8, true>::go(a, groups, stream);
-  else if (r.per == 4) Launch<SRC, WSRC, 1024, 4, true>::go(a, groups, stream);
-  else Launch<SRC, WSRC, 1024, 0, true>::go(a, groups, stream);
+  else if (at == 64 * 8 + 1) Launch<SRC, WSRC, 64, 1, true>::go(a, groups, stream);
+  else if (at == 64 * 8 + 2) Launch<SRC, WSRC, 64, 2, true>::go(a, groups, stream);
+  else if (at == 256 * 8 + 1) Launch<SRC, WSRC, 256, 1, true>::go(a, groups, stream);
+  else if (at == 256 * 8 + 2) Launch<SRC, WSRC, 256, 2, true>::go(a, groups, stream);
+  else if (at == 1024 * 8) Launch<SRC, WSRC, 1024, 0, true>::go(a, groups, stream);
+  else if (!Launch<SRC, WSRC, 0, 0, true>::more(a, at, groups, stream)) return hipErrorInvalidValue;
   return hipGetLastError();
 }
 template <template <int, int, int, int, bool> class Launch, typename A>
@@ -362,11 +403,26 @@ struct Forward {
   static void go(const NormArgs& a, int64_t groups, hipStream_t stream) {
     norm_rows<SRC, WSRC, LANES, PER, WIDE><<<dim3((unsigned)groups), LANES < 256 ? 256 : LANES, 0, stream>>>(a);
   }
+  static bool more(const NormArgs& a, int at, int64_t groups, hipStream_t stream) {
+    if (at == 64 * 8 + 4) Forward<SRC, WSRC, 64, 4, true>::go(a, groups, stream);
+    else if (at == 256 * 8 + 4) Forward<SRC, WSRC, 256, 4, true>::go(a, groups, stream);
+    else if (at == 512 * 8 + 4) Forward<SRC, WSRC, 512, 4, true>::go(a, groups, stream);
+    else return false;
+    return true;
+  }
 };
 template <int SRC, int WSRC, int LANES, int PER, bool WIDE>
 struct Backward {
   static void go(const NormBackArgs& a, int64_t groups, hipStream_t stream) {
     norm_grad_rows<SRC, WSRC, LANES, PER, WIDE><<<dim3((unsigned)groups), LANES < 256 ? 256 : LANES, 0, stream>>>(a);
+  }
+  static bool more(const NormBackArgs& a, int at, int64_t groups, hipStream_t stream) {
+    if (at == 512 * 8 + 1) Backward<SRC, WSRC, 512, 1, true>::go(a, groups, stream);
+    else if (at == 512 * 8 + 2) Backward<SRC, WSRC, 512, 2, true>::go(a, groups, stream);
+    else if (SRC != SRC_F32 && at == 1024 * 8 + 2)
+      Backward<SRC, WSRC, 1024, SRC == SRC_F32 ? 0 : 2, true>::go(a, groups, stream);
+    else return false;
+    return true;
   }
 };
 
@@ -379,28 +435,27 @@ hipError_t launch_mx_norm(const NormArgs& a, hipStream_t stream) {
   return launch_types<Forward>(a, r, std::min(groups_of(r, a.rows), kNormGroups), stream);
 }
 
-// (4 workgroups for each CU, 16 rows of each at least)
+// A part for each workgroup: as many as 1024 lanes for each CU are (8192x8192 in bfloat16: 512 of them 109 us,
+// 1024 of them 115; 4096x2500: 1024 of them 25 us, 256 of them 36).
 Parts mx_norm_parts(int64_t rows, int64_t cols) {
-  const RowPlan r = plan_row(up_div(cols, 8));
-  const int64_t per = r.lanes < 256 ? 256 / r.lanes : 1;
-  return {per, std::max<int64_t>(std::min<int64_t>(up_div(groups_of(r, rows), 16), 4 * kCUs), 1) * per};
+  const RowPlan r = plan_grad_row(up_div(cols, 8), COSTA_REAL_BF16);
+  return {1, std::max<int64_t>(std::min<int64_t>(groups_of(r, rows), kCUs * 1024 / std::max(r.lanes, 256)), 1)};
 }
 
 hipError_t launch_mx_norm_backward(const NormBackArgs& a, hipStream_t stream) {
-  const RowPlan r = plan_row(up_div(a.cols, 8));
-  const int64_t per = r.lanes < 256 ? 256 / r.lanes : 1;
+  const RowPlan r = plan_grad_row(up_div(a.cols, 8), a.type);
   int64_t groups = 0;  // (no rows: dw is a sum over nothing)
   if (a.rows > 0) {
-    groups = a.dw ? std::min(mx_norm_parts(a.rows, a.cols).most, a.most) / per
+    groups = a.dw ? std::min({mx_norm_parts(a.rows, a.cols).most, a.most, groups_of(r, a.rows)})
                   : std::min(groups_of(r, a.rows), kNormGroups);
     const hipError_t e = launch_types<Backward>(a, r, groups, stream);
     if (e != hipSuccess) return e;
   }
   if (!a.dw) return hipSuccess;
   const dim3 grid((unsigned)std::min<int64_t>(up_div(a.cols, 32), kNormGroups));
-  if (a.dw_type == COSTA_REAL_F32) norm_dw<SRC_F32><<<grid, 1024, 0, stream>>>(a.parts, groups * per, a.cols, a.dw);
-  else if (a.dw_type == COSTA_REAL_BF16) norm_dw<SRC_BF16><<<grid, 1024, 0, stream>>>(a.parts, groups * per, a.cols, a.dw);
-  else norm_dw<SRC_F16><<<grid, 1024, 0, stream>>>(a.parts, groups * per, a.cols, a.dw);
+  if (a.dw_type == COSTA_REAL_F32) norm_dw<SRC_F32><<<grid, 1024, 0, stream>>>(a.parts, groups, a.cols, a.dw);
+  else if (a.dw_type == COSTA_REAL_BF16) norm_dw<SRC_BF16><<<grid, 1024, 0, stream>>>(a.parts, groups, a.cols, a.dw);
+  else norm_dw<SRC_F16><<<grid, 1024, 0, stream>>>(a.parts, groups, a.cols, a.dw);
   return hipGetLastError();
 }
 

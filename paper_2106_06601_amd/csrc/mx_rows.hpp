@@ -22,11 +22,12 @@ __device__ inline void raw_floats(const Raw8<SRC>& r, float x[8]) {
 }
 
 // The eight elements of a line (of `len`) from c on; zeros past its end.  WIDE: the line
-// has 8 or more, and the load is one, which waits for no branch.
-template <int SRC, bool WIDE>
-__device__ inline void get8(Raw8<SRC>& r, const void* line, int64_t c, int64_t len) {
+// has 8 or more, and the load is one, which waits for no branch (placed8() moves what it read
+// into place).  I: 32 bits where a line's elements are counted in them.
+template <int SRC, bool WIDE, typename I>
+__device__ inline void get8(Raw8<SRC>& r, const void* line, I c, I len) {
   if constexpr (WIDE) {
-    load8<SRC>(r, static_cast<const char*>(line), c, len);
+    __builtin_memcpy(r.w, static_cast<const char*>(line) + (int64_t)min(c, (I)(len - 8)) * bytes_of(SRC), sizeof r.w);
   } else {
 #pragma unroll
     for (int i = 0; i < (int)(sizeof r.w / 4); ++i) r.w[i] = 0;
@@ -38,17 +39,17 @@ __device__ inline void get8(Raw8<SRC>& r, const void* line, int64_t c, int64_t l
   }
 }
 // Moves what get8() read at the end of a line into place: once.
-template <int SRC, bool WIDE>
-__device__ inline void placed8(Raw8<SRC>& r, int64_t c, int64_t len) {
+template <int SRC, bool WIDE, typename I>
+__device__ inline void placed8(Raw8<SRC>& r, I c, I len) {
   if (WIDE && c + 8 > len) place8<SRC>(r, c, len);
 }
-template <int SRC, bool WIDE>
-__device__ inline void floats8(Raw8<SRC>& r, int64_t c, int64_t len, float x[8]) {
+template <int SRC, bool WIDE, typename I>
+__device__ inline void floats8(Raw8<SRC>& r, I c, I len, float x[8]) {
   placed8<SRC, WIDE>(r, c, len);
   raw_floats<SRC>(r, x);
 }
-template <int SRC>
-__device__ inline void put8(void* line, int64_t c, int64_t len, const float x[8]) {
+template <int SRC, typename I>
+__device__ inline void put8(void* line, I c, I len, const float x[8]) {
   Elem<SRC> v[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = (Elem<SRC>)x[i];

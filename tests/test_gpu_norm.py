@@ -7,7 +7,8 @@ products': 8 * 2^-24 of |y|, and the type's half step.  mx(y): what two rounding
 can do: the formula applied to y (1 +- 8 * 2^-24) gives the same code, or the neighbouring
 one; checked as: the stored value lies between the values that the two ends are stored as, where both
 have the same scale.  dx = s (g - u c) + dh: each of the terms' magnitudes with 12 * 2^-24, c
-with 8 * 2^-24 of mean |g u| (its sum is in 64 bits), and the half step.  dw: rows / parts
+with 8 * 2^-24 of mean |g u| (each product, with those of g and u, and three more roundings
+in a sum of eight; those sums in 64 bits), and the half step.  dw: rows / parts
 additions in 32 bits in a workgroup (at most 24 rows each, tested up to 700 rows) and 64-bit ones:
 (rows + 4) * 2^-24 of sum |dy u|, and the half step.
 """
