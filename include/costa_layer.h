@@ -103,7 +103,8 @@ costa_status costa_mx_adapter_gradient_workspace(int64_t m, int64_t len, int32_t
  *     L = alpha X W^^T,  lse_i = log sum_j exp(L_ij),  loss_i = lse_i - L_i,target(i)
  *
  * X m x k, W n x k (n: the vocabulary), target, loss, lse: m entries.  A row whose target
- * is not in 0 .. n-1 does not count: its loss is 0.  L is not kept. */
+ * is not in 0 .. n-1 does not count: its loss is 0.  A logit that is NaN or +infinity makes its
+ * row's lse NaN.  L is not kept. */
 costa_status costa_mx_loss(float alpha, const costa_matrix* X, const costa_mx* W, const int64_t* target, float* loss,
                            float* lse, void* workspace, size_t workspace_bytes, hipStream_t stream);
 

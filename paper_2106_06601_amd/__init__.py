@@ -684,9 +684,11 @@ def _line(t):
     """A vector as a matrix of one row."""
     if t is None:
         return None
-    if t.dim() != 1 or not t.is_contiguous():
-        raise ValueError("a contiguous 1-D tensor is needed")
-    return _matrix(t.view(1, -1))
+    real = _REAL_OF.get(t.dtype)
+    if real is None or t.dim() != 1 or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError("a contiguous 1-D float64, float32, bfloat16 or float16 tensor on the GPU is needed")
+    n = t.shape[0]
+    return CostaMatrix(real, 1, 1, n, n or 1, t.data_ptr() or None)
 
 
 def _vector(t, dtype, n, what: str):

@@ -145,9 +145,9 @@ __global__ __launch_bounds__(256) void adapter_add_row(AdapterAddArgs p, int64_t
 // ---- many rows, on the matrix units ---------------------------------------------
 // A workgroup has BM rows and RN ranks of a part of the sum, which goes by 64: both operands' steps
 // go through shared memory (read straight to registers in the instruction's order, sixteen
-// neighbouring lanes touch sixteen lines: 4096 rows by 64 ranks over 8192 took 73 us so), four of them
+// neighbouring lanes touch sixteen lines: 4096 rows by 64 ranks over 8192 took 73 us so), two of them
 // on their way while one is worked on.  Eight waves of sixteen rows by 16 NT ranks.
-constexpr int kDotAhead = 4;
+constexpr int kDotAhead = 2;
 template <int SRC, int BM, int RN>
 __global__ __launch_bounds__(kLanes, parts_of(SRC) == 1 ? 4 : 2) void adapter_dots_tile(AdapterDotsArgs p, int64_t row0, int64_t per) {
   constexpr int P = parts_of(SRC), STRIPS = BM / 16, NT = RN / 16 / (kWaves / STRIPS), HALVES = BM / 64;
@@ -194,13 +194,15 @@ __global__ __launch_bounds__(kLanes, parts_of(SRC) == 1 ? 4 : 2) void adapter_do
     const int c = threadIdx.x % 8, ar = threadIdx.x / 8;
     auto load = [&](int set, int64_t t) {
       if (t >= last) return;
-      xl[set].load(x, i0, t * kStepBf16);
-      if (ar < RN) load8<SRC>(al[set], low, t * kStepBf16 + 8 * c, p.k);
+      const int64_t k0 = t * kStepBf16;
+      xl[set].load(x, i0, k0);
+      if (ar < RN) load8<SRC>(al[set], low, k0 + 8 * c, p.k);
     };
     auto store = [&](int set, int64_t t, int s) {
       xl[set].store(x, i0, xs[s]);
       if (ar < RN) {
-        if ((t + 1) * kStepBf16 > p.k) place8<SRC>(al[set], t * kStepBf16 + 8 * c, p.k);
+        const int64_t k0 = t * kStepBf16;
+        if (k0 + kStepBf16 > p.k) place8<SRC>(al[set], k0 + 8 * c, p.k);
         v4u out[P];
         raw_parts<SRC>(al[set], out);
 #pragma unroll

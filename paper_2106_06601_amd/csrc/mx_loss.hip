@@ -150,7 +150,7 @@ dim3 groups_for(int64_t units) { return dim3((unsigned)std::min(up_div(units, 25
 }  // namespace
 
 hipError_t launch_mx_loss_stats(const LogitsPart& p, LossStat* stats, float* at, hipStream_t stream) {
-  constexpr int64_t kRows = 1 << 18, kChunks = 1 << 6;  // of a launch
+  constexpr int64_t kRows = 1 << 18, kChunks = 1 << 5;  // of a launch: below 2^32 lanes
   const int64_t chunks = up_div(p.n, kLossChunk);
   for (int64_t j = 0; j < chunks; j += kChunks)
     for (int64_t i = 0; i < p.m; i += kRows) {
