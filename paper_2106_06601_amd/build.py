@@ -27,7 +27,8 @@ COMMON = ["-O3", "-fPIC", "-std=c++17", "-ffp-contract=off",
           "-Wall", "-Wno-unused-function"]
 SOURCES = ["layout.cpp", "lap.cpp", "plan.cpp", "api.cpp", "scalapack.cpp", "kernels.hip",
            "mx.cpp", "mx_store.hip", "mx_product.hip", "mx_tiles.hip",
-           "mx_layer.cpp", "mx_norm.hip", "mx_adapters.hip", "mx_loss.hip", "mx_tiles_adapted.hip", "mx_tiles_loss.hip"]
+           "mx_layer.cpp", "mx_norm.hip", "mx_adapters.hip", "mx_loss.hip", "mx_tiles_adapted.hip", "mx_tiles_loss.hip",
+           "mx_tiles_few.hip"]
 
 
 def _run(cmd):

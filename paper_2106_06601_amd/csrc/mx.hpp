@@ -105,6 +105,7 @@ hipError_t launch_mx_product(const ProductArgs& a, hipStream_t stream);
 // The sums alone (k > 0), neither scaled nor joined: `splits` parts of m x n floats in the
 // workspace, which holds one at least.  Of a, alpha, beta and C are not looked at.
 hipError_t launch_mx_product_parts(const ProductArgs& a, int& splits, hipStream_t stream);
+size_t mx_product_parts_workspace(int64_t m, int64_t n, int64_t k);  // what it can use
 
 // ---- entry points (mx.cpp) -------------------------------------------------------
 // Frees the layout tables (called by costa_finalize); waits for the kernels that read them.

@@ -194,7 +194,7 @@ int64_t slice_rows(int64_t m, int64_t n) {
 // Bytes of the sums of `rows` rows, and of those with what a split sum can use.
 size_t sums_bytes(int64_t rows, int64_t n) { return (size_t)rows * n * 4; }
 size_t split_bytes(int64_t rows, int64_t n, int64_t k) {
-  return std::max(mx_product_workspace(rows, n, k), sums_bytes(rows, n));
+  return std::max(mx_product_parts_workspace(rows, n, k), sums_bytes(rows, n));
 }
 
 // The adapters' index and, where they are given, A and B.
@@ -442,14 +442,14 @@ extern "C" costa_status costa_mx_loss_workspace(int64_t m, int64_t n, int64_t k,
       const size_t sums = piece_bytes(m, n, 4);
       // (statistics of every 32 columns, where the logits stay in the tiles)
       give(most, at + std::max(up16((size_t)m * chunks_kept(n, kPieceColumns) * sizeof(LossStat)) +
-                                   std::max(sums, mx_product_workspace(m, std::min(n, piece_columns(m, n, sums, 4)), k)),
+                                   std::max(sums, mx_product_parts_workspace(m, std::min(n, piece_columns(m, n, sums, 4)), k)),
                                (size_t)m * ((n + 31) / 32) * sizeof(LossStat)));
     } else {
       const size_t dx = up16((size_t)m * k * 4) + 16;  // what dX is summed in, and G's scale
       give(least, dx + up16(least_piece(m, n, 4)) + up16(least_piece(m, n, 4)));
       const size_t g = piece_bytes(m, n, 4);
       const int64_t per = piece_columns(m, n, g, 4);
-      give(most, dx + up16(g) + std::max({up16(g), mx_product_workspace(m, per, k), mx_product_workspace(m, k, per),
+      give(most, dx + up16(g) + std::max({up16(g), mx_product_parts_workspace(m, per, k), mx_product_workspace(m, k, per),
                                           mx_product_workspace(per, k, m)}));
     }
     return COSTA_SUCCESS;

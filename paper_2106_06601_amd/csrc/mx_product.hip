@@ -360,9 +360,33 @@ hipError_t launch_sums(const ProductArgs& a, const Epilogue& e, bool parts, Prod
                                       : launch_tiles_scaled(p, plan, stream);
 }
 
+// Splits of a product whose sums go on in parts, in tiles of 64 rows; 0 where other kernels take it.
+// (61 rows by 8192x8192 in 4 bits, joined: bfloat16 32 us, with the kernel for few rows 41; float16 35 and 75;
+// float 45 and 91.  32 rows of bfloat16: 28 both.)
+int64_t some_rows_splits(int src, int64_t m, int64_t n, int64_t k) {
+  const int64_t tiles = up_div(n, 128);
+  if (m > 64 || m <= (src == SRC_BF16 ? 32 : 16) || k < 256 || tiles > 1 << 20) return 0;
+  // a workgroup for each CU, or two where that leaves sums whole
+  const int64_t fill = kCUs / tiles >= 2 ? kCUs / tiles : 2 * kCUs / tiles;
+  return std::max<int64_t>(std::min(fill, k / 256), 1);
+}
+
 }  // namespace
 
+size_t mx_product_parts_workspace(int64_t m, int64_t n, int64_t k) {
+  if (m == 0 || n == 0 || k == 0) return 0;
+  const int64_t some = some_rows_splits(SRC_F32, m, n, k);
+  return std::max(mx_product_workspace(m, n, k), (size_t)std::max<int64_t>(some, 1) * m * n * 4);
+}
+
 hipError_t launch_mx_product_parts(const ProductArgs& a, int& splits, hipStream_t stream) {
+  const int src = a.a_type == COSTA_REAL_BF16 ? SRC_BF16 : a.a_type == COSTA_REAL_F16 ? SRC_F16 : SRC_F32;
+  const int64_t some = a.amx.bits == 0 && a.a_cs == 1 ? some_rows_splits(src, a.m, a.n, a.k) : 0;
+  if (some > 0) {
+    splits = (int)std::max<int64_t>(std::min<int64_t>(some, a.workspace_bytes / ((size_t)a.m * a.n * 4)), 1);
+    const Epilogue e{a.workspace, a.n, 1, COSTA_REAL_F32, a.n % 4 == 0, 1.0f, 0.0f};
+    return launch_tiles_few(src, Args{a.m, a.n, a.k, a.amx, a.b, a.real, a.a_rs, a.a_cs, e, a.m * a.n}, splits, stream);
+  }
   ProductPlan plan{};
   const hipError_t err = launch_sums(a, Epilogue{}, true, plan, stream);
   splits = plan.splits;

@@ -167,6 +167,7 @@ __device__ inline v4f mfma_bf16(v4u a, v4u b, v4f c) {
 }
 
 hipError_t launch_tiles_bf16(int src, const Args& p, const ProductPlan& plan, hipStream_t stream);
+hipError_t launch_tiles_few(int src, const Args& p, int splits, hipStream_t stream);
 hipError_t launch_tiles_scaled(const Args& p, const ProductPlan& plan, hipStream_t stream);
 
 }  // namespace costa

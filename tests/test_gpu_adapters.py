@@ -109,7 +109,8 @@ class Case:
 
 
 SHAPES = [(1, 1, 1, 1, 1), (1, 40, 300, 3, 4), (3, 7, 5, 2, 3), (5, 2049, 8, 4, 16), (17, 130, 2500, 6, 24), (64, 515, 127, 9, 33),
-          (65, 1, 9, 2, 5), (66, 5, 3, 2, 17), (70, 129, 1030, 3, 16), (200, 520, 257, 40, 8), (333, 199, 1250, 5, 100),
+          (65, 1, 9, 2, 5), (66, 5, 3, 2, 17), (33, 1000, 300, 2, 8), (61, 702, 1030, 6, 16),
+          (70, 129, 1030, 3, 16), (200, 520, 257, 40, 8), (333, 199, 1250, 5, 100),
           (130, 1000, 64, 2, 256), (513, 260, 2048, 7, 64)]
 
 

@@ -86,7 +86,7 @@ class Case:
         return dx, ex, dw, ew
 
 
-SHAPES = [(1, 1, 1), (1, 40, 300), (3, 7, 5), (5, 2049, 8), (17, 130, 2500), (64, 5150, 127), (65, 1, 9), (66, 5, 3),
+SHAPES = [(1, 1, 1), (1, 40, 300), (3, 7, 5), (5, 2049, 8), (17, 130, 2500), (64, 5150, 127), (61, 2501, 520), (65, 1, 9), (66, 5, 3),
           (70, 129, 1030), (200, 2500, 257), (333, 1999, 40), (300, 4200, 64), (257, 513, 1029), (513, 1030, 130)]
 
 
