@@ -440,10 +440,10 @@ extern "C" costa_status costa_mx_loss_workspace(int64_t m, int64_t n, int64_t k,
       const size_t at = up16((size_t)m * 4);
       give(least, at + up16((size_t)m * chunks_kept(n, kPieceColumns) * sizeof(LossStat)) + least_piece(m, n, 4));
       const size_t sums = piece_bytes(m, n, 4);
-      // (statistics of every 32 columns, where the logits stay in the tiles)
+      // (statistics of every 128 columns, where the logits stay in the tiles)
       give(most, at + std::max(up16((size_t)m * chunks_kept(n, kPieceColumns) * sizeof(LossStat)) +
                                    std::max(sums, mx_product_parts_workspace(m, std::min(n, piece_columns(m, n, sums, 4)), k)),
-                               (size_t)m * ((n + 31) / 32) * sizeof(LossStat)));
+                               (size_t)m * ((n + 127) / 128) * sizeof(LossStat)));
     } else {
       const size_t dx = up16((size_t)m * k * 4) + 16;  // what dX is summed in, and G's scale
       give(least, dx + up16(least_piece(m, n, 4)) + up16(least_piece(m, n, 4)));

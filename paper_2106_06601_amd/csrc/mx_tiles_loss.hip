@@ -20,16 +20,16 @@ struct LossTile {
   const float* scale;  // dloss is divided by it (null: 1)
 };
 
-// Largest logit and the sum of exponentials from it of a wave's columns, to stats[wave column * m + row]; the
+// Largest logit and the sum of exponentials from it of a tile's columns, to stats[tile column * m + row]; the
 // target's logit, to at[row].
 template <int SRC, int BBITS, int BM, int BN>
 __global__ __launch_bounds__(kLanes) void tiles_loss_stats(Args p, LossTile a, uint32_t nm, uint32_t nn) {
-  constexpr int MT = BM / 2 / 16, NT = BN / (kWaves / 2) / 16;
+  constexpr int WN = kWaves / 2, MT = BM / 2 / 16, NT = BN / WN / 16;
   TileSums<MT, NT> t;
   tile_sums<SRC, false, BBITS, BM, BN, 2, 1, true, 0>(p, nm, nn, t);
   const int lane = threadIdx.x % 64, l = lane % 16, g = lane / 16;
-  LossStat* const to = a.stats + t.col / (16 * NT) * p.m;
-  if (t.col >= p.n) return;
+  const int64_t row0 = t.row - t.wave / WN * (BM / 2);  // of the tile
+  LossStat* const red = reinterpret_cast<LossStat*>(t.shared);  // a row's, of the waves that have its columns
   int64_t target[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) target[i] = a.target[min(t.row + 16 * i + l, p.m - 1)];
@@ -56,7 +56,15 @@ __global__ __launch_bounds__(kLanes) void tiles_loss_stats(Args p, LossTile a, u
       for (int q = 0; q < 4; ++q) sum += exp_of(t.acc[i][j][q] - from);
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
-    if (g == 0 && row < p.m) to[row] = LossStat{top, sum};
+    if (g == 0) red[t.wave % WN * BM + (int)(row - row0)] = LossStat{top, sum};
+  }
+  __syncthreads();
+  const int64_t row = row0 + threadIdx.x;
+  if (threadIdx.x < BM && row < p.m) {
+    LossStat all = red[threadIdx.x];
+#pragma unroll
+    for (int w = 1; w < WN; ++w) all = join_stats(all, red[w * BM + threadIdx.x]);
+    a.stats[(t.col - t.wave % WN * (16 * NT)) / BN * p.m + row] = all;
   }
 }
 
@@ -153,7 +161,7 @@ bool mx_loss_fused(costa_real type, int bits, int64_t m, int64_t n, int64_t k) {
 }
 
 int64_t mx_loss_tile_chunks(costa_real type, int bits, int64_t m, int64_t n, int64_t k) {
-  return up_div(n, plan_loss(source_of(type), bits, m, n, k).bn / 4);
+  return up_div(n, plan_loss(source_of(type), bits, m, n, k).bn);
 }
 
 hipError_t launch_mx_loss_tiles(const ProductArgs& x, const int64_t* target, LossStat* stats, float* at,
