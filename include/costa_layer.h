@@ -62,7 +62,7 @@ costa_status costa_mx_norm_workspace(int64_t rows, int64_t cols, size_t* least, 
  * and of B (count*rank x n) are those of adapter a, both kept rank by rank: B is
  * the transpose of the usual n x rank matrix, so that the two change places in the backward
  * pass.  ranks (device memory, `count` entries; NULL: all of them `rank`): how many of its
- * rows an adapter has (taken into 0 .. rank); those past it are not read.  scales (device
+ * rows an adapter has (taken into 0 .. rank); what stands past them has no effect.  scales (device
  * memory, `count`; NULL: 1): s below. */
 typedef struct {
   int32_t count, rank;
@@ -117,7 +117,7 @@ costa_status costa_mx_loss(float alpha, const costa_matrix* X, const costa_mx* W
  * dloss (NULL: ones): m floats, the gradient that reaches each row's loss.  dX with WT and dW
  * with XT may be NULL, not both.  lse: what costa_mx_loss() gave.  Probabilities below 2^-126 are 0.
  * G is held in 32 bits, or, where dX and dW (those wanted) are BF16, in bfloat16 as G divided by
- * the largest |dloss| (dW: where the vocabulary is large enough for whole tiles); it goes
+ * the largest |dloss| of rows that count (dW: where the vocabulary is large enough for whole tiles); it goes
  * back in before dX and dW are rounded. */
 costa_status costa_mx_loss_backward(float alpha, const costa_matrix* X, const costa_mx* W, const int64_t* target,
                                     const float* lse, const float* dloss, const costa_mx* WT, const costa_matrix* dX,

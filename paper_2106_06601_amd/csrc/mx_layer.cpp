@@ -573,7 +573,7 @@ extern "C" costa_status costa_mx_loss_backward(float alpha, const costa_matrix* 
       per = piece_columns(m, n, half, 4);
       fused = mx_loss_fused(X->type, w.bits, m, per, k);
     }
-    if (bf16) HIP_OR_FAIL(launch_mx_loss_scale(m, dloss, scale, stream));
+    if (bf16) HIP_OR_FAIL(launch_mx_loss_scale(m, n, target, dloss, scale, stream));
     const float* const by = bf16 ? scale : nullptr;
     void* const g = room;
     const size_t taken = up16((size_t)m * per * (fused && bf16 ? 2 : 4));

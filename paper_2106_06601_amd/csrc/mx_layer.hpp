@@ -144,9 +144,12 @@ hipError_t launch_mx_loss_tiles(const ProductArgs& x, const int64_t* target, Los
 hipError_t launch_mx_loss_grad_tiles(const ProductArgs& x, int64_t vocabulary, int64_t col0, const int64_t* target,
                                      const float* lse, const float* dloss, const float* scale, void* g, bool bf16,
                                      hipStream_t stream);
-// scale <- the largest |dloss| (1 where that is 0 or not finite, and without dloss): what a G in bfloat16
-// is divided by, and its products are multiplied by.
-hipError_t launch_mx_loss_scale(int64_t m, const float* dloss, float* scale, hipStream_t stream);
+// scale <- the largest |dloss| of rows that count (1 where that is 0 or not finite, and without dloss): what a
+// G in bfloat16 is divided by, and its products are multiplied by.  (Where all of them are equal,
+// as in a mean, the target's element of an unsure row, nearly -1, loses nothing to its rounding;
+// rounded as a part of 1/3686 all of them were 1.6e-3 off, in the same direction.)
+hipError_t launch_mx_loss_scale(int64_t m, int64_t n, const int64_t* target, const float* dloss, float* scale,
+                                hipStream_t stream);
 // The gradient of the vocabulary's weights from a G in bfloat16, with the scale out of device memory:
 // C <- alpha scale G^T B^^T + beta C, where the products' tiles take it (G m x n by rows, n rows of C).
 bool mx_loss_dw_fused(int bits, int64_t m, int64_t n, int64_t k);

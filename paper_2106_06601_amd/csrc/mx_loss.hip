@@ -111,12 +111,17 @@ __global__ __launch_bounds__(256) void loss_grad(LogitsPart p, int64_t vocabular
   }
 }
 
-__global__ __launch_bounds__(1024) void loss_scale(int64_t m, const float* dloss, float* scale) {
+__global__ __launch_bounds__(1024) void loss_scale(int64_t m, int64_t n, const int64_t* target, const float* dloss,
+                                                   float* scale) {
   __shared__ uint32_t red[16];
   uint32_t top = 0;  // (magnitudes' bits: NaN above infinity above the finite ones)
   if (dloss)
 #pragma unroll 8
-    for (int64_t i = threadIdx.x; i < m; i += 1024) top = max(top, magnitude(dloss[i]));
+    for (int64_t i = threadIdx.x; i < m; i += 1024) {
+      const int64_t t = target[i];
+      const uint32_t d = magnitude(dloss[i]);
+      top = max(top, t >= 0 && t < n ? d : 0u);
+    }
 #pragma unroll
   for (int by = 32; by > 0; by /= 2) top = max(top, (uint32_t)__shfl_xor((int)top, by));
   if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = top;
@@ -169,8 +174,9 @@ hipError_t launch_mx_loss_join(int64_t m, int64_t n, int64_t chunks, const LossS
   return hipGetLastError();
 }
 
-hipError_t launch_mx_loss_scale(int64_t m, const float* dloss, float* scale, hipStream_t stream) {
-  loss_scale<<<1, 1024, 0, stream>>>(m, dloss, scale);
+hipError_t launch_mx_loss_scale(int64_t m, int64_t n, const int64_t* target, const float* dloss, float* scale,
+                                hipStream_t stream) {
+  loss_scale<<<1, 1024, 0, stream>>>(m, n, target, dloss, scale);
   return hipGetLastError();
 }
 

@@ -256,6 +256,26 @@ def test_rows_that_do_not_count_see_nothing():
             assert not wide(DX)[3].any() and np.isnan(wide(DX)[5]).all() and np.isfinite(wide(DX)[fine]).all()
 
 
+@pytest.mark.parametrize("m,n", [(20, 300), (200, 9000)])
+def test_factors_of_rows_that_do_not_count(m, n):
+    """In bfloat16 G is held as a part of the largest factor: NaN, infinities and huge ones of rows that do not
+    count have no part in that, nor factors that are all 0."""
+    k = 64
+    c = Case(m, n, k, "bf16", 8)
+    x, target = c.x.cuda(), c.target.cuda()
+    lse = torch.from_numpy(c.lse.astype(np.float32)).cuda()
+    kept = c.d.clone()
+    for odd in (float("nan"), float("inf"), 3e38):
+        c.d = torch.where(torch.from_numpy(c.counts), kept, torch.tensor(odd))
+        dx, ex, _, _ = c.gradients(True, np.zeros((n, k)), np.where(c.counts, wide(kept), 0))
+        DX = torch.full((m, k), 7.0).bfloat16().cuda()
+        C.costa_mx_loss_backward(1.0, x, c.wq, target, lse, c.d.cuda(), WT=c.wtq, dX=DX)
+        assert (np.abs(wide(DX) - dx) <= ex + HALF["bf16"] * np.abs(dx) + TINY["bf16"]).all()
+    DX = torch.full((m, k), 7.0).bfloat16().cuda()
+    C.costa_mx_loss_backward(1.0, x, c.wq, target, lse, torch.zeros(m).cuda(), WT=c.wtq, dX=DX)
+    assert not DX.any()
+
+
 def test_nothing_to_do():
     for m, n, k in ((0, 5, 6), (5, 0, 6), (5, 4, 0), (100, 0, 6), (100, 4, 0)):
         x, (w, wq), (_, wtq), (_, xtq) = torch.ones(m, k).cuda(), keep(np.ones((n, k), np.float32), 8), keep(np.ones((k, n), np.float32), 8), keep(np.ones((k, m), np.float32), 8)
