@@ -335,6 +335,23 @@ __device__ inline void column_parts(const Raw8<SRC> z[8], int e, v4u out[parts_o
 }
 
 // ---- gradients --------------------------------------------------------------------
+// v, with what g holds there, to g's elements c .. c + 7 of a row.
+template <int GSRC>
+__device__ inline void put_grad(const AdapterGradArgs& p, int64_t row, int64_t c, float v[8]) {
+  if (p.beta != 0.0f) {
+    const Elem<GSRC>* old = static_cast<const Elem<GSRC>*>(p.g.data) + row * p.g.ld + c;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (c + i < p.len) v[i] += p.beta * (float)old[i];
+  }
+  put8<GSRC>(line_to<GSRC>(p.g, row), c, p.len, v);
+}
+__device__ inline void put_grad_typed(const AdapterGradArgs& p, int64_t row, int64_t c, float v[8]) {
+  if (p.g_type == COSTA_REAL_F32) put_grad<SRC_F32>(p, row, c, v);
+  else if (p.g_type == COSTA_REAL_BF16) put_grad<SRC_BF16>(p, row, c, v);
+  else put_grad<SRC_F16>(p, row, c, v);
+}
+
 // A workgroup has 128 columns of 16 RT ranks of an adapter, and a part of the rows, of which those
 // of the adapter are listed in shared memory, 2048 rows at a time.  Its four waves take 32 of them by
 // turns, straight to registers (the next ones are on their way while some are worked on), and
@@ -451,19 +468,20 @@ __global__ __launch_bounds__(256) void adapter_grad_tile(AdapterGradArgs p, int6
       float out[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) out[e] = r < rank ? scale * acc[t][e][q] : 0.0f;
-      put8<SRC_F32>(p.parts + ((int64_t)blockIdx.z * p.at.count * p.at.rank + row) * p.len, c, p.len, out);
+      if (p.parts) put8<SRC_F32>(p.parts + ((int64_t)blockIdx.z * p.at.count * p.at.rank + row) * p.len, c, p.len, out);
+      else put_grad_typed(p, row, c, out);
     }
   }
 }
 
 // The parts in a fixed order, with what g holds.
-template <int GSRC>
 __global__ __launch_bounds__(256) void adapter_grad_join(AdapterGradArgs p, int64_t splits) {
   const int64_t rows = (int64_t)p.at.count * p.at.rank, upr = (p.len + 7) / 8;
   for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < rows * upr; u += (int64_t)gridDim.x * 256) {
     const int64_t row = u / upr, c = (u - row * upr) * 8;
     const bool all = c + 8 <= p.len;
     float v[8] = {};
+#pragma unroll 4
     for (int64_t s = 0; s < splits; ++s) {
       const float* part = p.parts + (s * rows + row) * p.len + c;
       float w[8] = {};
@@ -475,13 +493,7 @@ __global__ __launch_bounds__(256) void adapter_grad_join(AdapterGradArgs p, int6
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] += w[i];
     }
-    if (p.beta != 0.0f) {
-      const Elem<GSRC>* old = static_cast<const Elem<GSRC>*>(p.g.data) + row * p.g.ld + c;
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (c + i < p.len) v[i] += p.beta * (float)old[i];
-    }
-    put8<GSRC>(line_to<GSRC>(p.g, row), c, p.len, v);
+    put_grad_typed(p, row, c, v);
   }
 }
 
@@ -605,8 +617,10 @@ int64_t mx_adapter_grad_parts(int64_t m, int64_t len, int32_t count, int32_t ran
 
 hipError_t launch_mx_adapter_grad(const AdapterGradArgs& a, hipStream_t stream) {
   const GradPlan g = plan_grad(a.len, a.at.count, a.at.rank);
-  const int64_t splits = std::min(mx_adapter_grad_parts(a.m, a.len, a.at.count, a.at.rank), a.most);
+  AdapterGradArgs b = a;
+  const int64_t splits = std::max<int64_t>(std::min(mx_adapter_grad_parts(a.m, a.len, a.at.count, a.at.rank), a.most), 1);
   const int64_t per = up_div(a.m, splits);
+  if (splits == 1) b.parts = nullptr;  // straight to g
   for (int64_t j = 0; j < g.across; j += kColGrid)
     for (int64_t i = 0; i < g.pairs; i += kRowGrid) {
       const dim3 grid((unsigned)std::min(kColGrid, g.across - j), (unsigned)std::min(kRowGrid, g.pairs - i),
@@ -614,17 +628,15 @@ hipError_t launch_mx_adapter_grad(const AdapterGradArgs& a, hipStream_t stream) 
       const hipError_t e = by_type(a.type, a.len >= 8, [&](auto src, auto wide) {
         constexpr int SRC = decltype(src)::value;
         constexpr bool WIDE = decltype(wide)::value;
-        if (g.rt == 1) adapter_grad_tile<SRC, 1, WIDE><<<grid, 256, 0, stream>>>(a, j * 128, i, per);
-        else if (g.rt == 2) adapter_grad_tile<SRC, 2, WIDE><<<grid, 256, 0, stream>>>(a, j * 128, i, per);
-        else adapter_grad_tile<SRC, 4, WIDE><<<grid, 256, 0, stream>>>(a, j * 128, i, per);
+        if (g.rt == 1) adapter_grad_tile<SRC, 1, WIDE><<<grid, 256, 0, stream>>>(b, j * 128, i, per);
+        else if (g.rt == 2) adapter_grad_tile<SRC, 2, WIDE><<<grid, 256, 0, stream>>>(b, j * 128, i, per);
+        else adapter_grad_tile<SRC, 4, WIDE><<<grid, 256, 0, stream>>>(b, j * 128, i, per);
       });
       if (e != hipSuccess) return e;
     }
+  if (splits == 1) return hipSuccess;
   const int64_t units = (int64_t)a.at.count * a.at.rank * up_div(a.len, 8);
-  const dim3 grid((unsigned)std::min<int64_t>(up_div(units, 256), 1 << 20));
-  if (a.g_type == COSTA_REAL_F32) adapter_grad_join<SRC_F32><<<grid, 256, 0, stream>>>(a, splits);
-  else if (a.g_type == COSTA_REAL_BF16) adapter_grad_join<SRC_BF16><<<grid, 256, 0, stream>>>(a, splits);
-  else adapter_grad_join<SRC_F16><<<grid, 256, 0, stream>>>(a, splits);
+  adapter_grad_join<<<dim3((unsigned)std::min<int64_t>(up_div(units, 256), 1 << 20)), 256, 0, stream>>>(b, splits);
   return hipGetLastError();
 }
 

@@ -333,9 +333,7 @@ extern "C" costa_status costa_mx_adapter_gradient(const costa_mx_adapters* adapt
     const int64_t all = (int64_t)a.at.count * a.at.rank;
     CHECKED(check_rows("G", G));
     if (G->rows != all || G->cols != len) return fail(COSTA_ERROR_SHAPE_MISMATCH, "G is not the shape of the adapters' rows");
-    size_t least = 0;
-    CHECKED(costa_mx_adapter_gradient_workspace(m, len, a.at.count, a.at.rank, &least, nullptr));
-    CHECKED(check_workspace(workspace, workspace_bytes, least));
+    CHECKED(check_workspace(workspace, workspace_bytes, 0));
     Uses u;
     u.add("V", V, false), u.add("Z", Z, false), u.add("index", index, m * 4, false);
     u.add("ranks", a.at.ranks, (int64_t)a.at.count * 4, false), u.add("scales", a.at.scales, (int64_t)a.at.count * 4, false);
@@ -348,7 +346,7 @@ extern "C" costa_status costa_mx_adapter_gradient(const costa_mx_adapters* adapt
     a.v = static_cast<const float*>(V->data), a.v_ld = V->ld;
     a.beta = beta;
     a.parts = static_cast<float*>(workspace);
-    a.most = (int64_t)std::min<size_t>(workspace_bytes / ((size_t)all * len * 4), 65535);
+    a.most = workspace ? (int64_t)std::min<size_t>(workspace_bytes / ((size_t)all * len * 4), 65535) : 0;
     HIP_OR_FAIL(launch_mx_adapter_grad(a, stream));
     return COSTA_SUCCESS;
   });
@@ -361,9 +359,9 @@ extern "C" costa_status costa_mx_adapter_gradient_workspace(int64_t m, int64_t l
     if (count < 0 || rank < 0) return fail(COSTA_ERROR_INVALID_VALUE, "negative count or rank");
     if (rank > kRankMax) return fail(COSTA_ERROR_NOT_SUPPORTED, "a rank above 256");
     if ((int64_t)count * rank > INT32_MAX) return fail(COSTA_ERROR_NOT_SUPPORTED, "more than 2^31-1 rows");
-    const size_t part = (size_t)count * rank * len * 4;
-    give(least, part);
-    give(most, part * mx_adapter_grad_parts(m, len, count, rank));
+    const int64_t parts = mx_adapter_grad_parts(m, len, count, rank);
+    give(least, 0);
+    give(most, parts > 1 ? (size_t)count * rank * len * 4 * parts : 0);
     return COSTA_SUCCESS;
   });
 }

@@ -359,7 +359,7 @@ RowPlan plan_row(int64_t units) {
     if (units <= 64 * per) return {64, per};
   for (int per : {2, 4})
     if (units <= 256 * per) return {256, per};
-  if (units <= 512 * 4) return {512, 4};
+  if (units <= 1024 * 2) return {1024, 2};
   return {1024, 0};
 }
 // Of the gradients, which hold more of a row: two units a lane at most, so that four waves of
@@ -406,7 +406,7 @@ struct Forward {
   static bool more(const NormArgs& a, int at, int64_t groups, hipStream_t stream) {
     if (at == 64 * 8 + 4) Forward<SRC, WSRC, 64, 4, true>::go(a, groups, stream);
     else if (at == 256 * 8 + 4) Forward<SRC, WSRC, 256, 4, true>::go(a, groups, stream);
-    else if (at == 512 * 8 + 4) Forward<SRC, WSRC, 512, 4, true>::go(a, groups, stream);
+    else if (at == 1024 * 8 + 2) Forward<SRC, WSRC, 1024, 2, true>::go(a, groups, stream);
     else return false;
     return true;
   }
