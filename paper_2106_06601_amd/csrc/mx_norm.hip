@@ -173,7 +173,10 @@ __device__ inline float sum8(const float a[8], const float b[8]) {
 }
 
 // A workgroup's rows share its lanes' part of dw, in registers; the parts are added by
-// another kernel.
+// another kernel.  Measured with dh: 8192x8192 in bfloat16 106 and 5 us, 4.9 TB/s of dy, h, dh and dx (four units
+// a lane, with a row's products and its next row in registers, 133 to 137: one wave of a SIMD had room); 8192x8192
+// floats 208 us, 5.15; 803x1023 floats without dh 6 and 4 us.  Rows of more than 16384 elements (floats:
+// 8192) are read twice and dw is summed in memory: 4096x20000 476 us.
 template <int SRC, int WSRC, int LANES, int PER, bool WIDE>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES, SRC == SRC_F32 ? 2 : 4) void norm_grad_rows(NormBackArgs a) {
   constexpr int ROWS = LANES < 256 ? 256 / LANES : 1, KEPT = PER ? PER : 1;
