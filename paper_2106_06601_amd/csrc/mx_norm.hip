@@ -35,11 +35,25 @@ __device__ inline double row_sum(double v, double* shared) {
 }
 
 // 1 / sqrt(v): the instruction's estimate and one step of Newton's, which leaves about
-// 46 bits.  0 for an infinity.
-__device__ inline float rsqrt_of(double v) {
-  const double r = __builtin_amdgcn_rsq(v);
-  const double e = fma(-0.5 * v * r, r, 0.5);
-  return (float)(v < __builtin_inf() ? fma(r, e, r) : r);
+// 46 bits: a float and what it is off by.  0 for an infinity.
+struct Factor {
+  float s, rest;
+};
+__device__ inline Factor rsqrt_of(double v) {
+  const double r0 = __builtin_amdgcn_rsq(v);
+  const double e = fma(-0.5 * v * r0, r0, 0.5);
+  const double r = v < __builtin_inf() ? fma(r0, e, r0) : r0;
+  const float s = (float)r;
+  return Factor{s, (float)(r - (double)s)};
+}
+
+// h f w with its roundings made good, so that it is the nearest float (all but where it lies within
+// 2^-20 steps of the middle of two): a rounding to few bits then falls on the side that the
+// definition's does.  Three instructions of each kind more than two products.
+__device__ inline float scaled(float h, Factor f, float w) {
+  const float p = h * f.s, e = fmaf(h, f.s, -p) + h * f.rest;
+  const float t = p * w, y = t + (fmaf(p, w, -t) + e * w);
+  return __builtin_fabsf(t) < __builtin_inff() ? y : t;
 }
 
 // y in few bits: a block's scale from four neighbouring lanes.  Lanes past the matrix have
@@ -70,19 +84,17 @@ __device__ inline void unit_h(const NormArgs& a, Raw8<SRC>& x, Raw8<SRC>& r, I c
 }
 template <int SRC, int WSRC, bool WIDE, typename I>
 __device__ inline void unit_y(const NormArgs& a, int64_t row, I unit, I cols, const float h[8], const Raw8<WSRC>& w,
-                              float s) {
+                              Factor f) {
   const I c = unit * 8;
   if (a.h.data && c < cols) put8<SRC>(line_to<SRC>(a.h, row), c, cols, h);
   if (!a.y.data && !a.q.data) return;
-  float y[8];
+  float y[8], v[8];
+  if (a.w) raw_floats<WSRC>(w, v);
+  else
 #pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = h[i] * s;
-  if (a.w) {
-    float v[8];
-    raw_floats<WSRC>(w, v);
+    for (int i = 0; i < 8; ++i) v[i] = 1.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] *= v[i];
-  }
+  for (int i = 0; i < 8; ++i) y[i] = scaled(h[i], f, v[i]);
   if (c + 8 > cols)  // (what pads a row is +0, whatever s)
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = c + i < cols ? y[i] : 0.0f;
@@ -95,9 +107,10 @@ __device__ inline void unit_y(const NormArgs& a, int64_t row, I unit, I cols, co
 
 // LANES lanes a row, PER units of each: a wave for rows of up to 2048 elements, so that no barrier
 // stands between a row's sum and its results, then four, then sixteen.  PER 0: rows of any length,
-// which are read twice.  Measured (h and 8 bits out of x and r): 16384x8192 in bfloat16 187 us, 5.05 TB/s of
-// what is read and written (a plain copy reaches 5.1); 65536x512 40 us, 5.8; 4096x16384 109 us, 4.3;
-// 4096x20000 (twice read) 160 us, 3.5; 8192x8192 floats 181 us, 4.85; one row of 4096 3.8 us.
+// which are read twice.  Measured (h and 8 bits out of x and r): 16384x8192 in bfloat16 191 us, 4.95 TB/s of
+// what is read and written (a plain copy reaches 5.1; 187 us with y rounded twice more); 65536x512 41 us,
+// 5.7; 4096x16384 114 us, 4.1; 4096x20000 (twice read) 164 us, 3.5; 8192x8192 floats 181 us, 4.8; one row of 4096
+// 3.8 us.
 template <int SRC, int WSRC, int LANES, int PER, bool WIDE>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_rows(NormArgs a) {
   constexpr int ROWS = LANES < 256 ? 256 / LANES : 1, KEPT = PER ? PER : 1;
@@ -132,11 +145,11 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_rows(NormArgs 
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum = fma((double)h[p][i], (double)h[p][i], sum);
       }
-      const float s = rsqrt_of(row_sum<LANES>(sum, sums) * a.inverse + (double)a.eps);
+      const Factor f = rsqrt_of(row_sum<LANES>(sum, sums) * a.inverse + (double)a.eps);
       if (mine < a.rows) {
-        if (a.rstd && lane == 0) a.rstd[row] = s;
+        if (a.rstd && lane == 0) a.rstd[row] = f.s;
 #pragma unroll
-        for (int p = 0; p < PER; ++p) unit_y<SRC, WSRC, WIDE>(a, row, lane + p * LANES, cols, h[p], w[p], s);
+        for (int p = 0; p < PER; ++p) unit_y<SRC, WSRC, WIDE>(a, row, lane + p * LANES, cols, h[p], w[p], f);
       }
     } else {
       Raw8<SRC> x, r;
@@ -148,8 +161,8 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_rows(NormArgs 
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum = fma((double)h[i], (double)h[i], sum);
       }
-      const float s = rsqrt_of(row_sum<LANES>(sum, sums) * a.inverse + (double)a.eps);
-      if (a.rstd && lane == 0) a.rstd[row] = s;
+      const Factor f = rsqrt_of(row_sum<LANES>(sum, sums) * a.inverse + (double)a.eps);
+      if (a.rstd && lane == 0) a.rstd[row] = f.s;
       // (whole rounds of lanes: a block's four lanes stay together)
       for (I u = lane; u < (units + LANES - 1) / LANES * LANES; u += LANES) {
         get8<SRC, WIDE>(x, xl, u * 8, cols);
@@ -159,7 +172,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_rows(NormArgs 
           placed8<WSRC, WIDE>(w[0], u * 8, cols);
         }
         unit_h<SRC, WIDE>(a, x, r, u * 8, cols, h);
-        unit_y<SRC, WSRC, WIDE>(a, row, u, cols, h, w[0], s);
+        unit_y<SRC, WSRC, WIDE>(a, row, u, cols, h, w[0], f);
       }
     }
   }

@@ -122,6 +122,22 @@ def test_norm(shape, dtype, wtype, res):
                 into.copy_(kept)
 
 
+@pytest.mark.parametrize("dtype,wtype", [("bf16", "bf16"), ("bf16", "f32"), ("f16", "f16"), ("f32", "f32")])
+@pytest.mark.parametrize("bits", [4, 8])
+def test_few_bits_are_those_of_the_definition(dtype, wtype, bits):
+    """y is the float nearest to the formula's in 64 bits, but where that lies within about 2^-20 steps of the
+    middle of two (or x + r is no float: no residual for floats, and sums of 16-bit values that lie within 2^13 of one
+    another are): the codes are those of that float, for each of some 300000 elements and these inputs."""
+    m, n = 61, 5003
+    rng = np.random.default_rng(17)
+    x, r, w = inputs(rng, m, n, dtype, dtype != "f32", wtype)
+    y = formula(x, r, w)[2]
+    q = C.MxMatrix.empty(bits, m, n)
+    C.costa_mx_norm(EPS, x.cuda(), w.cuda(), R=None if r is None else r.cuda(), Q=q)
+    data, scales = F.encode(y.astype(np.float32), bits)
+    assert (q.data.cpu().numpy().reshape(m, -1) == data).all() and (q.scales.cpu().numpy().reshape(m, -1) == scales).all()
+
+
 @pytest.mark.parametrize("shape", SHAPES + [(700, 33), (300, 257), (130, 2055), (65, 5000)], ids=str)
 @pytest.mark.parametrize("dtype,wtype", [("f32", "f32"), ("bf16", "f32"), ("f16", "f16"), ("bf16", None)])
 @pytest.mark.parametrize("res", [False, True])
@@ -197,6 +213,16 @@ def test_magnitudes_that_do_not_square_in_floats():
         s = 1 / np.sqrt((h * h).mean(1) + 2.0**-126)
         assert (np.abs(wide(rstd) - s) <= 3 * U * s).all()
         assert (np.abs(wide(Y) - h * s[:, None]) <= 8 * U * np.abs(h * s[:, None]) + 2.0**-149).all()
+
+
+def test_weights_that_are_not_finite():
+    x, w = torch.ones(3, 40).cuda(), torch.ones(40).cuda()
+    w[5], w[7], w[9] = float("inf"), float("nan"), 3e38
+    Y = torch.zeros_like(x)
+    C.costa_mx_norm(EPS, x * torch.tensor([[1.0], [-2.0], [4.0]]).cuda(), w, Y=Y)
+    y = wide(Y)
+    assert (y[:, 5] == np.array([np.inf, -np.inf, np.inf])).all() and np.isnan(y[:, 7]).all()
+    assert np.isfinite(np.delete(y, (5, 7), 1)).all()
 
 
 def test_rows_of_zeros_infinities_and_nan():
