@@ -42,15 +42,18 @@ inline int64_t splits_max(int64_t m, int64_t n) {
 // 1041x1999x2501.)
 // (512x8192x8192 in bfloat16: 128x128 unsplit 88 us, 256x256 unsplit 232, split in four 86;
 // 256x8192x8192: 128x128 split in four 53, 128x64 unsplit 72; 1024^3: 128x64 13, 128x128 17.)
-inline double tiled_time(bool scaled, int parts, int64_t bm, int64_t bn, int64_t splits, int64_t m, int64_t n, int64_t k) {
+// in_parts: the sums stay in parts, split or not, for a kernel that reads them anyway.
+inline double tiled_time(bool scaled, int parts, int64_t bm, int64_t bn, int64_t splits, int64_t m, int64_t n, int64_t k,
+                         bool in_parts = false) {
   const double size = (double)(bm * bn * parts) / 65536.0;
   const double share = scaled ? 0.2 + 2.4 * size : 0.22 + 1.55 * size, alone = scaled ? 1.0 : 0.66;
   const int64_t groups = up_div(m, bm) * up_div(n, bn) * splits, steps = up_div(up_div(k, scaled ? 256 : 64), splits);
   const double step = std::max(alone, (double)up_div(groups, kCUs) * share);
-  return 3.0 + (double)steps * step + (splits > 1 ? 3.0 + (double)splits * m * n * 8e-6 / 4.0 : 0.0);
+  const double way = (double)splits * m * n * 8e-6 / 4.0;
+  return 3.0 + (double)steps * step + (in_parts ? way : splits > 1 ? 3.0 + way : 0.0);
 }
 
-inline ProductPlan plan_product(int src, bool k_next, int bbits, int64_t m, int64_t n, int64_t k) {
+inline ProductPlan plan_product(int src, bool k_next, int bbits, int64_t m, int64_t n, int64_t k, bool in_parts = false) {
   ProductPlan r{};
   if (src != SRC_MX4 && src != SRC_MX8 && k < 8) {
     r.variant = THIN;
@@ -82,7 +85,7 @@ inline ProductPlan plan_product(int src, bool k_next, int bbits, int64_t m, int6
     for (int64_t c = 0; c < 8; ++c) {
       const int64_t s = std::min(c < 4 ? c + 1 : (c - 3) * kCUs / std::max<int64_t>(tiles, 1), most);
       if (s < 1) continue;
-      const double t = tiled_time(scaled, parts, bm, bn, s, m, n, k);
+      const double t = tiled_time(scaled, parts, bm, bn, s, m, n, k, in_parts);
       if (r.splits == 0 || t < best) {
         best = t;
         r.bm = bm;

@@ -322,17 +322,18 @@ __global__ __launch_bounds__(256) void scale_only(Epilogue e, int64_t m, int64_t
 
 }  // namespace
 
-size_t mx_product_workspace(int64_t m, int64_t n, int64_t k) {
+static size_t split_workspace(int64_t m, int64_t n, int64_t k, bool in_parts) {
   size_t most = 0;
   if (m == 0 || n == 0 || k == 0) return 0;
   for (int src : {SRC_MX4, SRC_MX8, SRC_BF16, SRC_F16, SRC_F32})
     for (int bbits : {4, 8})
       for (bool k_next : {true, false}) {
-        const ProductPlan r = plan_product(src, k_next, bbits, m, n, k);
+        const ProductPlan r = plan_product(src, k_next, bbits, m, n, k, in_parts);
         if (r.splits > 1) most = std::max(most, (size_t)r.splits * m * n * sizeof(float));
       }
   return most;
 }
+size_t mx_product_workspace(int64_t m, int64_t n, int64_t k) { return split_workspace(m, n, k, false); }
 
 namespace {
 
@@ -345,7 +346,7 @@ hipError_t launch_sums(const ProductArgs& a, const Epilogue& e, bool parts, Prod
                   : a.a_type == COSTA_REAL_F16    ? SRC_F16
                                                   : SRC_F32;
   const bool k_next = a.amx.bits != 0 || a.a_cs == 1;
-  plan = plan_product(src, k_next, a.b.bits, a.m, a.n, a.k);
+  plan = plan_product(src, k_next, a.b.bits, a.m, a.n, a.k, parts);
   Args p{a.m, a.n, a.k, a.amx, a.b, a.real, a.a_rs, a.a_cs, e, 0};
   const size_t part = (size_t)a.m * a.n * sizeof(float);
   plan.splits = (int)std::min<size_t>(plan.splits, a.workspace_bytes / part);
@@ -376,7 +377,7 @@ int64_t some_rows_splits(int src, int64_t m, int64_t n, int64_t k) {
 size_t mx_product_parts_workspace(int64_t m, int64_t n, int64_t k) {
   if (m == 0 || n == 0 || k == 0) return 0;
   const int64_t some = some_rows_splits(SRC_F32, m, n, k);
-  return std::max(mx_product_workspace(m, n, k), (size_t)std::max<int64_t>(some, 1) * m * n * 4);
+  return std::max(split_workspace(m, n, k, true), (size_t)std::max<int64_t>(some, 1) * m * n * 4);
 }
 
 hipError_t launch_mx_product_parts(const ProductArgs& a, int& splits, hipStream_t stream) {
