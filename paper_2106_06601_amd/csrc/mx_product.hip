@@ -362,11 +362,13 @@ hipError_t launch_sums(const ProductArgs& a, const Epilogue& e, bool parts, Prod
 }
 
 // Splits of a product whose sums go on in parts, in tiles of 64 rows; 0 where other kernels take it.
-// (61 rows by 8192x8192 in 4 bits, joined: bfloat16 32 us, with the kernel for few rows 41; float16 35 and 75;
-// float 45 and 91.  32 rows of bfloat16: 28 both.)
+// (61 rows by 8192x8192 in 4 bits, joined: bfloat16 25 us, with the kernel for few rows 41; float16 31 and 75;
+// float 39 and 91.  17 to 32 rows of bfloat16, tiles and the kernel for few rows: 8192x8192 22 and 25 to 28 us,
+// 20000 columns of 4096 26 and 28 to 30, 4096x4096 14 both, 1024 columns of 8192 16 and 14.)
 int64_t some_rows_splits(int src, int64_t m, int64_t n, int64_t k) {
   const int64_t tiles = up_div(n, 128);
-  if (m > 64 || m <= (src == SRC_BF16 ? 32 : 16) || k < 256 || tiles > 1 << 20) return 0;
+  if (m > 64 || m <= 16 || k < 256 || tiles > 1 << 20) return 0;
+  if (src == SRC_BF16 && m <= 32 && tiles < kCUs / 4) return 0;
   // a workgroup for each CU, or two where that leaves sums whole
   const int64_t fill = kCUs / tiles >= 2 ? kCUs / tiles : 2 * kCUs / tiles;
   return std::max<int64_t>(std::min(fill, k / 256), 1);

@@ -139,6 +139,17 @@ def test_adapted_product(shape, dtype, how):
         assert torch.equal(y, got[0])  # V kept or not, and a second time: the same bits
 
 
+# some tens of rows: sums in steps of 128 whose last one holds 1, 127 and all, one step a part and more; 17 to 32 rows of
+# bfloat16 in the tiles of 64 rows (from 64 tiles of columns on) and not; the last tile of one column
+SOME = [(17, 8200, 385, 2, 8), (32, 8065, 641, 3, 5), (32, 8064, 640, 3, 5), (18, 129, 256, 2, 4), (64, 131, 2431, 2, 8), (49, 260, 2433, 3, 12)]
+
+
+@pytest.mark.parametrize("shape", SOME, ids=str)
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_adapted_product_of_some_rows(shape, dtype):
+    test_adapted_product(shape, dtype, "mixed")
+
+
 # rows enough for the products' own tiles to add the adapters' part: tiles of 256 columns and of 128, last
 # ones cut in both directions, ranks that are no multiple of 32, columns no multiple of 4
 TILED = [(2047, 8190, 100, 3, 20), (2048, 8191, 130, 40, 70), (1024, 4096, 64, 2, 32), (1030, 2051, 300, 9, 5), (1300, 1999, 40, 1, 100)]
