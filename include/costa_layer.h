@@ -116,9 +116,10 @@ costa_status costa_mx_loss(float alpha, const costa_matrix* X, const costa_mx* W
  *
  * dloss (NULL: ones): m floats, the gradient that reaches each row's loss.  dX with WT and dW
  * with XT may be NULL, not both.  lse: what costa_mx_loss() gave.  Probabilities below 2^-126 are 0.
- * G is held in 32 bits, or, where dX and dW (those wanted) are BF16, in bfloat16 as G divided by
- * the largest |dloss| of rows that count (dW: where the vocabulary is large enough for whole tiles); it goes
- * back in before dX and dW are rounded. */
+ * G is held in 32 bits, or, where dX and dW (those wanted) are BF16, in bfloat16: for dX alone a row as a part
+ * of |dloss| (1 - p), p the target's probability, so that the target's element is -1 and rounds to itself; with
+ * dW (where the vocabulary is large enough for whole tiles) as a part of the largest |dloss| of rows that
+ * count.  The factors are in 32 bits and go back in before dX and dW are rounded. */
 costa_status costa_mx_loss_backward(float alpha, const costa_matrix* X, const costa_mx* W, const int64_t* target,
                                     const float* lse, const float* dloss, const costa_mx* WT, const costa_matrix* dX,
                                     const costa_mx* XT, float beta, const costa_matrix* dW, void* workspace,

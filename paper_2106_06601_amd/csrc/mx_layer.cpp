@@ -443,7 +443,7 @@ extern "C" costa_status costa_mx_loss_workspace(int64_t m, int64_t n, int64_t k,
                                    std::max(sums, mx_product_parts_workspace(m, std::min(n, piece_columns(m, n, sums, 4)), k)),
                                (size_t)m * ((n + 127) / 128) * sizeof(LossStat)));
     } else {
-      const size_t dx = up16((size_t)m * k * 4) + 16;  // what dX is summed in, and G's scale
+      const size_t dx = up16((size_t)m * k * 4) + up16((size_t)m * 4);  // what dX is summed in, and the factors of G's rows
       give(least, dx + up16(least_piece(m, n, 4)) + up16(least_piece(m, n, 4)));
       const size_t g = piece_bytes(m, n, 4);
       const int64_t per = piece_columns(m, n, g, 4);
@@ -558,9 +558,9 @@ extern "C" costa_status costa_mx_loss_backward(float alpha, const costa_matrix* 
     char* room = static_cast<char*>(workspace);
     float* const sum = reinterpret_cast<float*>(room);  // of dX
     room += up16((size_t)m * k * 4);
-    float* const scale = reinterpret_cast<float*>(room);
-    room += 16;
-    size_t left = workspace_bytes - up16((size_t)m * k * 4) - 16;
+    float* const factor = reinterpret_cast<float*>(room);  // of G's rows
+    room += up16((size_t)m * 4);
+    size_t left = workspace_bytes - up16((size_t)m * k * 4) - up16((size_t)m * 4);
     // half for G, half for the logits, where they are kept, and for what products split
     const size_t half = std::min(left / 32 * 16, up16(piece_bytes(m, n, 4)));
     int64_t per = piece_columns(m, n, half, 2);
@@ -571,8 +571,9 @@ extern "C" costa_status costa_mx_loss_backward(float alpha, const costa_matrix* 
       per = piece_columns(m, n, half, 4);
       fused = mx_loss_fused(X->type, w.bits, m, per, k);
     }
-    if (bf16) HIP_OR_FAIL(launch_mx_loss_scale(m, n, target, dloss, scale, stream));
-    const float* const by = bf16 ? scale : nullptr;
+    if (bf16 && dW) HIP_OR_FAIL(launch_mx_loss_scale(m, n, target, dloss, factor, stream));
+    else if (bf16) HIP_OR_FAIL(launch_mx_loss_factors(logits_of(X, w, 0, n, alpha), target, lse, dloss, factor, stream));
+    const float* const by = bf16 ? factor : nullptr;
     void* const g = room;
     const size_t taken = up16((size_t)m * per * (fused && bf16 ? 2 : 4));
     room += taken, left -= taken;

@@ -131,10 +131,9 @@ hipError_t launch_mx_loss_stats(const LogitsPart& p, LossStat* stats, float* at,
 // From the stats of all chunks.  n: the vocabulary.
 hipError_t launch_mx_loss_join(int64_t m, int64_t n, int64_t chunks, const LossStat* stats, const float* at,
                                const int64_t* target, float* loss, float* lse, hipStream_t stream);
-// g (m x p.n by rows; bfloat16 or float) <- dloss (exp(logit - lse) - [target]); g may be the first part of sums
-// / *scale (null: 1)
+// g (m x p.n by rows; bfloat16 or float; apart from the sums) <- dloss (exp(logit - lse) - [target]) / factor (null: 1)
 hipError_t launch_mx_loss_grad(const LogitsPart& p, int64_t vocabulary, const float* lse, const float* dloss,
-                               const float* scale, void* g, bool bf16, hipStream_t stream);
+                               const float* factor, void* g, bool bf16, hipStream_t stream);
 // Both in the product's own kernel (mx_tiles_loss.hip), where that takes one: statistics by mx_loss_tile_chunks() chunks of
 // columns; of the arguments C, beta and the workspace are not looked at.
 bool mx_loss_fused(costa_real type, int bits, int64_t m, int64_t n, int64_t k);
@@ -142,20 +141,29 @@ int64_t mx_loss_tile_chunks(costa_real type, int bits, int64_t m, int64_t n, int
 hipError_t launch_mx_loss_tiles(const ProductArgs& x, const int64_t* target, LossStat* stats, float* at,
                                 hipStream_t stream);
 hipError_t launch_mx_loss_grad_tiles(const ProductArgs& x, int64_t vocabulary, int64_t col0, const int64_t* target,
-                                     const float* lse, const float* dloss, const float* scale, void* g, bool bf16,
+                                     const float* lse, const float* dloss, const float* factor, void* g, bool bf16,
                                      hipStream_t stream);
-// scale <- the largest |dloss| of rows that count (1 where that is 0 or not finite, and without dloss): what a
-// G in bfloat16 is divided by, and its products are multiplied by.  (Where all of them are equal,
-// as in a mean, the target's element of an unsure row, nearly -1, loses nothing to its rounding;
-// rounded as a part of 1/3686 all of them were 1.6e-3 off, in the same direction.)
-hipError_t launch_mx_loss_scale(int64_t m, int64_t n, const int64_t* target, const float* dloss, float* scale,
+// What the rows of a G in bfloat16 are divided by, and its products are multiplied by, in 32 bits: m floats.
+//
+// For dX alone, whose rows can each have a factor of their own: |dloss| (1 - p), p the target's probability (at least
+// 2^-24 |dloss|; 1 where that is 0 or not finite, and in rows that do not count).  The target's element is then -1
+// and loses nothing to its rounding, and with it goes nearly all of the error: the others' roundings are as
+// large of each, but theirs are many and small.  (4096 rows of 4096 over 65536 words: dX 1.97e-3 off 64 bits with one
+// factor for all rows; so 1.7e-3, which are dX's own rounding, as with a G in 32 bits.)
+hipError_t launch_mx_loss_factors(const ProductArgs& x, const int64_t* target, const float* lse, const float* dloss,
+                                  float* factor, hipStream_t stream);
+// For dW, which sums over the rows, the same for all: the largest |dloss| of rows that count (1 where that is 0 or
+// not finite, and without dloss).  (Where all of them are equal, as in a mean, the target's element of an unsure
+// row, nearly -1, loses little to its rounding; rounded as a part of 1/3686 all of them were 1.6e-3
+// off, in the same direction.)
+hipError_t launch_mx_loss_scale(int64_t m, int64_t n, const int64_t* target, const float* dloss, float* factor,
                                 hipStream_t stream);
-// The gradient of the vocabulary's weights from a G in bfloat16, with the scale out of device memory:
-// C <- alpha scale G^T B^^T + beta C, where the products' tiles take it (G m x n by rows, n rows of C).
+// The gradient of the vocabulary's weights from a G in bfloat16, with the rows' common factor out of device
+// memory: C <- alpha *factor G^T B^^T + beta C, where the products' tiles take it (G m x n by rows, n rows of C).
 bool mx_loss_dw_fused(int bits, int64_t m, int64_t n, int64_t k);
-hipError_t launch_mx_loss_dw(const ProductArgs& a, const float* scale, hipStream_t stream);
-// y <- scale x (scale null: x): floats, to a row-major matrix
-hipError_t launch_mx_round(int64_t m, int64_t n, const float* x, const float* scale, const RowsView& y, costa_real type,
+hipError_t launch_mx_loss_dw(const ProductArgs& a, const float* factor, hipStream_t stream);
+// y <- x times its row's factor (null: x): floats, to a row-major matrix
+hipError_t launch_mx_round(int64_t m, int64_t n, const float* x, const float* factor, const RowsView& y, costa_real type,
                            hipStream_t stream);
 
 }  // namespace costa

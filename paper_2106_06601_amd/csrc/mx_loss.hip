@@ -97,7 +97,7 @@ __global__ __launch_bounds__(1024) void loss_join(int64_t m, int64_t n, int64_t 
 
 template <int GSRC>
 __global__ __launch_bounds__(256) void loss_grad(LogitsPart p, int64_t vocabulary, const float* lse,
-                                                 const float* dloss, const float* scale, void* g) {
+                                                 const float* dloss, const float* factor, void* g) {
   const int64_t upr = (p.n + 7) / 8, units = p.m * upr;
   for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (int64_t)gridDim.x * 256) {
     const int64_t row = ((u | upr) >> 32) == 0 ? (int64_t)((uint32_t)u / (uint32_t)upr) : u / upr, c = (u - row * upr) * 8;
@@ -105,15 +105,52 @@ __global__ __launch_bounds__(256) void loss_grad(LogitsPart p, int64_t vocabular
     logits8(p, row, c, x);
     const int64_t t = p.target[row];
     const bool counts = t >= 0 && t < vocabulary;
-    const float d = counts && dloss ? (scale ? dloss[row] / *scale : dloss[row]) : 1.0f, l = lse[row];
+    const float d = counts ? (dloss ? dloss[row] : 1.0f) / (factor ? factor[row] : 1.0f) : 1.0f, l = lse[row];
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = counts ? d * (exp_of(x[i] - l) - (t - p.col0 - c == i ? 1.0f : 0.0f)) : 0.0f;
     put8<GSRC>(static_cast<Elem<GSRC>*>(g) + row * p.n, c, p.n, x);
   }
 }
 
+// A wave has a row: the target's logit again, and from it how far the row is from sure.
+template <int SRC, int BITS, bool WIDE>
+__global__ __launch_bounds__(256) void loss_factors(int64_t m, int64_t k, RowsView x, MxView w, float alpha,
+                                                    const int64_t* target, const float* lse, const float* dloss,
+                                                    float* factor) {
+  const int lane = threadIdx.x % 64;
+  for (int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64; row < m; row += (int64_t)gridDim.x * 4) {
+    const int64_t t = target[row];
+    if (t < 0 || t >= w.rows) {
+      if (lane == 0) factor[row] = 1.0f;
+      continue;
+    }
+    const void* const xl = line_of<SRC>(x, row);
+    const uint8_t* const data = w.data + t * w.row_bytes;
+    const uint8_t* const scales = w.scales + t * w.row_scales;
+    float sum = 0.0f;
+#pragma unroll 4
+    for (int64_t c = lane * 8; c < k; c += 512) {  // (a row of w is padded with zeros to whole steps of eight)
+      Raw8<SRC> raw;
+      get8<SRC, WIDE>(raw, xl, c, k);
+      v2u d = {0u, 0u};
+      if (BITS == 4) d.x = *reinterpret_cast<const uint32_t*>(data + c / 2);
+      else d = *reinterpret_cast<const v2u*>(data + c);
+      float a[8], b[8];
+      mx_decode8<BITS>(d, scales[c / kMxBlock], b);
+      floats8<SRC, WIDE>(raw, c, k, a);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum = fmaf(a[i], b[i], sum);
+    }
+#pragma unroll
+    for (int by = 32; by > 0; by /= 2) sum += __shfl_xor(sum, by);
+    const float rest = fminf(fmaxf(1.0f - exp_of(alpha * sum - lse[row]), 0x1p-24f), 1.0f);  // (NaN: 2^-24)
+    const float f = (dloss ? __builtin_fabsf(dloss[row]) : 1.0f) * rest;
+    if (lane == 0) factor[row] = f > 0.0f && f < __builtin_inff() ? f : 1.0f;
+  }
+}
+
 __global__ __launch_bounds__(1024) void loss_scale(int64_t m, int64_t n, const int64_t* target, const float* dloss,
-                                                   float* scale) {
+                                                   float* factor) {
   __shared__ uint32_t red[16];
   uint32_t top = 0;  // (magnitudes' bits: NaN above infinity above the finite ones)
   if (dloss)
@@ -127,18 +164,18 @@ __global__ __launch_bounds__(1024) void loss_scale(int64_t m, int64_t n, const i
   for (int by = 32; by > 0; by /= 2) top = max(top, (uint32_t)__shfl_xor((int)top, by));
   if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = top;
   __syncthreads();
-  if (threadIdx.x != 0) return;
 #pragma unroll
   for (int i = 0; i < 16; ++i) top = max(top, red[i]);
-  *scale = top == 0 || top >= 0x7f800000u ? 1.0f : __builtin_bit_cast(float, top);
+  const float all = top == 0 || top >= 0x7f800000u ? 1.0f : __builtin_bit_cast(float, top);
+  for (int64_t i = threadIdx.x; i < m; i += 1024) factor[i] = all;
 }
 
 template <int SRC>
-__global__ __launch_bounds__(256) void round_rows(int64_t m, int64_t n, const float* x, const float* scale, RowsView y) {
+__global__ __launch_bounds__(256) void round_rows(int64_t m, int64_t n, const float* x, const float* factor, RowsView y) {
   const int64_t upr = (n + 7) / 8;
-  const float by = scale ? *scale : 1.0f;
   for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < m * upr; u += (int64_t)gridDim.x * 256) {
     const int64_t row = u / upr, c = (u - row * upr) * 8;
+    const float by = factor ? factor[row] : 1.0f;
     float v[8] = {};
     if (c + 8 <= n) __builtin_memcpy(v, x + row * n + c, sizeof v);
     else
@@ -175,26 +212,46 @@ hipError_t launch_mx_loss_join(int64_t m, int64_t n, int64_t chunks, const LossS
   return hipGetLastError();
 }
 
-hipError_t launch_mx_loss_scale(int64_t m, int64_t n, const int64_t* target, const float* dloss, float* scale,
+hipError_t launch_mx_loss_scale(int64_t m, int64_t n, const int64_t* target, const float* dloss, float* factor,
                                 hipStream_t stream) {
-  loss_scale<<<1, 1024, 0, stream>>>(m, n, target, dloss, scale);
+  loss_scale<<<1, 1024, 0, stream>>>(m, n, target, dloss, factor);
+  return hipGetLastError();
+}
+
+template <int SRC>
+static void launch_factors(const ProductArgs& x, const int64_t* target, const float* lse, const float* dloss, float* factor,
+                           hipStream_t stream) {
+  const dim3 grid((unsigned)std::min<int64_t>(up_div(x.m, 4), 1 << 16));
+  auto go = [&](auto bits, auto wide) {
+    loss_factors<SRC, decltype(bits)::value, decltype(wide)::value><<<grid, 256, 0, stream>>>(
+        x.m, x.k, RowsView{const_cast<void*>(x.real), x.a_rs}, x.b, x.alpha, target, lse, dloss, factor);
+  };
+  auto of = [&](auto bits) { x.k >= 8 ? go(bits, std::true_type{}) : go(bits, std::false_type{}); };
+  if (x.b.bits == 4) of(std::integral_constant<int, 4>{});
+  else of(std::integral_constant<int, 8>{});
+}
+hipError_t launch_mx_loss_factors(const ProductArgs& x, const int64_t* target, const float* lse, const float* dloss,
+                                  float* factor, hipStream_t stream) {
+  if (x.a_type == COSTA_REAL_BF16) launch_factors<SRC_BF16>(x, target, lse, dloss, factor, stream);
+  else if (x.a_type == COSTA_REAL_F16) launch_factors<SRC_F16>(x, target, lse, dloss, factor, stream);
+  else launch_factors<SRC_F32>(x, target, lse, dloss, factor, stream);
   return hipGetLastError();
 }
 
 hipError_t launch_mx_loss_grad(const LogitsPart& p, int64_t vocabulary, const float* lse, const float* dloss,
-                               const float* scale, void* g, bool bf16, hipStream_t stream) {
+                               const float* factor, void* g, bool bf16, hipStream_t stream) {
   const dim3 grid = groups_for(p.m * up_div(p.n, 8));
-  if (bf16) loss_grad<SRC_BF16><<<grid, 256, 0, stream>>>(p, vocabulary, lse, dloss, scale, g);
-  else loss_grad<SRC_F32><<<grid, 256, 0, stream>>>(p, vocabulary, lse, dloss, scale, g);
+  if (bf16) loss_grad<SRC_BF16><<<grid, 256, 0, stream>>>(p, vocabulary, lse, dloss, factor, g);
+  else loss_grad<SRC_F32><<<grid, 256, 0, stream>>>(p, vocabulary, lse, dloss, factor, g);
   return hipGetLastError();
 }
 
-hipError_t launch_mx_round(int64_t m, int64_t n, const float* x, const float* scale, const RowsView& y, costa_real type,
+hipError_t launch_mx_round(int64_t m, int64_t n, const float* x, const float* factor, const RowsView& y, costa_real type,
                            hipStream_t stream) {
   const dim3 grid = groups_for(m * up_div(n, 8));
-  if (type == COSTA_REAL_F32) round_rows<SRC_F32><<<grid, 256, 0, stream>>>(m, n, x, scale, y);
-  else if (type == COSTA_REAL_BF16) round_rows<SRC_BF16><<<grid, 256, 0, stream>>>(m, n, x, scale, y);
-  else round_rows<SRC_F16><<<grid, 256, 0, stream>>>(m, n, x, scale, y);
+  if (type == COSTA_REAL_F32) round_rows<SRC_F32><<<grid, 256, 0, stream>>>(m, n, x, factor, y);
+  else if (type == COSTA_REAL_BF16) round_rows<SRC_BF16><<<grid, 256, 0, stream>>>(m, n, x, factor, y);
+  else round_rows<SRC_F16><<<grid, 256, 0, stream>>>(m, n, x, factor, y);
   return hipGetLastError();
 }
 

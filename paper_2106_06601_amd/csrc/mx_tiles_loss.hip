@@ -21,7 +21,7 @@ struct LossTile {
   float* at;
   const float* lse;
   const float* dloss;
-  const float* scale;  // dloss is divided by it (null: 1)
+  const float* factor;  // a row's dloss is divided by its own (null: 1)
 };
 
 // Largest logit and the sum of exponentials from it of a tile's columns, to stats[tile column * m + row]; the
@@ -83,7 +83,7 @@ __global__ __launch_bounds__(kLanes) void tiles_loss_grad(Args p, LossTile a, ui
   for (int i = 0; i < MT; ++i) {
     const int64_t row = min(t.row + 16 * i + l, p.m - 1), target = a.target[row];
     const bool counts = target >= 0 && target < a.n;
-    const float d = counts && a.dloss ? (a.scale ? a.dloss[row] / *a.scale : a.dloss[row]) : 1.0f, lse = a.lse[row];
+    const float d = counts ? (a.dloss ? a.dloss[row] : 1.0f) / (a.factor ? a.factor[row] : 1.0f) : 1.0f, lse = a.lse[row];
     const int64_t at = target - a.col0 - t.col - 4 * g;
 #pragma unroll
     for (int j = 0; j < NT; ++j)
@@ -97,11 +97,11 @@ __global__ __launch_bounds__(kLanes) void tiles_loss_grad(Args p, LossTile a, ui
 
 // A product with a transposed left operand in bfloat16 whose factor is in device memory.
 template <int BBITS, int BM, int BN, bool EDGE>
-__global__ __launch_bounds__(kLanes) void tiles_loss_dw(Args p, const float* scale, uint32_t nm, uint32_t nn) {
+__global__ __launch_bounds__(kLanes) void tiles_loss_dw(Args p, const float* factor, uint32_t nm, uint32_t nn) {
   constexpr int MT = BM / 2 / 16, NT = BN / (kWaves / 2) / 16;
   TileSums<MT, NT> t;
   tile_sums<SRC_BF16, true, BBITS, BM, BN, 2, 1, EDGE, 0>(p, nm, nn, t);
-  p.e.alpha *= *scale;
+  p.e.alpha *= *factor;
   put_wave<MT, NT>(p, t.acc, t.shared, t.wave, t.row, t.col);
 }
 
@@ -115,14 +115,14 @@ ProductPlan plan_loss(int src, int bits, int64_t m, int64_t n, int64_t k) {
 }
 
 template <int BBITS>
-hipError_t launch_dw(const Args& p, const float* scale, hipStream_t stream) {
+hipError_t launch_dw(const Args& p, const float* factor, hipStream_t stream) {
   ProductPlan plan = plan_product(SRC_BF16, false, BBITS, p.m, p.n, p.k);
   if (plan.bn < 256) plan.bm = plan.bn = 128;
   const uint32_t nm = (uint32_t)up_div(p.m, plan.bm), nn = (uint32_t)up_div(p.n, plan.bn);
   const dim3 grid(nm * nn);
-  if (plan.bn < 256) tiles_loss_dw<BBITS, 128, 128, true><<<grid, kLanes, 0, stream>>>(p, scale, nm, nn);
-  else if (p.m % 4 == 0) tiles_loss_dw<BBITS, 256, 256, false><<<grid, kLanes, 0, stream>>>(p, scale, nm, nn);
-  else tiles_loss_dw<BBITS, 256, 256, true><<<grid, kLanes, 0, stream>>>(p, scale, nm, nn);
+  if (plan.bn < 256) tiles_loss_dw<BBITS, 128, 128, true><<<grid, kLanes, 0, stream>>>(p, factor, nm, nn);
+  else if (p.m % 4 == 0) tiles_loss_dw<BBITS, 256, 256, false><<<grid, kLanes, 0, stream>>>(p, factor, nm, nn);
+  else tiles_loss_dw<BBITS, 256, 256, true><<<grid, kLanes, 0, stream>>>(p, factor, nm, nn);
   return hipGetLastError();
 }
 
@@ -175,11 +175,11 @@ hipError_t launch_mx_loss_tiles(const ProductArgs& x, const int64_t* target, Los
 }
 
 hipError_t launch_mx_loss_grad_tiles(const ProductArgs& x, int64_t vocabulary, int64_t col0, const int64_t* target,
-                                     const float* lse, const float* dloss, const float* scale, void* g, bool bf16,
+                                     const float* lse, const float* dloss, const float* factor, void* g, bool bf16,
                                      hipStream_t stream) {
   const Epilogue e{g, x.n, 1, bf16 ? COSTA_REAL_BF16 : COSTA_REAL_F32, x.n % 4 == 0, 1.0f, 0.0f};
   return launch_loss_type(x.a_type, args_of(x, e),
-                          LossTile{x.alpha, vocabulary, col0, target, nullptr, nullptr, lse, dloss, scale}, stream);
+                          LossTile{x.alpha, vocabulary, col0, target, nullptr, nullptr, lse, dloss, factor}, stream);
 }
 
 bool mx_loss_dw_fused(int bits, int64_t m, int64_t n, int64_t k) {
@@ -187,11 +187,11 @@ bool mx_loss_dw_fused(int bits, int64_t m, int64_t n, int64_t k) {
   return r.variant == TILES_BF16 && r.splits == 1 && r.bn >= 128 && up_div(n, 128) * up_div(k, 128) <= kTileSlice;
 }
 
-hipError_t launch_mx_loss_dw(const ProductArgs& a, const float* scale, hipStream_t stream) {
+hipError_t launch_mx_loss_dw(const ProductArgs& a, const float* factor, hipStream_t stream) {
   const int64_t es = a.c_type == COSTA_REAL_F32 ? 4 : 2;
   const Epilogue e{a.c, a.c_rs, 1, a.c_type, a.c_rs % 4 == 0 && (uintptr_t)a.c % (4 * es) == 0, a.alpha, a.beta};
   const Args p{a.m, a.n, a.k, MxView{}, a.b, a.real, a.a_rs, a.a_cs, e, 0};
-  return a.b.bits == 4 ? launch_dw<4>(p, scale, stream) : launch_dw<8>(p, scale, stream);
+  return a.b.bits == 4 ? launch_dw<4>(p, factor, stream) : launch_dw<8>(p, factor, stream);
 }
 
 }  // namespace costa

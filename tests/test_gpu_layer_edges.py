@@ -1,0 +1,83 @@
+"""The operators around products on the GPU, at the edges of what they say."""
+import numpy as np
+import pytest
+import torch
+
+import test_gpu_loss as L
+
+C = pytest.importorskip("paper_2106_06601_amd")
+pytestmark = pytest.mark.gpu
+U = L.U
+
+
+def bf16(x):
+    return torch.from_numpy(x).to(torch.float32).to(torch.bfloat16)
+
+
+@pytest.mark.parametrize("m,n,k", [(20, 4097, 40), (64, 1025, 256), (90, 4097, 7), (300, 8193, 136), (1000, 4097, 520)])
+@pytest.mark.parametrize("dtype,bits", [("f32", 8), ("bf16", 4), ("f16", 8)])
+@pytest.mark.parametrize("factors", [True, False])
+def test_the_target_s_part_of_a_gradient_in_bfloat16_is_whole(m, n, k, dtype, bits, factors):
+    """Rows of zeros over 2^a + 1 words: every word has 1 / n, and as a part of d (1 - 1 / n) the target's element
+    is -1 and each other one 2^-a, which bfloat16 holds (the logits' and lse's roundings, some 2^-20, round
+    off).  So dX is off by its sums in 32 bits alone, and is the rounded one of the formula in 64 bits
+    wherever those do not reach another rounding."""
+    c = L.Case(m, n, k, dtype, bits)
+    c.x.zero_()
+    t = np.arange(m) * 7 % n
+    t[::5] = -1
+    d = c.d.numpy().astype(np.float64) if factors else np.ones(m)
+    x, target = c.x.cuda(), torch.from_numpy(t).cuda()
+    loss, lse = torch.zeros(m).cuda(), torch.zeros(m).cuda()
+    C.costa_mx_loss(1.0, x, c.wq, target, loss, lse)
+    DX = torch.full((m, k), 7.0).bfloat16().cuda()
+    C.costa_mx_loss_backward(0.75, x, c.wq, target, lse, c.d.cuda() if factors else None, WT=c.wtq, dX=DX)
+    g = np.full((m, n), 1.0 / n)
+    g[np.arange(m), np.maximum(t, 0)] -= 1
+    g *= np.where(t >= 0, d, 0)[:, None]
+    want = 0.75 * (g @ c.wt.T)
+    # a factor off by 2^-20 / n of itself and 8 * 2^-24; sums of n, and the pieces'
+    off = (2 * (n / 32 + 12) + 8 + 8 + n / 256) * U * 0.75 * (np.abs(g) @ np.abs(c.wt).T)
+    low, high = bf16(want - off), bf16(want + off)
+    known = (low == high).numpy()
+    assert known.mean() > 0.8
+    assert (DX.cpu() == low).numpy()[known].all()
+
+
+@pytest.mark.parametrize("m", [9, 100, 300])
+@pytest.mark.parametrize("spread", [8.0, 40.0, 1000.0])
+@pytest.mark.parametrize("size", [1.0, 1e-30, 1e-40, 1e30])
+def test_sure_rows_and_odd_factors_in_bfloat16(m, spread, size):
+    """Rows from unsure to sure of their target and of another word; factors of all sizes, 0 and subnormal
+    ones among them."""
+    n, k = 3000, 32
+    c = L.Case(m, n, k, "bf16", 8, gain=spread)
+    t = np.where(np.arange(m) % 3, c.L.argmax(1), np.arange(m) % n)
+    c.target[:] = torch.from_numpy(t)
+    c.__dict__.update(counts=np.ones(m, bool), at=t)
+    c.d *= size
+    c.d[::4] = 0
+    dx, ex, _, _ = c.gradients(True, np.zeros((n, k)))
+    DX = torch.full((m, k), 7.0).bfloat16().cuda()
+    C.costa_mx_loss_backward(1.0, c.x.cuda(), c.wq, c.target.cuda(), torch.from_numpy(c.lse.astype(np.float32)).cuda(), c.d.cuda(),
+                             WT=c.wtq, dX=DX)
+    # (sums of the smallest factors end below the floats' own steps: 2^-149 a term, 2^-133 the result's)
+    least = n * 2.0**-149 * (1 + np.abs(c.wt).max()) + L.TINY["bf16"]
+    assert (np.abs(L.wide(DX) - dx) <= ex + L.HALF["bf16"] * np.abs(dx) + least).all()
+
+
+def test_a_factor_that_is_not_finite_stays_in_its_row():
+    m, n, k = 100, 3000, 64
+    c = L.Case(m, n, k, "bf16", 4)
+    c.target[:] = torch.arange(m) * 11 % n
+    c.__dict__.update(counts=np.ones(m, bool), at=c.target.numpy())
+    dx, ex, _, _ = c.gradients(True, np.zeros((n, k)))
+    d = c.d.clone()
+    d[7], d[8] = float("inf"), float("nan")
+    DX = torch.full((m, k), 7.0).bfloat16().cuda()
+    C.costa_mx_loss_backward(1.0, c.x.cuda(), c.wq, c.target.cuda(), torch.from_numpy(c.lse.astype(np.float32)).cuda(), d.cuda(),
+                             WT=c.wtq, dX=DX)
+    fine = np.ones(m, bool)
+    fine[[7, 8]] = False
+    assert (np.abs(L.wide(DX) - dx) <= ex + L.HALF["bf16"] * np.abs(dx) + L.TINY["bf16"])[fine].all()
+    assert np.isnan(L.wide(DX)[8]).all() and not np.isfinite(L.wide(DX)[7]).any()
