@@ -149,7 +149,7 @@ int source_of(costa_real type) { return type == COSTA_REAL_BF16 ? SRC_BF16 : typ
 }  // namespace
 
 bool mx_adapted_fused(costa_real type, int bits, int64_t m, int64_t n, int64_t k) {
-  if (k == 0 || m < 1024) return false;
+  if (n == 0 || k == 0 || m < 1024) return false;
   const ProductPlan r = plan_product(source_of(type), true, bits, m, n, k);
   return r.variant == TILES_BF16 && r.splits == 1 && r.bn >= 128 && up_div(m, r.bm) * up_div(n, r.bn) <= kTileSlice;
 }

@@ -158,7 +158,7 @@ Args args_of(const ProductArgs& a, const Epilogue& e) {
 }  // namespace
 
 bool mx_loss_fused(costa_real type, int bits, int64_t m, int64_t n, int64_t k) {
-  if (k == 0) return false;
+  if (m == 0 || n == 0 || k == 0) return false;  // (no tiles: nothing to launch)
   const ProductPlan r = plan_product(source_of(type), true, bits, m, n, k);
   // (tiles of 128 columns and more, whole sums: where there are fewer the logits are few, too)
   return r.variant == TILES_BF16 && r.splits == 1 && r.bn >= 128 && up_div(m, 128) * up_div(n, 128) <= kTileSlice;

@@ -447,6 +447,10 @@ hipError_t hipLaunchKernel(const void* f, dim3 grid, dim3, void** args, size_t, 
     before_launch = nullptr;
     call();
   }
+  if (grid.x == 0 || grid.y == 0 || grid.z == 0) {
+    fault("a launch of no workgroups: " + name);
+    return err(hipErrorInvalidConfiguration);
+  }
   if (name.find("costa_mover") != std::string::npos || name.find("costa_tiles") != std::string::npos) {
     const ArgTable table = arg<ArgTable>(args, 0);
     const Piece* pieces = arg<const Piece*>(args, 1);

@@ -81,3 +81,19 @@ def test_a_factor_that_is_not_finite_stays_in_its_row():
     fine[[7, 8]] = False
     assert (np.abs(L.wide(DX) - dx) <= ex + L.HALF["bf16"] * np.abs(dx) + L.TINY["bf16"])[fine].all()
     assert np.isnan(L.wide(DX)[8]).all() and not np.isfinite(L.wide(DX)[7]).any()
+
+
+@pytest.mark.parametrize("m,k", [(1, 64), (64, 64), (65, 8), (100, 64), (100, 128), (100, 129), (4096, 128), (300, 3000)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_a_loss_over_no_words(m, k, dtype):
+    """lse = log 0, no row counts; dX is a sum over nothing."""
+    x, target = torch.ones(m, k).to(L.TORCH[dtype]).cuda(), torch.zeros(m, dtype=torch.int64).cuda()
+    (_, w), (_, wt) = L.keep(np.ones((0, k), np.float32), 8), L.keep(np.ones((k, 0), np.float32), 8)
+    for size in (None, C.costa_mx_loss_workspace(m, 0, k, False)[0]):
+        loss, lse = torch.full((m,), 7.0).cuda(), torch.full((m,), 7.0).cuda()
+        ws = None if size is None else torch.empty(size, dtype=torch.uint8).cuda()
+        C.costa_mx_loss(1.0, x, w, target, loss, lse, workspace=ws)
+        assert (lse == -float("inf")).all() and not loss.any()
+        DX = torch.full((m, k), 7.0).to(L.TORCH[dtype]).cuda()
+        C.costa_mx_loss_backward(1.0, x, w, target, lse, None, WT=wt, dX=DX)
+        assert not DX.any()

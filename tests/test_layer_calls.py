@@ -1,0 +1,111 @@
+"""The calls around products on the CPU, as far as their launches: the library's host code over the
+stand-in of the HIP runtime (kernels are named and not run)."""
+import ctypes
+import itertools
+
+import pytest
+
+pytestmark = pytest.mark.spawns  # builds the stand-in
+
+F32, BF16, F16 = 1, 2, 3
+ROW = 1
+ROOM = 1 << 40  # bytes of workspace
+ref = lambda a: None if a is None else ctypes.byref(a)  # noqa: E731
+at = lambda k: k << 48  # noqa: E731  (addresses that nothing reads)
+
+
+@pytest.fixture(scope="module")
+def S():
+    import standin
+    S = standin.load()
+    S.lib.standin_tile_launches.argtypes = [ctypes.c_void_p, ctypes.c_int]
+    S.faults(), S.lib.standin_tile_launches(None, 0)
+    return S
+
+
+class Calls:
+    """Each call with operands of given sizes; `seen` has what the last one launched."""
+
+    def __init__(self, S, bits=8):
+        self.S, self.C, self.fmt = S, S.C, S.C.MX_FORMATS[bits]
+
+    def M(self, rows, cols, where, type):
+        return self.C.CostaMatrix(type, ROW, rows, cols, max(cols, 1), at(where))
+
+    def Q(self, rows, cols, where, fmt=None):
+        return self.C.CostaMx(self.fmt if fmt is None else fmt, rows, cols, at(where), at(where) + (1 << 47))
+
+    def done(self, status):
+        said = self.S.faults().decode()
+        tiles = self.S.lib.standin_tile_launches(None, 0)
+        self.empty = [s for s in said.splitlines() if "no workgroups" in s]
+        self.seen = [s.split(": ")[1] for s in said.splitlines() if "does not run" in s] + ["tiles_bf16"] * tiles
+        return status
+
+    def loss(self, m, n, k, type, room=ROOM):
+        return self.done(self.C._lib.costa_mx_loss(1.0, ref(self.M(m, k, 1, type)), ref(self.Q(n, k, 2)), at(3), at(4), at(5),
+                                                   at(20), room, None))
+
+    def loss_backward(self, m, n, k, type, out, x=True, w=True, room=ROOM):
+        return self.done(self.C._lib.costa_mx_loss_backward(
+            1.0, ref(self.M(m, k, 1, type)), ref(self.Q(n, k, 2)), at(3), at(5), None, ref(self.Q(k, n, 6) if x else None),
+            ref(self.M(m, k, 7, out) if x else None), ref(self.Q(k, m, 8, 1) if w else None), 0.5,
+            ref(self.M(n, k, 9, out) if w else None), at(20), room, None))
+
+    def adapted(self, m, n, k, count, rank, type, room=ROOM, V=True):
+        A, B = self.M(count * rank, k, 3, type), self.M(count * rank, n, 4, type)
+        a = self.C.CostaMxAdapters(count, rank, ctypes.pointer(A), ctypes.pointer(B), None, None)
+        return self.done(self.C._lib.costa_mx_product_adapted(
+            1.0, ref(self.M(m, k, 1, type)), ref(self.Q(n, k, 2)), ref(a), at(5), 0.5, ref(self.M(m, n, 6, type)),
+            ref(self.M(m, rank, 7, F32) if V else None), at(20), room, None))
+
+    def gradient(self, m, n, count, rank, type, room=ROOM):
+        a = self.C.CostaMxAdapters(count, rank, None, None, None, None)
+        return self.done(self.C._lib.costa_mx_adapter_gradient(
+            ref(a), at(5), ref(self.M(m, rank, 1, F32)), ref(self.M(m, n, 2, type)), 0.5, ref(self.M(count * rank, n, 6, type)),
+            at(20), room, None))
+
+    def norm(self, m, n, type):
+        return self.done(self.C._lib.costa_mx_norm(1e-5, ref(self.M(m, n, 1, type)), None, None, None, ref(self.M(m, n, 2, type)),
+                                                   ref(self.Q(m, n, 3)), at(4), None))
+
+    def norm_backward(self, m, n, type, room=ROOM):
+        return self.done(self.C._lib.costa_mx_norm_backward(
+            ref(self.M(m, n, 1, type)), ref(self.M(m, n, 2, type)), None, at(3), None, ref(self.M(m, n, 4, type)),
+            ref(self.M(1, n, 5, F32)), at(20), room, None))
+
+
+SIZES = [0, 1, 5, 8, 17, 64, 65, 128, 1000, 4096, 70000]
+
+
+@pytest.mark.parametrize("type", [F32, BF16, F16])
+def test_no_launch_is_empty(S, type):
+    """Sizes of nothing among others: a call succeeds and launches no grid without workgroups, which HIP refuses."""
+    c = Calls(S)
+
+    def fine(status):
+        assert status == c.C.SUCCESS, c.C.costa_last_error()
+        assert not c.empty
+
+    for m, n, k in itertools.product(SIZES, SIZES, SIZES):
+        if m * n * k > 1 << 36:
+            continue
+        fine(c.loss(m, n, k, type))
+        for out, x, w in ((type, True, True), (BF16, True, False), (F32, False, True)):
+            fine(c.loss_backward(m, n, k, type, out, x, w))
+        for count, rank in ((0, 3), (3, 0), (2, 20)):
+            fine(c.adapted(m, n, k, count, rank, type))
+    for m, n in itertools.product(SIZES, SIZES):
+        fine(c.norm(m, n, type))
+        fine(c.norm_backward(m, n, type))
+        for count, rank in ((0, 3), (3, 0), (2, 20), (40, 130)):
+            fine(c.gradient(m, n, count, rank, type))
+            fine(c.gradient(m, n, count, rank, type, room=0))
+
+
+def test_a_loss_over_no_words(S):
+    """Nothing but the join of no statistics, for products of every kind."""
+    for m, k, type in itertools.product((1, 64, 65, 100, 4096), (1, 8, 64, 128, 129, 5000), (F32, BF16, F16)):
+        c = Calls(S)
+        assert c.loss(m, 0, k, type) == c.C.SUCCESS
+        assert len(c.seen) == 1 and "loss_join" in c.seen[0], (m, k, type, c.seen)
