@@ -15,7 +15,9 @@
  *
  * Workspaces: device memory, 16-byte aligned, its contents neither needed nor kept.
  * The functions *_workspace say what a call has to have (`least`: with less it is
- * refused, INVALID_VALUE) and what it can use (`most`); either pointer may be NULL.
+ * refused, INVALID_VALUE) and what it can use (`most`); either pointer may be NULL.  In
+ * between, sums in 32 bits are split and ordered otherwise and a call is slower: results differ by
+ * those sums' roundings, no operand is held in fewer bits.
  */
 #ifndef COSTA_LAYER_H
 #define COSTA_LAYER_H
@@ -118,8 +120,8 @@ costa_status costa_mx_loss(float alpha, const costa_matrix* X, const costa_mx* W
  * with XT may be NULL, not both.  lse: what costa_mx_loss() gave.  Probabilities below 2^-126 are 0.
  * G is held in 32 bits, or, where dX and dW (those wanted) are BF16, in bfloat16: for dX alone a row as a part
  * of |dloss| (1 - p), p the target's probability, so that the target's element is -1 and rounds to itself; with
- * dW (where the vocabulary is large enough for whole tiles) as a part of the largest |dloss| of rows that
- * count.  The factors are in 32 bits and go back in before dX and dW are rounded. */
+ * dW (where m, n and k are large enough for whole tiles of both products, whatever the workspace) as a part of
+ * the largest |dloss| of rows that count.  The factors are in 32 bits and go back in before dX and dW are rounded. */
 costa_status costa_mx_loss_backward(float alpha, const costa_matrix* X, const costa_mx* W, const int64_t* target,
                                     const float* lse, const float* dloss, const costa_mx* WT, const costa_matrix* dX,
                                     const costa_mx* XT, float beta, const costa_matrix* dW, void* workspace,

@@ -414,6 +414,14 @@ costa_status check_loss(const costa_matrix* X, const costa_mx* W, const int64_t*
   return check_vector("target", target, X->rows, 8);
 }
 
+// Whether G, its types allowing it, is in bfloat16 where dW is wanted: both products take whole tiles of a piece as
+// large as the most workspace holds.  Not of the piece that a call's workspace holds: results would then have
+// more or fewer bits by the room that they were made in.
+bool bf16_with_dw(costa_real type, int bits, int xt_bits, int64_t m, int64_t n, int64_t k) {
+  const int64_t per = piece_columns(m, n, up16(piece_bytes(m, n, 4)), 2);
+  return mx_loss_fused(type, bits, m, per, k) && mx_loss_dw_fused(xt_bits, m, per, k);
+}
+
 ProductArgs logits_of(const costa_matrix* X, const MxView& w, int64_t first, int64_t n, float alpha) {
   ProductArgs p{};
   p.m = X->rows, p.n = n, p.k = X->cols;
@@ -563,10 +571,10 @@ extern "C" costa_status costa_mx_loss_backward(float alpha, const costa_matrix* 
     size_t left = workspace_bytes - up16((size_t)m * k * 4) - up16((size_t)m * 4);
     // half for G, half for the logits, where they are kept, and for what products split
     const size_t half = std::min(left / 32 * 16, up16(piece_bytes(m, n, 4)));
+    const bool bf16 = (!dX || dX->type == COSTA_REAL_BF16) && (!dW || dW->type == COSTA_REAL_BF16) &&
+                      (!dW || bf16_with_dw(X->type, w.bits, xt.bits, m, n, k));
     int64_t per = piece_columns(m, n, half, 2);
     bool fused = mx_loss_fused(X->type, w.bits, m, per, k);
-    const bool bf16 = (!dX || dX->type == COSTA_REAL_BF16) && (!dW || dW->type == COSTA_REAL_BF16) &&
-                      (!dW || (fused && mx_loss_dw_fused(xt.bits, m, per, k)));
     if (!bf16 || !fused) {
       per = piece_columns(m, n, half, 4);
       fused = mx_loss_fused(X->type, w.bits, m, per, k);

@@ -97,3 +97,25 @@ def test_a_loss_over_no_words(m, k, dtype):
         DX = torch.full((m, k), 7.0).to(L.TORCH[dtype]).cuda()
         C.costa_mx_loss_backward(1.0, x, w, target, lse, None, WT=wt, dX=DX)
         assert not DX.any()
+
+
+@pytest.mark.parametrize("m,n,k,bits", [(512, 8200, 1030, 4), (300, 8201, 1024, 8), (260, 2500, 520, 4), (600, 20001, 264, 4)])
+def test_gradients_have_the_same_precision_in_every_workspace(m, n, k, bits):
+    """dX and dW in bfloat16 of rows of zeros, so that G has the same bits however it is made: in another workspace
+    the sums in 32 bits come in another order, 2 (2 (n / 32 + 12) + 8) 2^-24 apart (1.4e-4 at most here, and mostly a
+    tenth of that), which moves one result of a hundred or so across the border of a step of 2^-8.  (G in 32 bits in
+    one of them and in bfloat16 in another one moves a quarter of them.)"""
+    c = L.Case(m, n, k, "bf16", bits)
+    x, target, lse = torch.zeros(m, k).bfloat16().cuda(), c.target.cuda(), torch.full((m,), float(np.log(n))).cuda()
+    least, most = C.costa_mx_loss_workspace(m, n, k, True)
+    got = []
+    for size in (most, least, least + (most - least) // 30, least + (most - least) // 3):
+        DX, DW = torch.zeros(m, k).bfloat16().cuda(), torch.zeros(n, k).bfloat16().cuda()
+        C.costa_mx_loss_backward(1.0, x, c.wq, target, lse, c.d.cuda(), WT=c.wtq, dX=DX, XT=c.xtq, dW=DW,
+                                 workspace=torch.full((size,), 0xFF, dtype=torch.uint8).cuda())
+        got.append((DX, DW))
+    for other in got[1:]:
+        for a, b in zip(got[0], other):
+            assert float((a != b).float().mean()) <= 0.05
+            a, b = a.float(), b.float()
+            assert ((a - b).abs() <= 2.0**-7 * torch.maximum(a.abs(), b.abs()) + 1e-3 * a.abs().mean()).all()

@@ -109,3 +109,17 @@ def test_a_loss_over_no_words(S):
         c = Calls(S)
         assert c.loss(m, 0, k, type) == c.C.SUCCESS
         assert len(c.seen) == 1 and "loss_join" in c.seen[0], (m, k, type, c.seen)
+
+
+@pytest.mark.parametrize("m,n,k", [(512, 8200, 1030), (260, 2500, 520), (4096, 65536, 4096), (2048, 20000, 2048), (300, 8201, 1024),
+                                   (70, 500, 100), (64, 8200, 1030)])
+def test_the_workspace_does_not_choose_the_precision(S, m, n, k):
+    """Whether G is in bfloat16 (with dW: its products' factor is in device memory) is the same for every room."""
+    c = Calls(S, 4)
+    least, most = c.C.costa_mx_loss_workspace(m, n, k, True)
+    for x in (True, False):
+        kinds = set()
+        for room in (least, least + (most - least) // 30, (least + most) // 2, most, ROOM):
+            assert c.loss_backward(m, n, k, BF16, BF16, x, True, room) == c.C.SUCCESS, c.C.costa_last_error()
+            kinds.add(any("tiles_loss_dw" in s for s in c.seen))
+        assert len(kinds) == 1
