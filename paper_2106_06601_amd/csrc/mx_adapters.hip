@@ -135,8 +135,9 @@ __global__ __launch_bounds__(256) void adapter_add_row(AdapterAddArgs p, int64_t
         for (int i = 0; i < 8; ++i) add[i] = fmaf(xr[j], b[i], add[i]);
       }
     }
+    if (rank > 0)  // (a sum over nothing is 0, whatever s)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += s * add[i];
+      for (int i = 0; i < 8; ++i) v[i] += s * add[i];
   }
   if (c >= p.n) return;
   if (p.c_type == COSTA_REAL_F32) put_scaled<SRC_F32>(p, row, c, v);
@@ -387,6 +388,7 @@ __global__ __launch_bounds__(256) void adapter_grad_tile(AdapterGradArgs p, int6
   for (int t = 0; t < RT; ++t)
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[t][e] = v4f{0, 0, 0, 0};
+  bool some = false;  // rows of the adapter
   for (int64_t from = first; r0 < rank && from < last; from += kListed) {
     int n = 0;
     for (int64_t at = from; at < min(from + kListed, last); at += 256) {
@@ -405,6 +407,7 @@ __global__ __launch_bounds__(256) void adapter_grad_tile(AdapterGradArgs p, int6
       __syncthreads();
     }
     if (n == 0) continue;
+    some = true;
     if (threadIdx.x < 128) list[n + threadIdx.x] = list[n - 1];
     __syncthreads();
     Raw8<SRC> z[8];
@@ -473,7 +476,7 @@ __global__ __launch_bounds__(256) void adapter_grad_tile(AdapterGradArgs p, int6
       if (c >= p.len) continue;
       float out[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) out[e] = r < rank ? scale * acc[t][e][q] : 0.0f;
+      for (int e = 0; e < 8; ++e) out[e] = some && r < rank ? scale * acc[t][e][q] : 0.0f;  // (0, whatever the scale)
       if (p.parts) put8<SRC_F32>(p.parts + ((int64_t)blockIdx.z * p.at.count * p.at.rank + row) * p.len, c, p.len, out);
       else put_grad_typed(p, row, c, out);
     }

@@ -119,3 +119,37 @@ def test_gradients_have_the_same_precision_in_every_workspace(m, n, k, bits):
             assert float((a != b).float().mean()) <= 0.05
             a, b = a.float(), b.float()
             assert ((a - b).abs() <= 2.0**-7 * torch.maximum(a.abs(), b.abs()) + 1e-3 * a.abs().mean()).all()
+
+
+@pytest.mark.parametrize("m,how", [(40, "few"), (40, "none"), (3000, "few"), (3000, "none")])
+@pytest.mark.parametrize("odd", [float("inf"), float("nan")])
+def test_scales_that_are_not_finite_stay_with_their_rows(m, how, odd):
+    """An adapter without rows has a gradient of beta G whatever its scale; one whose rows are all in one part of a
+    split sum gets that part's; one of rank 0 adds nothing to its rows."""
+    n, k, count, rank = 130, 256, 4, 8
+    rng = np.random.default_rng(m)
+    index = rng.integers(0, 2, m)
+    index[index == 1] = 3
+    if how == "few":
+        index[:5] = 1
+    index[5:8] = 2
+    scales, ranks = torch.tensor([1.0, odd, odd, 0.5]), torch.tensor([8, 8, 0, 3], dtype=torch.int32)
+    new = lambda *s: torch.from_numpy(rng.standard_normal(s).astype(np.float32)).cuda()  # noqa: E731
+    A, B, x, v = new(count, rank, k), new(count, rank, n), new(m, k), new(m, rank)
+    ad = C.MxAdapters(A, B, ranks.cuda(), scales.cuda())
+    at = torch.from_numpy(index.astype(np.int32)).cuda()
+    for beta in (0.0, 2.0):
+        for size in C.costa_mx_adapter_gradient_workspace(m, k, count, rank):
+            G = torch.full((count, rank, k), 3.0 if beta else float("nan")).cuda()
+            C.costa_mx_adapter_gradient(ad, at, v, x, beta, G, workspace=torch.full((size,), 0xFF, dtype=torch.uint8).cuda())
+            assert (G[2] == 3 * beta).all() and (G[3, 3:] == 3 * beta).all() and torch.isfinite(G[0]).all() and torch.isfinite(G[3]).all()
+            if how == "none":
+                assert (G[1] == 3 * beta).all()
+            else:
+                assert (torch.isnan(G[1]) if odd != odd else torch.isinf(G[1])).all()
+    w = C.MxMatrix.empty(8, n, k)
+    C.costa_mx_quantize(1.0, new(n, k), w)
+    y, plain = torch.zeros(m, n).cuda(), torch.zeros(m, n).cuda()
+    C.costa_mx_product_adapted(1.0, x, w, ad, at, 0.0, y)
+    C.costa_mx_product_adapted(1.0, x, w, ad, torch.full_like(at, -1), 0.0, plain)
+    assert torch.equal(y[5:8], plain[5:8]) and torch.isfinite(y[8:]).all()
