@@ -311,11 +311,18 @@ extern "C" costa_status costa_mx_adapted_workspace(int64_t m, int64_t n, int64_t
     CHECKED(check_dims("X", m, k));
     if (rank < 0) return fail(COSTA_ERROR_INVALID_VALUE, "negative rank");
     if (rank > kRankMax) return fail(COSTA_ERROR_NOT_SUPPORTED, "a rank above 256");
-    const size_t v = up16((size_t)m * rank * 4) + mx_spread_bytes(m, rank);
-    const bool sums = m > 0 && n > 0 && k > 0;
-    give(least, v + (sums ? sums_bytes(std::min<int64_t>(m, 256), n) : 0));
-    give(most, v + std::max(sums ? split_bytes(slice_rows(m, n), n, k) : 0,
-                            (size_t)m * rank * 4 * mx_adapter_dots_parts(m, k, rank)));
+    // what calls of these sizes do, of whatever types: spread v, or keep sums
+    bool spreads = false, sums = false;
+    for (const costa_real type : {COSTA_REAL_F32, COSTA_REAL_BF16, COSTA_REAL_F16})
+      for (const int bits : {4, 8}) {
+        const bool fused = mx_adapted_fused(type, bits, m, n, k);
+        spreads |= fused;
+        sums |= !fused && m > 0 && n > 0 && k > 0;
+      }
+    const size_t v = up16((size_t)m * rank * 4), spread = spreads ? mx_spread_bytes(m, rank) : 0;
+    give(least, v + std::max(spread, sums ? sums_bytes(std::min<int64_t>(m, 256), n) : 0));
+    give(most, v + spread + std::max(sums ? split_bytes(slice_rows(m, n), n, k) : 0,
+                                     (size_t)m * rank * 4 * mx_adapter_dots_parts(m, k, rank)));
     return COSTA_SUCCESS;
   });
 }

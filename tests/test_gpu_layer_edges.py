@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+import test_gpu_adapters as AD
 import test_gpu_loss as L
 
 C = pytest.importorskip("paper_2106_06601_amd")
@@ -153,3 +154,51 @@ def test_scales_that_are_not_finite_stay_with_their_rows(m, how, odd):
     C.costa_mx_product_adapted(1.0, x, w, ad, at, 0.0, y)
     C.costa_mx_product_adapted(1.0, x, w, ad, torch.full_like(at, -1), 0.0, plain)
     assert torch.equal(y[5:8], plain[5:8]) and torch.isfinite(y[8:]).all()
+
+
+def guarded(size):
+    """A workspace of so many bytes, with more behind it that a call has no part in."""
+    room = torch.full((size + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+    return room, room[:size]
+
+
+@pytest.mark.parametrize("m,n,k,count,rank", [(1, 40, 300, 3, 4), (61, 702, 1030, 6, 16), (333, 199, 1250, 5, 100), (900, 2000, 64, 3, 4),
+                                              (1023, 260, 520, 7, 64), (1024, 4096, 64, 2, 32), (1300, 1999, 40, 1, 100),
+                                              (2101, 10, 4161, 5, 70)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_no_call_writes_past_its_workspace(m, n, k, count, rank, dtype):
+    c = AD.Case(m, n, k, count, rank, dtype, 4, "mixed")
+    l = L.Case(m, n, k, dtype, 4)
+    x, index, target = c.x.cuda(), c.index.cuda(), l.target.cuda()
+    t = L.TORCH[dtype]
+
+    def check(sizes, call):
+        least, most = sizes
+        for size in (least, (least + (most - least) // 3) // 16 * 16 if most > least else least, most):
+            if size < least:
+                continue
+            room, ws = guarded(size)
+            call(ws)
+            assert (room[size:] == 0xA5).all()
+
+    v, ev, want, off = c.forward(1.0, 0.0, dtype)
+    for V in (None, torch.zeros(m, rank).cuda()):
+        y = torch.zeros(m, n, dtype=t).cuda()
+
+        def product(ws):
+            y.fill_(float("nan"))
+            C.costa_mx_product_adapted(1.0, x, c.wq, c.adapters, index, 0.0, y, V=V, workspace=ws)
+            assert (np.abs(L.wide(y) - want) <= off).all()
+
+        check(C.costa_mx_adapted_workspace(m, n, k, rank), product)
+    G, V = torch.zeros(count, rank, k).cuda(), torch.zeros(m, rank).cuda()
+    check(C.costa_mx_adapter_gradient_workspace(m, k, count, rank),
+          lambda ws: C.costa_mx_adapter_gradient(c.adapters, index, V, x, 0.0, G, workspace=ws))
+    loss, lse = torch.zeros(m).cuda(), torch.zeros(m).cuda()
+    check(C.costa_mx_loss_workspace(m, n, k, False), lambda ws: C.costa_mx_loss(1.0, l.x.cuda(), l.wq, target, loss, lse, workspace=ws))
+    DX, DW = torch.zeros(m, k, dtype=t).cuda(), torch.zeros(n, k, dtype=t).cuda()
+    for dx, dw in ((DX, None), (DX, DW), (None, DW)):
+        check(C.costa_mx_loss_workspace(m, n, k, True),
+              lambda ws: C.costa_mx_loss_backward(1.0, l.x.cuda(), l.wq, target, lse, None, WT=l.wtq, dX=dx, XT=l.xtq, dW=dw, workspace=ws))
+    H, D, dw, s = torch.ones(m, n, dtype=t).cuda(), torch.zeros(m, n, dtype=t).cuda(), torch.zeros(n).cuda(), torch.ones(m).cuda()
+    check(C.costa_mx_norm_workspace(m, n), lambda ws: C.costa_mx_norm_backward(H, H, None, s, D, dW=dw, workspace=ws))

@@ -123,3 +123,21 @@ def test_the_workspace_does_not_choose_the_precision(S, m, n, k):
             assert c.loss_backward(m, n, k, BF16, BF16, x, True, room) == c.C.SUCCESS, c.C.costa_last_error()
             kinds.add(any("tiles_loss_dw" in s for s in c.seen))
         assert len(kinds) == 1
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+def test_an_adapted_product_asks_for_what_it_uses(S, bits):
+    """The least workspace holds v and either 256 rows of sums or v spread, and calls of every type get by with it: v is
+    spread by products of 1024 rows and more alone."""
+    c, up16 = Calls(S, bits), lambda x: -(-x // 16) * 16
+    spreads = 0
+    for m, n, k, rank in itertools.product((1, 17, 300, 1000, 1023, 1024, 4096, 20000), (1, 130, 1999, 8192), (1, 64, 2501, 8192), (1, 16, 33, 256)):
+        least, most = c.C.costa_mx_adapted_workspace(m, n, k, rank)
+        v, sums, spread = up16(4 * m * rank), 4 * min(m, 256) * n, -(-m // 16) * -(-rank // 32) * 3072
+        assert least in ((v + sums,) if m < 1024 else (v + sums, v + spread, v + max(sums, spread))) and least <= most
+        for type in (F32, BF16, F16):
+            assert c.adapted(m, n, k, 3, rank, type, room=least, V=False) == c.C.SUCCESS, c.C.costa_last_error()
+            spreads += any("adapter_spread" in s for s in c.seen)
+            assert least >= v + (spread if any("adapter_spread" in s for s in c.seen) else sums)
+            assert c.adapted(m, n, k, 3, rank, type, room=least - 1, V=False) == c.C.INVALID_VALUE
+    assert spreads
