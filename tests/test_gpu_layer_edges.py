@@ -202,3 +202,31 @@ def test_no_call_writes_past_its_workspace(m, n, k, count, rank, dtype):
               lambda ws: C.costa_mx_loss_backward(1.0, l.x.cuda(), l.wq, target, lse, None, WT=l.wtq, dX=dx, XT=l.xtq, dW=dw, workspace=ws))
     H, D, dw, s = torch.ones(m, n, dtype=t).cuda(), torch.zeros(m, n, dtype=t).cuda(), torch.zeros(n).cuda(), torch.ones(m).cuda()
     check(C.costa_mx_norm_workspace(m, n), lambda ws: C.costa_mx_norm_backward(H, H, None, s, D, dW=dw, workspace=ws))
+
+
+@pytest.mark.parametrize("shape", [(900, 2000, 64, 3, 4), (1000, 4099, 300, 5, 4), (700, 3001, 129, 4, 33), (521, 2501, 1030, 2, 100)], ids=str)
+@pytest.mark.parametrize("dtype,bits", [("f32", 4), ("bf16", 8), ("f16", 4)])
+@pytest.mark.parametrize("how", ["runs", "mixed"])
+def test_sums_that_go_by_slices_of_rows(shape, dtype, bits, how):
+    """Fewer rows than the products' own tiles take, and a workspace that does not hold their sums: X, the index, V and C
+    are each at the slice's first row, and the sums' room is used again.  Within the bounds of the whole, which
+    count any order of the sums (a slice may be split otherwise than the whole)."""
+    m, n, k, count, rank = shape
+    c = AD.Case(m, n, k, count, rank, dtype, bits, how)
+    out = "f32" if how == "mixed" else dtype
+    v, ev, want, off = c.forward(-0.5, 0.25, out)
+    X, index = AD.strided(c.x, dtype, k + 3), c.index.cuda()
+    least, most = C.costa_mx_adapted_workspace(m, n, k, rank)
+    sums, kept = 4 * n, -(-4 * m * rank // 16) * 16  # a row's; v's
+    slices = []
+    for size in (least, least + 100 * sums, least + 300 * sums, most):
+        for V in (None, AD.strided(np.full((m, rank), np.nan), "f32", rank + 2)):
+            room = size - (kept if V is None else 0)
+            slices.append(-(-m // (room // sums)))
+            y, ws = AD.strided(c.c0, out, n + 5), torch.full((size,), 0xFF, dtype=torch.uint8).cuda()
+            C.costa_mx_product_adapted(-0.5, X, c.wq, c.adapters, index, 0.25, y, V=V, workspace=ws)
+            assert (np.abs(L.wide(y) - want) <= off).all()
+            assert (y._base[:, n:] == 77).all()
+            if V is not None:
+                assert (np.abs(L.wide(V) - v) <= ev).all()
+    assert slices[0] > 1 and slices[1] > 1 and slices[-1] == 1

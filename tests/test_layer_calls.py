@@ -141,3 +141,28 @@ def test_an_adapted_product_asks_for_what_it_uses(S, bits):
             assert least >= v + (spread if any("adapter_spread" in s for s in c.seen) else sums)
             assert c.adapted(m, n, k, 3, rank, type, room=least - 1, V=False) == c.C.INVALID_VALUE
     assert spreads
+
+
+@pytest.mark.parametrize("m,n,k,rank", [(900, 2000, 64, 4), (1000, 4099, 300, 4), (700, 3001, 129, 33), (521, 2501, 1030, 100)])
+def test_slices_of_rows_are_products_of_their_own(S, m, n, k, rank):
+    """Each with operands that begin at its first row, one after another over all of them."""
+    import numpy as np
+    c, out = Calls(S, 4), np.zeros((64, 10), np.int64)
+    least, most = c.C.costa_mx_adapted_workspace(m, n, k, rank)
+    for type in (F32, BF16, F16):
+        for room in (least, least + 400 * n, most):
+            A, B = c.M(3 * rank, k, 3, type), c.M(3 * rank, n, 4, type)
+            a = c.C.CostaMxAdapters(3, rank, ctypes.pointer(A), ctypes.pointer(B), None, None)
+            st = c.C._lib.costa_mx_product_adapted(1.0, ref(c.M(m, k, 1, type)), ref(c.Q(n, k, 2)), ref(a), at(5), 0.0,
+                                                   ref(c.M(m, n, 6, type)), None, at(20), room, None)
+            assert st == c.C.SUCCESS
+            S.faults()
+            got = out[:S.lib.standin_tile_launches(out.ctypes.data, len(out))].tolist()
+            per, row, es = (room - -(-4 * m * rank // 16) * 16) // (4 * n), 0, 4 if type == F32 else 2
+            for rows, cols, _, _, _, _, x, _, _, to in got:
+                assert (cols, x, to) == (n, at(1) + row * k * es, at(20) + -(-4 * m * rank // 16) * 16)
+                assert rows == min(per, m - row)
+                row += rows
+            # (up to 64 rows at the end are no tiles' but the kernels' for few rows)
+            assert row == m or (row == m // per * per and m - row <= 64)
+            assert (row < m or len(got) > 1) == (per < m)
