@@ -230,3 +230,45 @@ def test_sums_that_go_by_slices_of_rows(shape, dtype, bits, how):
             if V is not None:
                 assert (np.abs(L.wide(V) - v) <= ev).all()
     assert slices[0] > 1 and slices[1] > 1 and slices[-1] == 1
+
+
+# Relative to the whole gradient.  Eight results follow one another (y1, z, h2, y2 and, back, those of y2, h2, y1 and x), each
+# rounded by at most half a step h of its elements: 2^-8, 2^-11, spread evenly over it at the worst, so h / sqrt(3) of its
+# norm; independent of one another, sqrt(8 / 3) h together, and the norms and the softmax between them
+# pass on no more than some 2.5 times as much: 4 h.
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("tokens,inputs,words,requests,rank", [(130, 200, 1003, 3, 20), (1100, 512, 2500, 4, 16), (300, 256, 9000, 2, 32)])
+def test_a_training_step_is_off_by_its_roundings(dtype, tokens, inputs, words, requests, rank):
+    import test_gpu_layer_step as T
+    import adapted_layer as E
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(tokens + 1)
+    M = E.Model(inputs, words, requests, rank, dtype, gen)
+    x = torch.randn(tokens, inputs, generator=gen, device="cuda").to(dtype)
+    index = torch.randint(-1, requests, (tokens,), generator=gen, device="cuda").to(torch.int32)
+    target = torch.randint(0, words, (tokens,), generator=gen, device="cuda")
+    loss, grads = M.step(x, index, target)
+    want, wants = T.chain(M, x, index.cpu().numpy(), target.cpu().numpy())
+    half = torch.finfo(dtype).eps / 2
+    assert abs(float(loss) - want) <= 4 * half * want
+    off = {name: T.off(grads[name], wants[name]) / half for name in wants}
+    assert max(off.values()) <= 4, off
+
+
+@pytest.mark.parametrize("m,n", [(5, 1023), (9, 2501), (3, 8191), (2, 16400), (700, 33)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("bits", [4, 8])
+def test_a_norm_s_few_bits_alone_are_the_same(m, n, dtype, bits):
+    """Codes, scales and what pads them, with H, Y and rstd beside them and without."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(m * n)
+    new = lambda *s: torch.randn(*s, generator=gen, device="cuda").to(L.TORCH[dtype])  # noqa: E731
+    x, r, w = new(m, n), new(m, n), new(n)
+    kept = []
+    for more in (dict(), dict(H=torch.empty_like(x), Y=torch.empty_like(x), rstd=torch.empty(m, device="cuda"))):
+        q = C.MxMatrix(bits, m, n, *(torch.full((k,), 0xA5, dtype=torch.uint8, device="cuda") for k in C.costa_mx_sizes(bits, m, n)))
+        C.costa_mx_norm(1e-5, x, w, R=r, Q=q, **more)
+        kept.append(q)
+    assert torch.equal(kept[0].data, kept[1].data) and torch.equal(kept[0].scales, kept[1].scales)
+    pad = -(-n // 32)
+    assert not kept[0].scales.view(m, -1)[:, pad:].any()
