@@ -117,7 +117,10 @@ costa_status costa_mx_loss(float alpha, const costa_matrix* X, const costa_mx* W
  *     dW <- alpha G^T X'^ + beta dW    X' = XT^T, XT = mx(X^T), k x m
  *
  * dloss (NULL: ones): m floats, the gradient that reaches each row's loss.  dX with WT and dW
- * with XT may be NULL, not both.  lse: what costa_mx_loss() gave.  Probabilities below 2^-126 are 0.
+ * with XT may be NULL, not both.  lse: what costa_mx_loss() gave.  Probabilities below 2^-126 are 0.  lse is one
+ * float: its rounding, up to 2^-24 |lse|, is a factor exp(that) of all of a row's probabilities, and an error as large
+ * of the target's element p - 1, which of a row that is sure up to about that much keeps no digit (the row's loss
+ * does: it is not made from lse).
  * G is held in 32 bits, or, where dX and dW (those wanted) are BF16, in bfloat16: for dX alone a row as a part
  * of |dloss| (1 - p), p the target's probability, so that the target's element is -1 and rounds to itself; with
  * dW (where m, n and k are large enough for whole tiles of both products, whatever the workspace) as a part of

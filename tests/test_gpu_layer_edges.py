@@ -272,3 +272,40 @@ def test_a_norm_s_few_bits_alone_are_the_same(m, n, dtype, bits):
     assert torch.equal(kept[0].data, kept[1].data) and torch.equal(kept[0].scales, kept[1].scales)
     pad = -(-n // 32)
     assert not kept[0].scales.view(m, -1)[:, pad:].any()
+
+
+@pytest.mark.parametrize("m", [3, 100])
+@pytest.mark.parametrize("top,gap", [(112.0, 14.0), (96.0, 6.0), (-96.0, 12.0), (448.0, 14.0)])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_what_lse_s_rounding_costs_a_sure_row(m, top, gap, out):
+    """Logits that are whole numbers, `gap` below the target's, and weights behind that pick one word each, so that dX is
+    G: a probability is off by 2^-24 |lse| of itself, the target's element by as much, and some 8 * 2^-24 (1 + gap) of
+    the exponential's; the loss by its own last places alone."""
+    n, k = 40, 40
+    w, x = np.zeros((n, k), np.float32), np.zeros((m, k), np.float32)
+    x[:, 0], x[:, 32] = top, gap
+    w[:, 0], w[1:, 32] = 1.0, -1.0  # (two blocks of a stored row)
+    values, wq = L.keep(w, 8)
+    assert (values == w).all()
+    one, wtq = L.keep(np.eye(k, n, dtype=np.float32), 8)
+    assert (one == np.eye(k, n)).all()
+    logits = x.astype(np.float64) @ values.T
+    assert (logits[:, 0] == top).all() and (logits[:, 1:] == top - gap).all()
+    rest = (n - 1) * np.exp(-gap)
+    loss, lse, target = torch.zeros(m).cuda(), torch.zeros(m).cuda(), torch.zeros(m, dtype=torch.int64).cuda()
+    X = torch.from_numpy(x).cuda()
+    C.costa_mx_loss(1.0, X, wq, target, loss, lse)
+    want = np.log1p(rest)
+    # The sum 1 + rest, below 2, is of 40 exponentials: up to 15 additions in a lane, 6 between lanes and 3 between waves, each
+    # off by 2^-24 at most; the exponentials by 8 * 2^-24 (1 + gap) of themselves; the logarithm by two steps of its
+    # result, below 1.
+    assert (np.abs(L.wide(loss) - want) <= (24 + 8 * (1 + gap) * rest + 2) * U).all()
+    DX = torch.zeros(m, k).to(L.TORCH[out]).cuda()
+    C.costa_mx_loss_backward(1.0, X, wq, target, lse, None, WT=wtq, dX=DX)
+    g = np.full(n, np.exp(-gap) / (1 + rest))
+    g[0] = -rest / (1 + rest)
+    off = U * abs(top + want) + 8 * U * (1 + gap)
+    p = np.where(np.arange(n) == 0, 1.0, np.abs(g))
+    # (in bfloat16: G's half step of words that are not the target, and dX's)
+    halves = 0 if out == "f32" else 2 * L.HALF[out]
+    assert (np.abs(L.wide(DX) - g) <= p * off * (1 + halves) + (halves + L.HALF[out]) * np.abs(g)).all()
