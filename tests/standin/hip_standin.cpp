@@ -440,7 +440,7 @@ void __hipRegisterFunction(void**, const void* host, char*, const char* name, un
 }
 void __hipRegisterVar(void**, void* var, char*, char*, int, size_t size, int, int) { symbols[var] = {size, nullptr}; }
 
-hipError_t hipLaunchKernel(const void* f, dim3 grid, dim3, void** args, size_t, hipStream_t stream) {
+hipError_t hipLaunchKernel(const void* f, dim3 grid, dim3 block, void** args, size_t, hipStream_t stream) {
   const std::string name = kernels[f];
   if (before_launch) {
     void (*const call)() = before_launch;
@@ -449,6 +449,10 @@ hipError_t hipLaunchKernel(const void* f, dim3 grid, dim3, void** args, size_t, 
   }
   if (grid.x == 0 || grid.y == 0 || grid.z == 0) {
     fault("a launch of no workgroups: " + name);
+    return err(hipErrorInvalidConfiguration);
+  }
+  if ((uint64_t)grid.x * block.x >> 32 || grid.y > 65535 || grid.z > 65535) {
+    fault("a launch past what a grid holds: " + name);
     return err(hipErrorInvalidConfiguration);
   }
   if (name.find("costa_mover") != std::string::npos || name.find("costa_tiles") != std::string::npos) {

@@ -11,7 +11,7 @@ F32, BF16, F16 = 1, 2, 3
 ROW = 1
 ROOM = 1 << 40  # bytes of workspace
 ref = lambda a: None if a is None else ctypes.byref(a)  # noqa: E731
-at = lambda k: k << 48  # noqa: E731  (addresses that nothing reads)
+at = lambda k: k << 56  # noqa: E731  (addresses that nothing reads)
 
 
 @pytest.fixture(scope="module")
@@ -33,7 +33,7 @@ class Calls:
         return self.C.CostaMatrix(type, ROW, rows, cols, max(cols, 1), at(where))
 
     def Q(self, rows, cols, where, fmt=None):
-        return self.C.CostaMx(self.fmt if fmt is None else fmt, rows, cols, at(where), at(where) + (1 << 47))
+        return self.C.CostaMx(self.fmt if fmt is None else fmt, rows, cols, at(where), at(where) + (1 << 55))
 
     def done(self, status):
         said = self.S.faults().decode()
@@ -166,3 +166,28 @@ def test_slices_of_rows_are_products_of_their_own(S, m, n, k, rank):
             # (up to 64 rows at the end are no tiles' but the kernels' for few rows)
             assert row == m or (row == m // per * per and m - row <= 64)
             assert (row < m or len(got) > 1) == (per < m)
+
+
+LONG = [(2**31 - 1, 1, 8), (2**31 - 1, 40, 64), (1, 2**31 - 1, 64), (64, 2**28, 300), (300, 2**28, 64), (5000, 2**30, 8), (2**30, 3, 256),
+        (100, 100, 2**31 - 1), (2**28, 1000, 100), (4096, 2**28, 4096), (2**24, 2**24, 8)]
+
+
+@pytest.mark.parametrize("m,n,k", LONG)
+@pytest.mark.parametrize("type", [F32, BF16])
+def test_launches_of_long_operands_hold_in_a_grid(S, m, n, k, type):
+    """(Workspaces of whole TiB for row sums and statistics: of what the calls ask for.)"""
+    c = Calls(S)
+
+    def fine(status):
+        assert status == c.C.SUCCESS, c.C.costa_last_error()
+
+    need = lambda name, *sizes: c.C._two_sizes(name, *sizes)[0]  # noqa: E731
+    if m * k < 1 << 42 and m * n < 1 << 46:  # (a backward pass goes by pieces of the vocabulary, some million of them for the longest)
+        fine(c.loss(m, n, k, type, need("costa_mx_loss_workspace", m, n, k, 0)))
+    for count, rank in ((2, 20), (3000, 256)):
+        if count * rank * max(n, k) < 1 << 46 and m * n < 1 << 42:
+            fine(c.adapted(m, n, k, count, rank, type, need("costa_mx_adapted_workspace", m, n, k, rank)))
+            fine(c.adapted(m, n, k, count, rank, type, c.C._two_sizes("costa_mx_adapted_workspace", m, n, k, rank)[1]))
+            fine(c.gradient(m, n, count, rank, type))
+    fine(c.norm(m, n, type))
+    fine(c.norm_backward(m, n, type))
