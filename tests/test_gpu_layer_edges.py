@@ -309,3 +309,59 @@ def test_what_lse_s_rounding_costs_a_sure_row(m, top, gap, out):
     # (in bfloat16: G's half step of words that are not the target, and dX's)
     halves = 0 if out == "f32" else 2 * L.HALF[out]
     assert (np.abs(L.wide(DX) - g) <= p * off * (1 + halves) + (halves + L.HALF[out]) * np.abs(g)).all()
+
+
+def apart(t, ld):
+    """A copy of t with rows `ld` elements apart (what lies between is not set)."""
+    far = torch.empty(t.shape[0], ld, dtype=t.dtype, device="cuda")[:, :t.shape[1]]
+    far.copy_(t)
+    return far
+
+
+@pytest.mark.parametrize("m,n,k,rank", [(70, 130, 264, 16), (2100, 100, 4161, 20), (1100, 2051, 300, 5)])
+def test_rows_whose_offsets_pass_32_bits(m, n, k, rank):
+    """Elements past the 2^32nd of a buffer, in each operand: the same bits as next to one another."""
+    ld, count = (2**32 // m + 4096) // 8 * 8 + 3, 3
+    c, l = AD.Case(m, n, k, count, rank, "bf16", 4, "mixed"), L.Case(m, n, k, "bf16", 4)
+    x, dy, index, target = c.x.cuda(), c.dy.cuda(), c.index.cuda(), l.target.cuda()
+    X = apart(x, ld)
+
+    y, V = torch.zeros(m, n).bfloat16().cuda(), torch.zeros(m, rank).cuda()
+    C.costa_mx_product_adapted(1.0, x, c.wq, c.adapters, index, 0.0, y, V=V)
+    Y = apart(y * 0, ld)
+    C.costa_mx_product_adapted(1.0, X, c.wq, c.adapters, index, 0.0, Y)
+    assert torch.equal(Y, y)
+    del Y
+    G, H = torch.zeros(count, rank, k).cuda(), torch.zeros(count, rank, k).cuda()
+    C.costa_mx_adapter_gradient(c.adapters, index, V, x, 0.0, G)
+    C.costa_mx_adapter_gradient(c.adapters, index, V, X, 0.0, H)
+    assert torch.equal(G, H)
+    FV = apart(V, ld)
+    H.zero_()
+    C.costa_mx_adapter_gradient(c.adapters, index, FV, x, 0.0, H)
+    assert torch.equal(G, H)
+    FV.zero_()
+    C.costa_mx_product_adapted(1.0, x, c.wq, c.adapters, index, 0.0, y, V=FV)
+    assert torch.equal(FV, V)
+    del FV
+
+    one, far = [(torch.zeros(m).cuda(), torch.zeros(m).cuda()) for _ in range(2)]
+    C.costa_mx_loss(1.0, x, l.wq, target, *one)
+    C.costa_mx_loss(1.0, X, l.wq, target, *far)
+    assert torch.equal(one[0], far[0]) and torch.equal(one[1], far[1])
+    DX = torch.zeros(m, k).bfloat16().cuda()
+    FX = apart(DX, ld)
+    C.costa_mx_loss_backward(1.0, x, l.wq, target, one[1], l.d.cuda(), WT=l.wtq, dX=DX)
+    C.costa_mx_loss_backward(1.0, X, l.wq, target, one[1], l.d.cuda(), WT=l.wtq, dX=FX)
+    assert torch.equal(DX, FX)
+
+    w, s, t = torch.rand(k).cuda(), torch.zeros(m).cuda(), torch.zeros(m).cuda()
+    want, got = torch.zeros_like(x), FX
+    C.costa_mx_norm(1e-5, x, w, R=DX, Y=want, rstd=s)
+    kept = DX.clone()
+    C.costa_mx_norm(1e-5, X, w, R=kept, Y=got, rstd=t)
+    assert torch.equal(want, got) and torch.equal(s, t)
+    a, b = [torch.zeros(k).cuda() for _ in range(2)]
+    C.costa_mx_norm_backward(want, x, w, s, kept, dW=a)
+    C.costa_mx_norm_backward(got, X, w, s, got, dW=b)
+    assert torch.equal(kept, got) and torch.equal(a, b)
