@@ -38,7 +38,8 @@ extern "C" {
  * each may be NULL, not all.  X, R, H, Y: rows x cols of one type; W: 1 x cols of
  * that type or F32; rstd: `rows` floats.  h goes on in 32 bits, y is not made of the
  * rounded one; squares are summed in 64 bits (no h is too large or too small).  H may be
- * X or R itself (the same matrix: data, ld and type).  eps: at least 2^-126, finite. */
+ * X or R itself (the same matrix: data, ld and type).  eps: at least 2^-126, finite.
+ * Without columns there is no mean: nothing is written, rstd neither. */
 costa_status costa_mx_norm(float eps, const costa_matrix* X, const costa_matrix* W, const costa_matrix* R,
                            const costa_matrix* H, const costa_matrix* Y, const costa_mx* Q, float* rstd,
                            hipStream_t stream);

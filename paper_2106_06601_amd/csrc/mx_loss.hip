@@ -112,7 +112,8 @@ __global__ __launch_bounds__(256) void loss_grad(LogitsPart p, int64_t vocabular
   }
 }
 
-// A wave has a row: the target's logit again, and from it how far the row is from sure.
+// A wave has a row: the target's logit again, and from it how far the row is from sure.  Bound by reading x and the
+// targets' rows of w: 4096 rows of 4096 in bfloat16 by 4 bits 9 us.
 template <int SRC, int BITS, bool WIDE>
 __global__ __launch_bounds__(256) void loss_factors(int64_t m, int64_t k, RowsView x, MxView w, float alpha,
                                                     const int64_t* target, const float* lse, const float* dloss,

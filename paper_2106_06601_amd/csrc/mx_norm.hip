@@ -107,10 +107,9 @@ __device__ inline void unit_y(const NormArgs& a, int64_t row, I unit, I cols, co
 
 // LANES lanes a row, PER units of each: a wave for rows of up to 2048 elements, so that no barrier
 // stands between a row's sum and its results, then four, then sixteen.  PER 0: rows of any length,
-// which are read twice.  Measured (h and 8 bits out of x and r): 16384x8192 in bfloat16 191 us, 4.95 TB/s of
-// what is read and written (a plain copy reaches 5.1; 187 us with y rounded twice more); 65536x512 41 us,
-// 5.7; 4096x16384 114 us, 4.1; 4096x20000 (twice read) 164 us, 3.5; 8192x8192 floats 181 us, 4.8; one row of 4096
-// 3.8 us.
+// which are read twice.  Measured (h and 8 bits out of x and r): 16384x8192 in bfloat16 191 us, 4.9 TB/s of
+// what is read and written (a plain copy reaches 5.1); in 4 bits 175 us, 5.0; 65536x512 41 to 44 us, 5.3 to 5.7;
+// 4096x16384 103 us, 4.6; 4096x20000 (twice read) 153 us, 3.8; 8192x8192 floats 175 us, 5.0; one row of 4096 3.8 us.
 template <int SRC, int WSRC, int LANES, int PER, bool WIDE>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_rows(NormArgs a) {
   constexpr int ROWS = LANES < 256 ? 256 / LANES : 1, KEPT = PER ? PER : 1;
@@ -188,8 +187,9 @@ __device__ inline float sum8(const float a[8], const float b[8]) {
 // A workgroup's rows share its lanes' part of dw, in registers; the parts are added by
 // another kernel.  Measured with dh: 8192x8192 in bfloat16 106 and 5 us, 4.9 TB/s of dy, h, dh and dx (four units
 // a lane, with a row's products and its next row in registers, 133 to 137: one wave of a SIMD had room); 8192x8192
-// floats 208 us, 5.15; 803x1023 floats without dh 6 and 4 us.  Rows of more than 16384 elements (floats:
-// 8192) are read twice and dw is summed in memory: 4096x20000 476 us.
+// floats 207 us, 5.2; 803x1023 floats without dh 6 and 4 us.  Rows of 8193 to 16384 elements of 16 bits do not
+// quite fit 128 registers (11 to 13 are spilled: 4096x16384 131 us, 4.1 TB/s); longer rows (floats: past 8192)
+// are read twice and dw is summed in memory: 4096x20000 464 us, 1.4.
 template <int SRC, int WSRC, int LANES, int PER, bool WIDE>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES, SRC == SRC_F32 ? 2 : 4) void norm_grad_rows(NormBackArgs a) {
   constexpr int ROWS = LANES < 256 ? 256 / LANES : 1, KEPT = PER ? PER : 1;
@@ -452,8 +452,8 @@ int64_t groups_of(RowPlan r, int64_t rows) { return up_div(rows, r.lanes < 256 ?
 
 hipError_t launch_mx_norm(const NormArgs& a, hipStream_t stream) {
   const RowPlan r = plan_row(a.q.data ? a.q.row_scales * 4 : up_div(a.cols, 8));
-  // as many workgroups as 2048 lanes for each CU are, which keep w (4096x16384 in bfloat16 109 us, with a
-  // workgroup for each row 127; 16384x8192 187 and 193)
+  // as many workgroups as 2048 lanes for each CU are, which keep w (4096x16384 in bfloat16 103 us, with a
+  // workgroup for each row 117; 16384x8192 191 and 196)
   const int64_t most = r.per > 0 ? kCUs * 2048 / std::max(r.lanes, 256) : kNormGroups;
   return launch_types<Forward>(a, r, std::min(groups_of(r, a.rows), most), stream);
 }
