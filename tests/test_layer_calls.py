@@ -133,7 +133,7 @@ def test_an_adapted_product_asks_for_what_it_uses(S, bits):
     spreads = 0
     for m, n, k, rank in itertools.product((1, 17, 300, 1000, 1023, 1024, 4096, 20000), (1, 130, 1999, 8192), (1, 64, 2501, 8192), (1, 16, 33, 256)):
         least, most = c.C.costa_mx_adapted_workspace(m, n, k, rank)
-        v, sums, spread = up16(4 * m * rank), 4 * min(m, 256) * n, -(-m // 16) * -(-rank // 32) * 3072
+        v, sums, spread = up16(4 * m * rank), 4 * min(m, 256) * n, -(-m // 16) * -(-rank // 32) * 3 * 1024
         assert least in ((v + sums,) if m < 1024 else (v + sums, v + spread, v + max(sums, spread))) and least <= most
         for type in (F32, BF16, F16):
             assert c.adapted(m, n, k, 3, rank, type, room=least, V=False) == c.C.SUCCESS, c.C.costa_last_error()
